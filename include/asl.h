@@ -9,7 +9,8 @@
  * Conventions for every entry point
  *  - Pointers named q_obs, k, v, lse*, u, p_head, s_all, scores, rank*, idx*, *_ptrs, state, out
  *    are DEVICE pointers owned by the caller.  `params` and `ctx` are HOST pointers.  The library
- *    owns only the workspace inside asl_ctx (allocated by asl_create; no allocation afterwards).
+ *    owns only the workspace inside asl_ctx (allocated by asl_create, and by asl_paged_reserve for the
+ *    paged cache; no allocation afterwards).
  *  - `stream` is a hipStream_t passed as void* (NULL = the default stream).  Calls enqueue work
  *    and return; they never synchronise.  Calls sharing a ctx share its workspace: calls of the
  *    same family must not overlap.  The families use disjoint workspace regions, so one call each
@@ -250,13 +251,126 @@ asl_status asl_layer_step(asl_ctx* ctx, const asl_params* params, const void* q_
  * before the next layer starts; the compacted KV of a layer is needed at decoding time. */
 asl_status asl_join(asl_ctx* ctx, void* stream);
 
+/* ---- The paged cache -------------------------------------------------------------------------
+ * What follows the pruning: the layers' compacted caches kept in pages, so that sequences can grow, share
+ * a prompt and end (Sec. 4.2 "Decoding"), and the attention that reads them.
+ *
+ *   k_pages, v_pages [n_pages, Hk, page_size, d] (any strides, the same for both; d contiguous), one pair per layer.
+ *   table   [n_rows, row_stride] int32: row r's page numbers in token order; token t of it is slot t % page_size of
+ *           page table[r][t / page_size].  One table serves all layers whose caches have the same lengths.
+ *   kv_len  [n_rows] int32: tokens of each row.
+ *   refs    [n_pages] int32: how many rows hold a page; 0 = free.
+ * All of them are the caller's device memory; all-zero kv_len and refs are an empty cache.  The host reads none of it:
+ * every call can be captured in a HIP graph and replayed while the lengths go on.  What is out of range there (a row, a
+ * length, a token, a page number) is left out by the kernels and raises bit 1 of the fault word (asl_device_fault).
+ * Calls of this family share a workspace: two of them on one ctx must not overlap; any other call may run beside them. */
+typedef struct {
+  int32_t n_q_heads;      /* Hq (asl_paged_attention)                       */
+  int32_t n_kv_heads;     /* Hk, Hq % Hk == 0                               */
+  int32_t head_dim;       /* d; rows are multiples of 16 bytes              */
+  int32_t dtype;          /* asl_dtype of pages, sources, q and out         */
+  int32_t page_size;      /* tokens of a page: a power of two, 16 to 4096   */
+  int32_t n_pages;
+  int32_t n_rows;         /* rows of table and kv_len                       */
+  int32_t row_stride;     /* entries of a table row; row_stride * page_size <= 2^30 */
+  int64_t stride_page;    /* element strides of k_pages and v_pages, 16-byte multiples */
+  int64_t stride_head;
+  int64_t stride_tok;
+  float scale;            /* logit scale; <= 0 means 1/sqrt(d)              */
+  int32_t flags;          /* 0                                              */
+} asl_pages;
+
+/* A dense source of tokens: k, v [Hk, n_src, d] with element strides (16-byte multiples). */
+typedef struct {
+  int32_t n_src;
+  int32_t idx_rows;       /* rows of idx: 1 (shared by the heads) or Hk     */
+  int64_t k_stride_head;
+  int64_t k_stride_tok;
+  int64_t v_stride_head;
+  int64_t v_stride_tok;
+} asl_rows;
+
+/* The queries see the keys of their own sequence only up to themselves. */
+#define ASL_ATTN_CAUSAL 1
+
+/* A batch of queries. */
+typedef struct {
+  int32_t n_seqs;
+  int32_t total_q;        /* query tokens of all sequences                  */
+  int32_t max_q_len;      /* at least the query tokens of any one sequence  } they choose how the work is cut, */
+  int32_t max_kv_len;     /* at least the keys of any one sequence          } not what is computed             */
+  int32_t n_groups;       /* groups of sequences that share a prefix, or 0  */
+  int32_t flags;          /* ASL_ATTN_CAUSAL or 0                           */
+  int64_t q_stride_tok;   /* element strides of q and out, 16-byte multiples; d contiguous */
+  int64_t q_stride_head;
+  int64_t out_stride_tok;
+  int64_t out_stride_head;
+} asl_attn;
+
+/* Allocates the paged calls' part of the workspace, for at most max_seqs sequences per call (<= 4096) and attention of
+ * total_q * Hq <= max_query_rows, d <= max_head_dim (<= 256).  Call it once before them, outside stream capture; again to
+ * change the limits.  A call past them, or without it, returns ASL_ENOMEM. */
+asl_status asl_paged_reserve(asl_ctx* ctx, int32_t max_seqs, int32_t max_query_rows, int32_t max_head_dim);
+
+/* Makes row rows[i] add[i] tokens longer (>= 0), for i < n: kv_len grows, and where the tokens need pages the row gets the
+ * lowest-numbered free ones, in the order of the list.  A row that does not get all its pages (too few are free, or more than
+ * 65536 in one call), and all behind it in the list, stay as they were: compare kv_len.  No row twice. */
+asl_status asl_pages_grow(asl_ctx* ctx, const asl_pages* pages, const int32_t* rows, const int32_t* add, int32_t n,
+                          int32_t* table, int32_t* kv_len, int32_t* refs, void* stream);
+
+/* Row children[i], which is empty (kv_len 0), becomes a continuation of row parents[i]: it shares the parent's full pages,
+ * and gets a free page (as in asl_pages_grow) into which the tokens of the parent's last, partly filled page are copied, in
+ * every one of n_layers layers.  Where no page is free for it, it and all behind it stay empty.  A parent may be named any
+ * number of times, a child once; a child is no parent of the same call.
+ *   k_ptrs, v_ptrs  DEVICE arrays of n_layers device pointers to each layer's k_pages (v_pages). */
+asl_status asl_pages_fork(asl_ctx* ctx, const asl_pages* pages, void* const* k_ptrs, void* const* v_ptrs, int32_t n_layers,
+                          const int32_t* parents, const int32_t* children, int32_t n, int32_t* table, int32_t* kv_len,
+                          int32_t* refs, void* stream);
+
+/* Rows rows[0 .. n-1] give their pages back and become empty; a page is free when no row holds it. */
+asl_status asl_pages_free(asl_ctx* ctx, const asl_pages* pages, const int32_t* rows, int32_t n, const int32_t* table,
+                          int32_t* kv_len, int32_t* refs, void* stream);
+
+/* Writes tokens into the LAST positions of table rows (asl_pages_grow makes room for them first): tokens cu[i] .. cu[i+1]-1
+ * become the last ones of row rows[i], for i < n.  Token j is k[:, j], or with idx [idx_rows, total] k[h, idx[h or 0][j]]:
+ * the appended tokens of a decoding step, or what asl_select_topk kept of a prompt (Alg. 1 step 12 into pages).
+ *   cu [n+1] int32 ascending, cu[0] = 0, cu[n] = total. */
+asl_status asl_pages_write(asl_ctx* ctx, const asl_pages* pages, const asl_rows* src, const void* k, const void* v,
+                           const int32_t* rows, const int32_t* cu, int32_t n, int32_t total, const int32_t* idx,
+                           const int32_t* table, const int32_t* kv_len, void* k_pages, void* v_pages, void* stream);
+
+/* The same from pages to pages: token j of row dst_rows[i] is token idx[h or 0][j] of row src_rows[i].  The rows written to
+ * hold no page that the call reads. */
+asl_status asl_pages_compact(asl_ctx* ctx, const asl_pages* pages, const int32_t* src_rows, const int32_t* dst_rows,
+                             const int32_t* cu, int32_t n, int32_t total, const int32_t* idx, int32_t idx_rows,
+                             const int32_t* table, const int32_t* kv_len, void* k_pages, void* v_pages, void* stream);
+
+/* out = softmax(scale q K^T) V over the pages of each query's sequence, for one query token per sequence or many.
+ *   q, out [total_q, Hq, d] by the strides in attn; sequence b has the query tokens cu_q[b] .. cu_q[b+1]-1 and the keys of
+ *          table row rows[b] (rows NULL: row b).  cu_q [n_seqs+1] int32 ascending, cu_q[0] = 0, cu_q[n_seqs] = total_q.
+ *   lse    [Hq, total_q] f32 out or NULL: natural log-sum-exp of each row's scaled, masked logits; what asl_score_layer
+ *          takes as `lse` when the queries are the window.
+ * With ASL_ATTN_CAUSAL the queries are the last tokens of their sequence and query i of n sees keys up to
+ * kv_len - n + i; without it every query sees every key (an encoder's states, of any length).  A query that sees no key
+ * gets out = 0 and lse = -Inf.
+ * n_groups > 0: sequences group_start[g] .. group_start[g+1]-1 have their first prefix_len[g] tokens in common (their rows
+ * begin with the same pages, or with copies); those are read once for all of the group's queries.  group_start [n_groups+1]
+ * int32 ascending from 0 to n_seqs.  The result is that of n_groups = 0 up to rounding.
+ * Products take bf16 (fp32) operands and are summed in fp32; softmax and sums are fp32 and of a fixed order.  Masked keys and
+ * slots behind a sequence's end may hold anything. */
+asl_status asl_paged_attention(asl_ctx* ctx, const asl_pages* pages, const asl_attn* attn, const void* q, const void* k_pages,
+                               const void* v_pages, const int32_t* rows, const int32_t* table, const int32_t* kv_len,
+                               const int32_t* cu_q, const int32_t* group_start, const int32_t* prefix_len, void* out,
+                               float* lse, void* stream);
+
 /* Health check (not a step of the paper's method).  Workgroups of a launch that wait for other workgroups of it do so with
  * a bounded number of polls, and raise a fault word in the workspace if their wait runs out (every wave still exits):
  *  - the first workgroup of a statistic, for the others' partial sums: it then reports no result (evaluated = 0) and leaves the
  *    state as it was;
  *  - the compacting wavefronts of a layer step of up to 12288 past tokens, for the selection of their head's tokens: each then
  *    leaves its part of k_out and v_out unwritten, while scores, idx_out, ranks and statistic are as ever.
- * This call waits for the device to go idle, returns the word in *fault_out (0 = no wait ever ran out) and clears it.
+ * Those set bit 0; bit 1 is set by the calls of the paged cache for numbers out of range in table, lengths and lists.
+ * This call waits for the device to go idle, returns the word in *fault_out (0 = nothing of the kind) and clears it.
  * Results of calls issued since the last check, k_out and v_out among them, are valid iff it reads 0; the calls themselves
  * have returned ASL_OK.  Synchronises: not for the hot loop. */
 asl_status asl_device_fault(asl_ctx* ctx, int32_t* fault_out);

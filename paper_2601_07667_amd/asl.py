@@ -17,11 +17,14 @@ ASL_OK, ASL_EINVAL, ASL_ENOMEM, ASL_EHIP, ASL_EUNSUPPORTED = 0, -1, -2, -3, -4
 ASL_BF16, ASL_F32 = 0, 1
 ASL_FLAG_GENERIC_SCORE = 1
 ASL_FLAG_DEFER_JOIN = 2
+ASL_ATTN_CAUSAL = 1
 _STATUS = {0: "ASL_OK", -1: "ASL_EINVAL", -2: "ASL_ENOMEM", -3: "ASL_EHIP", -4: "ASL_EUNSUPPORTED"}
 
 EXPORTS = ["asl_create", "asl_destroy", "asl_last_error", "asl_workspace_bytes", "asl_score_layer",
            "asl_window_lse", "asl_gather_kv_layers", "asl_rank_static", "asl_static_last_error", "asl_pool", "asl_rank", "asl_rankvar", "asl_rank_stat", "asl_select_topk", "asl_gather_kv",
-           "asl_gather_rows", "asl_layer_step", "asl_join", "asl_device_fault", "asl_profile_enable", "asl_profile_collect"]
+           "asl_gather_rows", "asl_layer_step", "asl_join", "asl_device_fault", "asl_profile_enable", "asl_profile_collect",
+           "asl_paged_reserve", "asl_pages_grow", "asl_pages_fork", "asl_pages_free", "asl_pages_write", "asl_pages_compact",
+           "asl_paged_attention"]
 
 
 class AslParams(C.Structure):
@@ -42,6 +45,24 @@ class AslStat(C.Structure):
     _fields_ = [("var_top", C.c_double), ("rel_var", C.c_double), ("numerator", C.c_uint64),
                 ("union_size", C.c_int32), ("n_rows", C.c_int32), ("evaluated", C.c_int32),
                 ("selected", C.c_int32)]
+
+
+class AslPages(C.Structure):
+    _fields_ = [("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int32),
+                ("page_size", C.c_int32), ("n_pages", C.c_int32), ("n_rows", C.c_int32), ("row_stride", C.c_int32),
+                ("stride_page", C.c_int64), ("stride_head", C.c_int64), ("stride_tok", C.c_int64),
+                ("scale", C.c_float), ("flags", C.c_int32)]
+
+
+class AslRows(C.Structure):
+    _fields_ = [("n_src", C.c_int32), ("idx_rows", C.c_int32), ("k_stride_head", C.c_int64), ("k_stride_tok", C.c_int64),
+                ("v_stride_head", C.c_int64), ("v_stride_tok", C.c_int64)]
+
+
+class AslAttn(C.Structure):
+    _fields_ = [("n_seqs", C.c_int32), ("total_q", C.c_int32), ("max_q_len", C.c_int32), ("max_kv_len", C.c_int32),
+                ("n_groups", C.c_int32), ("flags", C.c_int32), ("q_stride_tok", C.c_int64), ("q_stride_head", C.c_int64),
+                ("out_stride_tok", C.c_int64), ("out_stride_head", C.c_int64)]
 
 
 class AslError(RuntimeError):
@@ -111,6 +132,16 @@ def load() -> C.CDLL:
     lib.asl_profile_enable.restype = C.c_int
     lib.asl_profile_collect.argtypes = [vp, i32, C.POINTER(C.c_double), C.POINTER(i32)]
     lib.asl_profile_collect.restype = C.c_int
+    for name, args in {
+            "asl_paged_reserve": [vp, i32, i32, i32],
+            "asl_pages_grow": [vp, C.POINTER(AslPages), vp, vp, i32, vp, vp, vp, vp],
+            "asl_pages_fork": [vp, C.POINTER(AslPages), vp, vp, i32, vp, vp, i32, vp, vp, vp, vp],
+            "asl_pages_free": [vp, C.POINTER(AslPages), vp, i32, vp, vp, vp, vp],
+            "asl_pages_write": [vp, C.POINTER(AslPages), C.POINTER(AslRows), vp, vp, vp, vp, i32, i32, vp, vp, vp, vp, vp, vp],
+            "asl_pages_compact": [vp, C.POINTER(AslPages), vp, vp, vp, i32, i32, vp, i32, vp, vp, vp, vp, vp],
+            "asl_paged_attention": [vp, C.POINTER(AslPages), C.POINTER(AslAttn)] + [vp] * 12}.items():
+        getattr(lib, name).argtypes = args
+        getattr(lib, name).restype = C.c_int
     _lib = lib
     return lib
 
@@ -133,6 +164,18 @@ def make_params(Hq: int, Hk: int, d: int, N: int, W: int, S: int, budget: int, d
     ks = k_strides or (N * d, d)
     vs = v_strides or (N * d, d)
     return AslParams(Hq, Hk, d, N, W, S, budget, dtype, ks[0], ks[1], vs[0], vs[1], scale, flags)
+
+
+def make_pages(Hq: int, Hk: int, d: int, page_size: int, n_pages: int, n_rows: int, row_stride: int, dtype: int = ASL_BF16,
+               strides=None, scale: float = 0.0) -> AslPages:
+    """strides: (page, head, token) in elements; pages [n_pages, Hk, page_size, d] without gaps if None."""
+    sp = strides or (Hk * page_size * d, page_size * d, d)
+    return AslPages(Hq, Hk, d, dtype, page_size, n_pages, n_rows, row_stride, sp[0], sp[1], sp[2], scale, 0)
+
+
+def make_attn(n_seqs: int, total_q: int, max_q_len: int, max_kv_len: int, n_groups: int = 0, causal: bool = True) -> AslAttn:
+    """The strides of q and out are set by each call from its tensors."""
+    return AslAttn(n_seqs, total_q, max_q_len, max_kv_len, n_groups, ASL_ATTN_CAUSAL if causal else 0, 0, 0, 0, 0)
 
 
 class Asl:
@@ -226,6 +269,48 @@ class Asl:
         ms, n = C.c_double(), C.c_int32()
         self._check(self.lib.asl_profile_collect(self.h, kernel_id, C.byref(ms), C.byref(n)))
         return ms.value, n.value
+
+    # -- the paged cache -------------------------------------------------------------------------
+    def asl_paged_reserve(self, max_seqs: int, max_query_rows: int, max_head_dim: int) -> None:
+        self._check(self.lib.asl_paged_reserve(self.h, max_seqs, max_query_rows, max_head_dim))
+
+    def asl_pages_grow(self, pages: AslPages, rows, add, n: int, table, kv_len, refs) -> None:
+        self._check(self.lib.asl_pages_grow(self.h, C.byref(pages), _ptr(rows), _ptr(add), n, _ptr(table), _ptr(kv_len),
+                                            _ptr(refs), _stream()))
+
+    def asl_pages_fork(self, pages: AslPages, k_ptrs, v_ptrs, n_layers: int, parents, children, n: int, table, kv_len,
+                       refs) -> None:
+        """k_ptrs, v_ptrs: int64 device tensors holding one device pointer per layer."""
+        self._check(self.lib.asl_pages_fork(self.h, C.byref(pages), _ptr(k_ptrs), _ptr(v_ptrs), n_layers, _ptr(parents),
+                                            _ptr(children), n, _ptr(table), _ptr(kv_len), _ptr(refs), _stream()))
+
+    def asl_pages_free(self, pages: AslPages, rows, n: int, table, kv_len, refs) -> None:
+        self._check(self.lib.asl_pages_free(self.h, C.byref(pages), _ptr(rows), n, _ptr(table), _ptr(kv_len), _ptr(refs),
+                                            _stream()))
+
+    def asl_pages_write(self, pages: AslPages, k, v, rows, cu, n: int, total: int, table, kv_len, k_pages, v_pages,
+                        idx=None) -> None:
+        """k, v: [Hk, n_src, d] of any strides (d contiguous); idx: [1 or Hk, total]."""
+        src = AslRows(k.shape[1], 0 if idx is None else idx.shape[0], k.stride(0), k.stride(1), v.stride(0), v.stride(1))
+        self._check(self.lib.asl_pages_write(self.h, C.byref(pages), C.byref(src), _ptr(k), _ptr(v), _ptr(rows), _ptr(cu), n,
+                                             total, _ptr(idx), _ptr(table), _ptr(kv_len), _ptr(k_pages), _ptr(v_pages),
+                                             _stream()))
+
+    def asl_pages_compact(self, pages: AslPages, src_rows, dst_rows, cu, n: int, total: int, idx, table, kv_len, k_pages,
+                          v_pages) -> None:
+        """idx: [1 or Hk, total]."""
+        self._check(self.lib.asl_pages_compact(self.h, C.byref(pages), _ptr(src_rows), _ptr(dst_rows), _ptr(cu), n, total,
+                                               _ptr(idx), idx.shape[0], _ptr(table), _ptr(kv_len), _ptr(k_pages),
+                                               _ptr(v_pages), _stream()))
+
+    def asl_paged_attention(self, pages: AslPages, attn: AslAttn, q, k_pages, v_pages, table, kv_len, cu_q, out, lse=None,
+                            rows=None, group_start=None, prefix_len=None) -> None:
+        """q, out: [total_q, Hq, d] of any strides (d contiguous); lse: [Hq, total_q]."""
+        attn.q_stride_tok, attn.q_stride_head, _ = q.stride()
+        attn.out_stride_tok, attn.out_stride_head, _ = out.stride()
+        self._check(self.lib.asl_paged_attention(self.h, C.byref(pages), C.byref(attn), _ptr(q), _ptr(k_pages), _ptr(v_pages),
+                                                 _ptr(rows), _ptr(table), _ptr(kv_len), _ptr(cu_q), _ptr(group_start),
+                                                 _ptr(prefix_len), _ptr(out), _ptr(lse), _stream()))
 
     def asl_gather_kv(self, params: AslParams, k, v, idx, idx_rows: int, n_idx: int, k_out, v_out) -> None:
         self._check(self.lib.asl_gather_kv(self.h, C.byref(params), _ptr(k), _ptr(v), _ptr(idx), idx_rows,

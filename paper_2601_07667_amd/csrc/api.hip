@@ -1,32 +1,16 @@
 // The C ABI of libasl: context/workspace management, host-side argument validation, and the
 // launch sequences behind each entry point declared in include/asl.h.
 #include <cmath>
-#include <cstdarg>
-#include <cstdio>
 #include <cstring>
 #include <new>
 
+#include "context.h"
 #include "rankvar_body.h"
-
-struct asl_ctx {
-  int device;
-  int32_t max_seq_len, max_kv_heads, max_q_rows;
-  void* base;
-  size_t bytes;
-  asl::Workspace ws;
-  asl::Prof prof;
-  hipStream_t side;          // second stream of asl_layer_step's fork/join (default priority)
-  hipEvent_t ev_fork, ev_join;
-  bool side_pending;         // a deferred asl_layer_step left work on `side` that nobody has waited for yet
-  char err[256];
-};
 
 namespace {
 
 constexpr int kMaxSelectRows = 1024;   // rows per call (KV heads, or layers x KV heads when batched)
 constexpr int kMaxPoolKernel = 129;
-
-size_t align_up(size_t x) { return (x + 255) & ~size_t(255); }
 
 // Lay the workspace out from `base` (may be null to only measure).  Returns total bytes.
 size_t carve(char* base, int32_t max_seq_len, int32_t max_kv_heads, int32_t max_q_rows,
@@ -63,39 +47,6 @@ size_t carve(char* base, int32_t max_seq_len, int32_t max_kv_heads, int32_t max_
   return off;
 }
 
-asl_status fail(asl_ctx* ctx, asl_status st, const char* fmt, ...) {
-  if (ctx) {
-    va_list ap;
-    va_start(ap, fmt);
-    vsnprintf(ctx->err, sizeof(ctx->err), fmt, ap);
-    va_end(ap);
-  }
-  return st;
-}
-
-asl_status hip_fail(asl_ctx* ctx, hipError_t e, const char* what) {
-  return fail(ctx, ASL_EHIP, "%s: %s", what, hipGetErrorString(e));
-}
-
-// Makes ctx->device current for the duration of a call and restores the caller's device.
-struct DeviceGuard {
-  int prev = -1;
-  bool switched = false;
-  hipError_t err = hipSuccess;
-  explicit DeviceGuard(int dev) {
-    err = hipGetDevice(&prev);
-    if (err == hipSuccess && prev != dev) {
-      err = hipSetDevice(dev);
-      switched = (err == hipSuccess);
-    }
-  }
-  ~DeviceGuard() {
-    if (switched) (void)hipSetDevice(prev);
-  }
-};
-
-int elem_bytes(int dtype) { return dtype == ASL_BF16 ? 2 : 4; }
-
 // Shape checks shared by the entry points that take asl_params.
 asl_status check_params(asl_ctx* ctx, const asl_params* p) {
   if (!ctx) return ASL_EINVAL;
@@ -123,8 +74,6 @@ asl_status check_params(asl_ctx* ctx, const asl_params* p) {
                 ctx->max_kv_heads, ctx->max_q_rows);
   return ASL_OK;
 }
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 }  // namespace
 
@@ -268,6 +217,10 @@ asl_status asl_destroy(asl_ctx* ctx) {
   (void)hipEventDestroy(ctx->ev_fork);
   (void)hipStreamDestroy(ctx->side);
   hipError_t e = hipFree(ctx->base);
+  if (ctx->paged.base) {
+    const hipError_t ep = hipFree(ctx->paged.base);
+    if (e == hipSuccess) e = ep;
+  }
   delete ctx;
   return e == hipSuccess ? ASL_OK : ASL_EHIP;
 }
@@ -633,16 +586,22 @@ asl_status asl_device_fault(asl_ctx* ctx, int32_t* fault_out) {
   if (!fault_out) return fail(ctx, ASL_EINVAL, "null output pointer");
   DeviceGuard guard(ctx->device);
   if (guard.err != hipSuccess) return hip_fail(ctx, guard.err, "set device");
-  uint32_t v = 0;
   hipError_t e = hipDeviceSynchronize();
-  if (e == hipSuccess) e = hipMemcpy(&v, ctx->ws.fault, sizeof(v), hipMemcpyDeviceToHost);
   if (e != hipSuccess) return hip_fail(ctx, e, "fault word read");
-  *fault_out = (int32_t)v;
-  if (v != 0) {
-    const uint32_t zero = 0;
-    e = hipMemcpy(ctx->ws.fault, &zero, sizeof(zero), hipMemcpyHostToDevice);
-    if (e != hipSuccess) return hip_fail(ctx, e, "fault word reset");
+  uint32_t all = 0;
+  for (uint32_t* word : {ctx->ws.fault, ctx->paged.fault}) {
+    if (!word) continue;                                   // nothing reserved for the paged cache
+    uint32_t v = 0;
+    e = hipMemcpy(&v, word, sizeof(v), hipMemcpyDeviceToHost);
+    if (e != hipSuccess) return hip_fail(ctx, e, "fault word read");
+    all |= v;
+    if (v != 0) {
+      const uint32_t zero = 0;
+      e = hipMemcpy(word, &zero, sizeof(zero), hipMemcpyHostToDevice);
+      if (e != hipSuccess) return hip_fail(ctx, e, "fault word reset");
+    }
   }
+  *fault_out = (int32_t)all;
   return ASL_OK;
 }
 
