@@ -20,9 +20,11 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hi
 
 # score.hip never produces NaNs from finite inputs (masked logits are -inf, never inf - inf); telling
 # the compiler so lets max() compile to bare v_max_f32 / v_max3_f32 without NaN-quieting moves.
+# attend.hip takes NaN as they come, so without the first of the two.
 # MFMA results are kept in ordinary VGPRs: the softmax arithmetic reads every accumulator, and
 # copies out of accumulation registers would cost one vector instruction per element.
-PER_FILE_FLAGS = {"score.hip": ["-fno-honor-nans", "-mllvm", "-amdgpu-mfma-vgpr-form"]}
+PER_FILE_FLAGS = {"score.hip": ["-fno-honor-nans", "-mllvm", "-amdgpu-mfma-vgpr-form"],
+                  "attend.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 
 
 def _hipcc() -> str:

@@ -1,97 +1,802 @@
 // Attention over a paged cache: for query i of a sequence of n_q queries and L keys, over the keys j < lim_i,
 //   x_j = scale q_i . k_j,  m = max x_j,  z = sum exp(x_j - m),  out = sum exp(x_j - m) v_j / z,  lse = m + log z,
 // lim_i = L - n_q + i + 1 (causal: the queries are the sequence's last tokens) or L.  A row without keys gets out 0, lse -inf.
+// Keys are taken once, in pieces: a piece's (m, z, unnormalised out) are joined by m = max m_p, z = sum z_p 2^(m_p - m) and the
+// same for out (attend_plan.h: how the work is cut).  Logits are kept in units of log 2.
+//
+// attend_split_kernel, for few rows: bound by reading K and V.  Each wavefront takes every fourth block of 32 keys (16 in fp32) of
+// the item, for all rows of its tile, straight from memory into registers in the layout of the matrix instruction's operand:
+//   x^T = K Q^T  (v_mfma_f32_16x16x32_bf16; lane (r = lane % 16, g = lane / 16) holds K[r][8 g ..]),
+//   out^T += V^T P^T.
+// The accumulator has the query in lane % 16 and keys 4 g .. 4 g + 3, so softmax statistics stay within a lane, and the
+// probabilities are the second product's operand where they stand, if the contraction takes the keys in the order
+// slot (g, j) = key 16 (j / 4) + 4 g + j % 4.  V rows are loaded in that order, 16 bytes of a row a lane, and turned with byte
+// permutes in registers: no LDS and no barrier until the four wavefronts join their results.
 #include "paged.h"
 
 #include "asl_internal.h"
+#include "attend_plan.h"
 
 namespace asl {
 
 namespace {
 
-constexpr int kSimpleThreads = 256;
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t Piece __attribute__((ext_vector_type(4)));
 
-__device__ __forceinline__ float to_f(float x) { return x; }
-__device__ __forceinline__ float to_f(__bf16 x) { return (float)x; }
+constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / 64;
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+// A row's reference moves when a logit exceeds it by more than this (in units of log 2): probabilities stay below 2^8 and most
+// blocks need no maximum over lanes and no rescaling.
+constexpr float kSlack = 8.f;
 
-// One workgroup per query token and head, 256 keys at a time: a key's logit per thread, then an output dimension per thread.
-template <typename T>
-__global__ void __launch_bounds__(kSimpleThreads) attend_simple_kernel(AttendArgs a) {
-  __shared__ float qs[kPagedMaxDim], ps[kSimpleThreads], red[4];
-  __shared__ int64_t off[kSimpleThreads];
-  const int tok = blockIdx.x, hq = blockIdx.y, hk = hq / a.G, tid = threadIdx.x;
-  int lo = 0, hi = a.n_seqs;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (a.cu_q[mid] <= tok) lo = mid; else hi = mid;
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// Maximum / sum over the four lanes that share lane % 16.
+__device__ __forceinline__ float max_over_g(float x) {
+  auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float sum_over_g(float x) {
+  auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+// ------------------------------------------------------------------------------------------------------------------
+// The cut, found by every wavefront for itself.
+
+struct Segment {
+  int c0, rows;            // first query token, rows of a KV head
+  int row, len;            // table row and its tokens
+  int t0, span;            // first key tile and number of key tiles
+  int shared;              // own segments: tokens in the group's shared segment
+};
+
+__device__ __forceinline__ int seq_row(const AttendArgs& a, int b) { return a.rows != nullptr ? a.rows[b] : b; }
+
+// Tokens shared by group g.
+__device__ __forceinline__ int group_shared(const AttendArgs& a, int g) {
+  const int b0 = a.group_start[g], b1 = a.group_start[g + 1];
+  if (b0 < 0 || b1 <= b0 || b1 > a.n_seqs) return 0;
+  int len;
+  row_length(a.map, seq_row(a, b0), &len);
+  return shared_tokens(a.prefix_len[g], len, b1 - b0);
+}
+__device__ __forceinline__ int group_of(const AttendArgs& a, int b) {
+  const int g = sequence_of(a.group_start, a.n_groups, b);
+  return a.group_start[g] <= b && b < a.group_start[g + 1] ? g : -1;
+}
+
+// Segment i: sequence i's own (SHARED false), or group i's shared one.  *bad: a number out of range.
+template <bool SHARED>
+__device__ __forceinline__ Segment segment_of(const AttendArgs& a, int i, bool* bad) {
+  Segment s = {0, 0, 0, 0, 0, 0, 0};
+  if (SHARED) {
+    const int p = group_shared(a, i);
+    if (p == 0) return s;
+    const int b0 = a.group_start[i], b1 = a.group_start[i + 1], c0 = a.cu_q[b0], c1 = a.cu_q[b1];
+    if (c0 < 0 || c1 < c0 || c1 > a.total_q) { *bad = true; return s; }
+    s.c0 = c0;
+    s.rows = (c1 - c0) * a.G;
+    s.row = seq_row(a, b0);
+    s.len = p;
+    s.span = p / kKeyTile;
+    return s;
   }
-  const PageMap& m = a.map;
-  const int row = a.rows != nullptr ? a.rows[lo] : lo;
-  int lim = 0;
-  if ((uint32_t)row < (uint32_t)m.n_rows && a.cu_q[lo] <= tok && tok < a.cu_q[lo + 1]) {
-    const int64_t cap = (int64_t)m.row_stride * m.ps;
-    const int L = m.kv_len[row];
-    if (L < 0 || L > cap) { if (tid == 0) atomicOr(m.fault, kFaultPaged); }
-    else lim = a.causal ? max(0, L - (a.cu_q[lo + 1] - tok) + 1) : L;
-  } else if (tid == 0) {
-    atomicOr(m.fault, kFaultPaged);
+  const int c0 = a.cu_q[i], c1 = a.cu_q[i + 1];
+  s.row = seq_row(a, i);
+  if (!row_length(a.map, s.row, &s.len)) *bad = true;
+  if (c0 < 0 || c1 < c0 || c1 > a.total_q) { *bad = true; return s; }
+  s.c0 = c0;
+  s.rows = (c1 - c0) * a.G;
+  if (a.n_groups > 0) {
+    const int g = group_of(a, i);
+    if (g >= 0) s.shared = group_shared(a, g); else *bad = true;
   }
-  const T* q = (const T*)a.q + (int64_t)tok * a.qt + (int64_t)hq * a.qh;
-  for (int e = tid; e < a.d; e += kSimpleThreads) qs[e] = to_f(q[e]);
-  __syncthreads();
-  float mx = -INFINITY, z = 0.f, acc = 0.f;
-  for (int j0 = 0; j0 < lim; j0 += kSimpleThreads) {
-    const int j = j0 + tid;
-    float x = -INFINITY;
-    int64_t o = -1;
-    if (j < lim) {
-      const int page = m.table[(int64_t)row * m.row_stride + (j >> m.ps_shift)];
-      if ((uint32_t)page < (uint32_t)m.n_pages) {
-        o = (int64_t)page * m.page + (int64_t)(j & (m.ps - 1)) * m.tok + (int64_t)hk * m.head;
-        const T* k = (const T*)((const char*)a.k + o);
-        float s = 0.f;
-        for (int e = 0; e < a.d; ++e) s += qs[e] * to_f(k[e]);
-        x = s * a.scale;
+  s.t0 = s.shared / kKeyTile;
+  s.span = max(0, (s.len + kKeyTile - 1) / kKeyTile - s.t0);
+  return s;
+}
+
+struct Item {
+  Segment seg;
+  int tile, h, split, splits;
+  int64_t slot;            // of the segment's first row of partial results, or -1: the results are whole
+};
+
+// What the joining kernel has to know of a segment: first token, rows, splits (0: nothing to join) and first slot.
+__device__ __forceinline__ int4 plan_entry(const Segment& s, int splits, bool partial, uint32_t slot) {
+  return make_int4(s.c0, s.rows, partial ? splits : 0, (int)slot);
+}
+
+template <bool SHARED>
+__device__ __forceinline__ bool find_item(const AttendArgs& a, const AttendCut& cut, int item, int4* plan, Item* out) {
+  const int lane = threadIdx.x & 63;
+  const int n = SHARED ? a.n_groups : a.n_seqs, per = (n + 63) / 64;
+  const bool writes = blockIdx.x == 0 && threadIdx.x < 64;
+  bool bad = false;
+  auto row_tiles = [&](const Segment& s) { return (uint32_t)((s.rows + cut.rows - 1) / cut.rows) * (uint32_t)a.Hk; };
+  auto is_partial = [&](const Segment& s, int splits) { return SHARED || splits > 1 || s.shared > 0; };
+  Segment own = {0, 0, 0, 0, 0, 0, 0};
+  unsigned long long work = 0;
+  for (int u = 0; u < per; ++u) {
+    const int i = lane * per + u;
+    if (i >= n) break;
+    own = segment_of<SHARED>(a, i, &bad);
+    work += (unsigned long long)row_tiles(own) * (uint32_t)max(own.span, 1);
+  }
+  if (writes && bad) atomicOr(a.map.fault, kFaultPaged);
+  int64_t per_item = tiles_per_item(cut, wave_sum(work));
+  uint32_t items, slots, upto, slots_upto;
+  for (int round = 0;; ++round) {
+    items = slots = 0;
+    for (int u = 0; u < per; ++u) {
+      const int i = lane * per + u;
+      if (i >= n) break;
+      if (per > 1) own = segment_of<SHARED>(a, i, &bad);
+      const int k = splits_of(own.span, per_item);
+      items += row_tiles(own) * (uint32_t)k;
+      slots += is_partial(own, k) ? (uint32_t)own.rows * (uint32_t)a.Hk * (uint32_t)k : 0u;
+    }
+    upto = wave_prefix_sum(items);
+    slots_upto = wave_prefix_sum(slots);
+    if (round > 0 || (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)slots_upto, 63) <= cut.cap) break;
+    per_item = int64_t(1) << 40;                           // no room for the pieces: whole spans
+  }
+  if (writes) {
+    uint32_t at = slots_upto - slots;
+    for (int u = 0; u < per; ++u) {
+      const int i = lane * per + u;
+      if (i >= n) break;
+      if (per > 1) own = segment_of<SHARED>(a, i, &bad);
+      const int k = splits_of(own.span, per_item);
+      const bool partial = is_partial(own, k);
+      plan[i] = plan_entry(own, k, partial && own.rows > 0, at);
+      if (partial) at += (uint32_t)own.rows * (uint32_t)a.Hk * (uint32_t)k;
+    }
+  }
+  const uint64_t past = __ballot(upto > (uint32_t)item);
+  if (past == 0) return false;
+  const int l = __ffsll((unsigned long long)past) - 1;
+  uint32_t base = (uint32_t)__builtin_amdgcn_readlane((int)(upto - items), l);
+  uint32_t slot = (uint32_t)__builtin_amdgcn_readlane((int)(slots_upto - slots), l);
+  int from = l;
+  if (per > 1) {                                           // the same among the lane's segments (per <= 64)
+    const int i = l * per + lane;
+    own = Segment{0, 0, 0, 0, 0, 0, 0};
+    items = slots = 0;
+    if (lane < per && i < n) {
+      own = segment_of<SHARED>(a, i, &bad);
+      const int k = splits_of(own.span, per_item);
+      items = row_tiles(own) * (uint32_t)k;
+      slots = is_partial(own, k) ? (uint32_t)own.rows * (uint32_t)a.Hk * (uint32_t)k : 0u;
+    }
+    upto = wave_prefix_sum(items);
+    slots_upto = wave_prefix_sum(slots);
+    const uint64_t more = __ballot(base + upto > (uint32_t)item);
+    if (more == 0) return false;
+    from = __ffsll((unsigned long long)more) - 1;
+    base += (uint32_t)__builtin_amdgcn_readlane((int)(upto - items), from);
+    slot += (uint32_t)__builtin_amdgcn_readlane((int)(slots_upto - slots), from);
+  }
+  Segment s;
+  s.c0 = __builtin_amdgcn_readlane(own.c0, from);
+  s.rows = __builtin_amdgcn_readlane(own.rows, from);
+  s.row = __builtin_amdgcn_readlane(own.row, from);
+  s.len = __builtin_amdgcn_readlane(own.len, from);
+  s.t0 = __builtin_amdgcn_readlane(own.t0, from);
+  s.span = __builtin_amdgcn_readlane(own.span, from);
+  s.shared = __builtin_amdgcn_readlane(own.shared, from);
+  out->seg = s;
+  out->splits = splits_of(s.span, per_item);
+  const uint32_t e = (uint32_t)item - base, tiles = (uint32_t)((s.rows + cut.rows - 1) / cut.rows);
+  out->h = (int)(e % (uint32_t)a.Hk);
+  out->tile = (int)(tiles - 1u - (e / (uint32_t)a.Hk) % tiles);    // causal: the longest first
+  out->split = (int)(e / (uint32_t)a.Hk / tiles);
+  out->slot = is_partial(s, out->splits) ? (int64_t)slot : -1;
+  return out->slot < 0 || (int64_t)slot + (int64_t)s.rows * a.Hk * out->splits <= cut.cap;
+}
+
+// Keys that row r of a segment sees.
+template <bool SHARED>
+__device__ __forceinline__ int row_limit(const AttendArgs& a, const Segment& s, int r) {
+  const int i = (int)((uint32_t)r / (uint32_t)a.G);
+  if (!SHARED) return a.causal ? max(0, s.len - s.rows / a.G + i + 1) : s.len;
+  const int tok = s.c0 + i, b = sequence_of(a.cu_q, a.n_seqs, tok);
+  int len;
+  row_length(a.map, seq_row(a, b), &len);
+  return min(s.len, a.causal ? max(0, len - (a.cu_q[b + 1] - tok) + 1) : len);
+}
+
+// ------------------------------------------------------------------------------------------------------------------
+// Registers of a block of keys, and the arithmetic on them.
+
+template <typename T, int D>
+struct Block {
+  static constexpr bool kBf16 = sizeof(T) == 2;
+  static constexpr int SUB = kBf16 ? 2 : 1;                // subtiles of 16 keys
+  static constexpr int KEYS = 16 * SUB;
+  static constexpr int KP = D * (int)sizeof(T) / 64;       // 16-byte pieces of K a lane holds of a subtile
+  static constexpr int VR = KEYS / 4;                      // rows of V that a lane holds parts of
+  static constexpr int CW = kBf16 && D >= 128 ? 8 : 4;     // consecutive elements of each
+  static constexpr int VW = CW * (int)sizeof(T) / 4;       // in words
+  static constexpr int HN = D / (16 * CW);                 // parts of a row: element 16 CW hf + CW (lane % 16) + e
+  static constexpr int NT = D / 16;                        // accumulators of out: index hf * CW + e
+  Piece k[SUB][KP];
+  uint32_t v[VR][HN][VW];
+  bool ok[SUB];                                            // the subtile's page number is in range
+
+  // Key of row j of V within the block.
+  static __device__ __forceinline__ int v_key(int j, int g) { return 16 * (j >> 2) + 4 * g + (j & 3); }
+};
+
+struct Source {
+  const char* k;           // pages of the KV head
+  const char* v;
+  const int32_t* table;    // the segment's row
+  int64_t page, tok;
+  int n_pages, ps, shift, last;    // last: the last key's subtile (no page number behind it is read)
+  int d;
+};
+
+template <typename T, int D, bool PAD>
+__device__ __forceinline__ void load_block(Block<T, D>& b, const Source& s, int key0) {
+  typedef Block<T, D> B;
+  const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+  const char* base[B::SUB];
+#pragma unroll
+  for (int t = 0; t < B::SUB; ++t) {
+    const int key = min(key0 + 16 * t, s.last);
+    const int page = __builtin_amdgcn_readfirstlane(s.table[key >> s.shift]);
+    b.ok[t] = (uint32_t)page < (uint32_t)s.n_pages;
+    const int64_t off = (int64_t)(b.ok[t] ? page : 0) * s.page + (int64_t)(key & (s.ps - 1)) * s.tok;
+    base[t] = s.v + off;
+    const char* kp = s.k + off + (int64_t)r * s.tok + g * 16;
+#pragma unroll
+    for (int p = 0; p < B::KP; ++p) {
+      if (PAD) {                                           // beyond d: the first piece again, then zeros
+        const bool in = (p * 64 + g * 16) < s.d * (int)sizeof(T);
+        const Piece x = *(const Piece*)(kp + (in ? p * 64 : -g * 16));
+        b.k[t][p] = in ? x : Piece{0, 0, 0, 0};
       } else {
-        atomicOr(m.fault, kFaultPaged);
+        b.k[t][p] = *(const Piece*)(kp + p * 64);
       }
     }
-    float w = x;
-    for (int o2 = 32; o2 > 0; o2 >>= 1) w = fmaxf(w, __shfl_xor(w, o2));
-    if ((tid & 63) == 0) red[tid >> 6] = w;
-    __syncthreads();
-    const float top = fmaxf(mx, fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3])));
-    const float base = top == -INFINITY ? 0.f : top;
-    const float p = o >= 0 ? expf(x - base) : 0.f, shrink = expf(mx - base);
-    ps[tid] = p;
-    off[tid] = o;
-    float sum = p;
-    for (int o2 = 32; o2 > 0; o2 >>= 1) sum += __shfl_xor(sum, o2);
-    __syncthreads();                                       // red has been read
-    if ((tid & 63) == 0) red[tid >> 6] = sum;
-    __syncthreads();
-    z = z * shrink + (red[0] + red[1]) + (red[2] + red[3]);
-    acc *= shrink;
-    mx = top;
-    if (tid < a.d)
-      for (int t = 0; t < kSimpleThreads; ++t)
-        if (off[t] >= 0) acc += ps[t] * to_f(((const T*)((const char*)a.v + off[t]))[tid]);
-    __syncthreads();
   }
-  if (tid < a.d) ((T*)a.out)[(int64_t)tok * a.ot + (int64_t)hq * a.oh + tid] = (T)(z == 0.f ? 0.f : acc / z);
-  if (tid == 0 && a.lse != nullptr) a.lse[(int64_t)hq * a.total_q + tok] = z == 0.f ? -INFINITY : mx + logf(z);
+#pragma unroll
+  for (int j = 0; j < B::VR; ++j) {
+#pragma unroll
+    for (int hf = 0; hf < B::HN; ++hf) {
+      const int e0 = 16 * B::CW * hf + B::CW * r;
+      const char* row = base[j >> 2] + (int64_t)(4 * g + (j & 3)) * s.tok;
+      const bool in = !PAD || e0 < s.d;
+      typedef uint32_t Words __attribute__((ext_vector_type(B::VW)));
+      const Words w = *(const Words*)(row + (in ? e0 : 0) * (int)sizeof(T));
+#pragma unroll
+      for (int x = 0; x < B::VW; ++x) b.v[j][hf][x] = in ? w[x] : 0u;
+    }
+  }
+}
+
+// The sign bit of each element of a word that is infinite or NaN (its exponent, all ones, carries into the sign's place).
+template <typename T> __device__ __forceinline__ uint32_t not_finite(uint32_t w) {
+  return sizeof(T) == 2 ? ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u : ((w & 0x7f800000u) + 0x00800000u) & 0x80000000u;
+}
+// All bits of the elements whose sign bit is set in `bits`.
+template <typename T> __device__ __forceinline__ uint32_t whole_elements(uint32_t bits) {
+  return sizeof(T) == 2 ? (bits - (bits >> 15)) | bits : (bits - (bits >> 31)) | bits;
+}
+// One for each element of a word that is of class c (0: +inf, 1: -inf, 2: NaN), else zero.
+template <typename T> __device__ __forceinline__ uint32_t word_class(uint32_t w, int c) {
+  const uint32_t sign = sizeof(T) == 2 ? 0x80008000u : 0x80000000u, top = sizeof(T) == 2 ? 0x7f807f80u : 0x7f800000u;
+  const uint32_t frac = ~(sign | top), one = sizeof(T) == 2 ? 0x3f803f80u : 0x3f800000u;
+  const uint32_t odd = whole_elements<T>(not_finite<T>(w));
+  // a carry out of the fraction: it is not zero
+  const uint32_t is_nan = whole_elements<T>((((w & frac) + frac) & (sizeof(T) == 2 ? 0x00800080u : 0x00800000u)) << 8);
+  const uint32_t neg = whole_elements<T>(w & sign);
+  const uint32_t is = c == 2 ? is_nan : c == 1 ? neg & ~is_nan : ~neg & ~is_nan;
+  return odd & is & one;
+}
+
+// Element e of eight rows' words as an operand: rows 2 p and 2 p + 1 in word p.
+__device__ __forceinline__ bf16x8 turn(const uint32_t (&w)[8], int odd) {
+  const uint32_t sel = odd ? 0x07060302u : 0x05040100u;
+  union { uint32_t u[4]; bf16x8 v; } x;
+#pragma unroll
+  for (int p = 0; p < 4; ++p) x.u[p] = __builtin_amdgcn_perm(w[2 * p + 1], w[2 * p], sel);
+  return x.v;
+}
+
+// Probabilities as the second product's operand.  (bf16: each rounds to 8 bits, so out is off by at most 2^-8 sum p |v| / z; a split in
+// two parts would take twice the products.  The sum z is that of the unrounded ones.)
+template <typename T> struct Weights;
+template <> struct Weights<__bf16> {
+  bf16x8 w;
+  __device__ __forceinline__ void set(const float (&p)[2][4]) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) w[j] = (__bf16)p[j >> 2][j & 3];
+  }
+};
+template <> struct Weights<float> {
+  float w[4];
+  __device__ __forceinline__ void set(const float (&p)[1][4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = p[0][i];
+  }
+};
+
+// out[mt] + V^T p for part hf, element e of the rows of V, whose words are word(j, hf, x).
+template <typename T, int MT, typename W>
+__device__ __forceinline__ void add_values(f32x4* (&o)[MT], const Weights<T> (&p)[MT], int hf, int e, W word) {
+  if constexpr (sizeof(T) == 2) {
+    const uint32_t w[8] = {word(0, hf, e / 2), word(1, hf, e / 2), word(2, hf, e / 2), word(3, hf, e / 2),
+                           word(4, hf, e / 2), word(5, hf, e / 2), word(6, hf, e / 2), word(7, hf, e / 2)};
+    const bf16x8 va = turn(w, e & 1);
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) *o[mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, p[mt].w, *o[mt], 0, 0, 0);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+        *o[mt] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(word(i, hf, e)), p[mt].w[i], *o[mt], 0, 0, 0);
+  }
+}
+
+// A wavefront's running results for MT tiles of 16 rows.
+template <typename T, int D, int MT>
+struct Rows {
+  typedef Block<T, D> B;
+  Piece q[MT][B::KP];
+  f32x4 o[MT][B::NT];
+  float m[MT], z[MT];      // reference and, of this lane's keys, sum
+  int lim[MT];
+
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      m[mt] = -INFINITY;
+      z[mt] = 0.f;
+#pragma unroll
+      for (int t = 0; t < B::NT; ++t) o[mt][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+  }
+
+  // MASKED: some row does not see some key of the block.  most: keys that any row sees.
+  template <bool MASKED>
+  __device__ __forceinline__ void step(Block<T, D>& b, int key0, int least, int most, float scale) {
+    const int g = (threadIdx.x & 63) >> 4;
+    f32x4 x[MT][B::SUB];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int t = 0; t < B::SUB; ++t) x[mt][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int p = 0; p < B::KP; ++p)
+#pragma unroll
+      for (int t = 0; t < B::SUB; ++t)
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+          if constexpr (B::kBf16) {
+            x[mt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, b.k[t][p]),
+                                                               __builtin_bit_cast(bf16x8, q[mt][p]), x[mt][t], 0, 0, 0);
+          } else {
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+              x[mt][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(b.k[t][p][u]), __uint_as_float(q[mt][p][u]),
+                                                              x[mt][t], 0, 0, 0);
+          }
+        }
+    float p[MT][B::SUB][4];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      float top = -INFINITY;
+#pragma unroll
+      for (int t = 0; t < B::SUB; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float y = x[mt][t][i] * scale;
+          if (MASKED) y = b.ok[t] && key0 + 16 * t + 4 * g + i < lim[mt] ? y : -INFINITY;
+          p[mt][t][i] = y;
+          top = fmaxf(top, y);
+        }
+      if (__any(top > m[mt] + kSlack)) {
+        const float to = fmaxf(m[mt], max_over_g(top));
+        const float by = to == -INFINITY ? 1.f : exp2_fast(m[mt] - to);
+        m[mt] = to;
+        z[mt] *= by;
+#pragma unroll
+        for (int t = 0; t < B::NT; ++t) o[mt][t] *= by;
+      }
+      const float base = m[mt] == -INFINITY ? 0.f : m[mt];
+#pragma unroll
+      for (int t = 0; t < B::SUB; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          p[mt][t][i] = exp2_fast(p[mt][t][i] - base);
+          z[mt] += p[mt][t][i];
+        }
+    }
+    Weights<T> w[MT];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) w[mt].set(p[mt]);
+    if (MASKED) {
+      // Probability 0 does not keep a value that is no number out of the sum.  Behind the last key that any row sees, and in pages out
+      // of range, values are replaced by zero; where rows differ in what they see, infinities and NaN are taken out and
+      // counted by class for the rows that see them (a product of zeros and ones), and each class added as itself.
+      uint32_t odd = 0;
+#pragma unroll
+      for (int j = 0; j < B::VR; ++j) {
+        const uint32_t seen = b.ok[j >> 2] && key0 + B::v_key(j, g) < most ? ~0u : 0u;
+#pragma unroll
+        for (int hf = 0; hf < B::HN; ++hf)
+#pragma unroll
+          for (int x2 = 0; x2 < B::VW; ++x2) {
+            b.v[j][hf][x2] &= seen;
+            odd |= not_finite<T>(b.v[j][hf][x2]);
+          }
+      }
+      if (least < most && __any(odd != 0)) {
+        Weights<T> see[MT];
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+          float one[B::SUB][4];
+#pragma unroll
+          for (int t = 0; t < B::SUB; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) one[t][i] = b.ok[t] && key0 + 16 * t + 4 * g + i < lim[mt] ? 1.f : 0.f;
+          see[mt].set(one);
+        }
+#pragma unroll 1
+        for (int c = 0; c < 3; ++c) {
+          const float what = c == 0 ? INFINITY : c == 1 ? -INFINITY : __uint_as_float(0x7fc00000u);
+#pragma unroll
+          for (int hf = 0; hf < B::HN; ++hf)
+#pragma unroll
+            for (int e = 0; e < B::CW; ++e) {
+              f32x4 n[MT];
+              f32x4* to[MT];
+#pragma unroll
+              for (int mt = 0; mt < MT; ++mt) {
+                n[mt] = f32x4{0.f, 0.f, 0.f, 0.f};
+                to[mt] = &n[mt];
+              }
+              add_values<T, MT>(to, see, hf, e, [&](int j, int hf2, int x2) {
+                uint32_t word = b.v[j][hf2][x2];
+                asm volatile("" : "+v"(word));             // or every word's classes are worked out and kept before the loop
+                return word_class<T>(word, c);
+              });
+#pragma unroll
+              for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[mt][hf * B::CW + e][i] += n[mt][i] > 0.f ? what : 0.f;
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < B::VR; ++j)
+#pragma unroll
+          for (int hf = 0; hf < B::HN; ++hf)
+#pragma unroll
+            for (int x2 = 0; x2 < B::VW; ++x2) b.v[j][hf][x2] &= ~whole_elements<T>(not_finite<T>(b.v[j][hf][x2]));
+      }
+    }
+#pragma unroll
+    for (int hf = 0; hf < B::HN; ++hf)
+#pragma unroll
+      for (int e = 0; e < B::CW; ++e) {
+        f32x4* to[MT];
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) to[mt] = &o[mt][hf * B::CW + e];
+        add_values<T, MT>(to, w, hf, e, [&](int j, int hf2, int x2) { return b.v[j][hf2][x2]; });
+      }
+  }
+};
+
+// ------------------------------------------------------------------------------------------------------------------
+
+struct Partials {
+  float* o;                // [cap][D]
+  float2* mz;              // [cap]
+  int4* plan;              // of the segments
+};
+
+// Writes row r of an item: to out and lse if its results are whole, else to its slot.  v: CNT elements from e0 on.
+template <typename T, int CNT>
+__device__ __forceinline__ void write_row(const AttendArgs& a, const Item& it, const Partials& pt, int D, int r, int e0,
+                                          const float (&v)[CNT], float m, float z) {
+  if (it.slot >= 0) {
+    const int64_t slot = it.slot + ((int64_t)it.h * it.splits + it.split) * it.seg.rows + r;
+#pragma unroll
+    for (int x = 0; x < CNT; x += 4) *(f32x4*)(pt.o + slot * D + e0 + x) = f32x4{v[x], v[x + 1], v[x + 2], v[x + 3]};
+    if (e0 == 0) pt.mz[slot] = make_float2(m, z);
+    return;
+  }
+  const int i = (int)((uint32_t)r / (uint32_t)a.G), tok = it.seg.c0 + i, hq = it.h * a.G + (r - i * a.G);
+  if (e0 < a.d) {
+    const float by = z == 0.f ? 0.f : 1.f / z;             // no key: the sums are zero
+    T* to = (T*)a.out + (int64_t)tok * a.ot + (int64_t)hq * a.oh + e0;
+    typedef T Out __attribute__((ext_vector_type(CNT)));
+    Out w;
+#pragma unroll
+    for (int x = 0; x < CNT; ++x) w[x] = (T)(v[x] * by);
+    *(Out*)to = w;
+  }
+  if (e0 == 0 && a.lse != nullptr) a.lse[(int64_t)hq * a.total_q + tok] = z == 0.f ? -INFINITY : (m + __log2f(z)) * kLn2;
+}
+
+template <typename T, int D, int MT, bool PAD, bool SHARED>
+__global__ void __launch_bounds__(kThreads, D * MT > 128 ? 1 : 2)
+attend_split_kernel(AttendArgs a, AttendCut cut, Partials pt) {
+  typedef Block<T, D> B;
+  constexpr int LD = D + 4;                                // padded row of the joining buffer
+  __shared__ __attribute__((aligned(16))) float so[kWaves][16][LD];
+  __shared__ float sm[kWaves][16], sz[kWaves][16];
+  Item it;
+  if (!find_item<SHARED>(a, cut, (int)blockIdx.x, pt.plan, &it)) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r16 = lane & 15, g = lane >> 4;
+  Rows<T, D, MT> rows;
+  rows.clear();
+  uint32_t least = 0x7fffffffu, most = 0;
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    const int r = it.tile * cut.rows + 16 * mt + r16;
+    const bool in = r < it.seg.rows;
+    rows.lim[mt] = in ? row_limit<SHARED>(a, it.seg, r) : 0;
+    least = min(least, in ? (uint32_t)rows.lim[mt] : 0x7fffffffu);
+    most = max(most, (uint32_t)rows.lim[mt]);
+    const int i = (int)((uint32_t)r / (uint32_t)a.G);
+    const T* q = (const T*)a.q + (int64_t)(it.seg.c0 + i) * a.qt + (int64_t)(it.h * a.G + (r - i * a.G)) * a.qh;
+#pragma unroll
+    for (int p = 0; p < B::KP; ++p) {
+      const int e = (p * 64 + g * 16) / (int)sizeof(T);
+      rows.q[mt][p] = in && e < a.d ? *(const Piece*)(q + e) : Piece{0, 0, 0, 0};
+    }
+  }
+  least = wave_min(least);
+  most = wave_max(most);
+  Source src;
+  src.k = (const char*)a.k + (int64_t)it.h * a.map.head;
+  src.v = (const char*)a.v + (int64_t)it.h * a.map.head;
+  src.table = a.map.table + (int64_t)it.seg.row * a.map.row_stride;
+  src.page = a.map.page;
+  src.tok = a.map.tok;
+  src.n_pages = a.map.n_pages;
+  src.ps = a.map.ps;
+  src.shift = a.map.ps_shift;
+  src.last = (it.seg.len - 1) & ~15;
+  src.d = a.d;
+  int t0, t1;
+  split_range(min(it.seg.span, max(0, ((int)most + kKeyTile - 1) / kKeyTile - it.seg.t0)), it.splits, it.split, &t0, &t1);
+  constexpr int STEP = kWaves * B::KEYS;
+  int key = (it.seg.t0 + t0) * kKeyTile + wave * B::KEYS;
+  const int end = min((it.seg.t0 + t1) * kKeyTile, (int)most);
+  const float scale = a.scale * kLog2e;
+  bool bad = false;
+  auto whole = [&](const Block<T, D>& b) { return b.ok[0] && b.ok[B::SUB - 1]; };
+  // blocks that every row sees, the next one on its way while one is worked on
+  if (key + B::KEYS <= min(end, (int)least)) {
+    Block<T, D> cur, nxt;
+    load_block<T, D, PAD>(cur, src, key);
+    while (whole(cur)) {
+      const bool more = key + STEP + B::KEYS <= min(end, (int)least);
+      if (more) load_block<T, D, PAD>(nxt, src, key + STEP);
+      rows.template step<false>(cur, key, (int)least, (int)most, scale);
+      key += STEP;
+      if (!more) break;
+      cur = nxt;
+    }
+  }
+  // the last ones, and all from a page number out of range on
+  for (; key < end; key += STEP) {
+    Block<T, D> b;
+    load_block<T, D, PAD>(b, src, key);
+    bad = bad || !whole(b);
+    rows.template step<true>(b, key, (int)least, (int)most, scale);
+  }
+  if (bad && lane == 0) atomicOr(a.map.fault, kFaultPaged);
+  // the wavefronts' results are joined, 16 threads a row
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    if (mt > 0) __syncthreads();
+    const float z = sum_over_g(rows.z[mt]);
+    if (g == 0) {
+      sm[wave][r16] = rows.m[mt];
+      sz[wave][r16] = z;
+    }
+#pragma unroll
+    for (int hf = 0; hf < B::HN; ++hf)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int e = 0; e < B::CW; e += 4)
+          *(f32x4*)&so[wave][r16][16 * B::CW * hf + B::CW * (4 * g + i) + e] =
+              f32x4{rows.o[mt][hf * B::CW + e][i], rows.o[mt][hf * B::CW + e + 1][i], rows.o[mt][hf * B::CW + e + 2][i],
+                    rows.o[mt][hf * B::CW + e + 3][i]};
+    __syncthreads();
+    const int row = threadIdx.x >> 4, part = threadIdx.x & 15, r = it.tile * cut.rows + 16 * mt + row;
+    if (r < it.seg.rows) {
+      float m = sm[0][row];
+#pragma unroll
+      for (int w = 1; w < kWaves; ++w) m = fmaxf(m, sm[w][row]);
+      float by[kWaves], total = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        by[w] = m == -INFINITY ? 1.f : exp2_fast(sm[w][row] - m);
+        total += sz[w][row] * by[w];
+      }
+      constexpr int CNT = D / 16 >= 8 ? 8 : 4;
+#pragma unroll
+      for (int e0 = 0; e0 < D / 16; e0 += CNT) {
+        float v[CNT];
+        const int at = part * CNT + e0 * 16;
+#pragma unroll
+        for (int x = 0; x < CNT; ++x) {
+          v[x] = 0.f;
+#pragma unroll
+          for (int w = 0; w < kWaves; ++w) v[x] += so[w][row][at + x] * by[w];
+        }
+        write_row<T, CNT>(a, it, pt, D, r, at, v, m, total);
+      }
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------------------------------
+// Joins the pieces of rows that were cut: NW wavefronts a row, each lane four elements of every so many-th piece.
+template <typename T, int D, int NW>
+__global__ void __launch_bounds__(kThreads) attend_join_kernel(AttendArgs a, Partials own, Partials shared) {
+  constexpr int LPP = D / 4;                               // lanes of a piece
+  constexpr int PPW = 64 / LPP;                            // pieces a wavefront takes at once
+  constexpr int RPB = kWaves / NW;
+  __shared__ __attribute__((aligned(16))) float so[kWaves][PPW][D];
+  __shared__ float sz[kWaves];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t row = (int64_t)blockIdx.x * RPB + wave / NW;
+  const bool live = row < (int64_t)a.total_q * a.Hq;
+  const int tok = live ? (int)(row / a.Hq) : 0, hq = (int)(row - (int64_t)tok * a.Hq), h = hq / a.G;
+  int n[2] = {0, 0};                                       // pieces of the sequence's own keys, of the shared ones
+  int64_t at[2] = {0, 0};
+  int rows[2] = {0, 0};
+  if (live) {
+    const int b = sequence_of(a.cu_q, a.n_seqs, tok);
+    const int4 p = own.plan[b];
+    const int r = (tok - p.x) * a.G + hq - h * a.G;
+    if (p.z > 0 && tok >= p.x && r < p.y) {
+      n[0] = p.z;
+      rows[0] = p.y;
+      at[0] = (int64_t)(uint32_t)p.w + (int64_t)h * p.z * p.y + r;
+      if (a.n_groups > 0) {
+        const int g = group_of(a, b);
+        if (g >= 0) {
+          const int4 s = shared.plan[g];
+          const int rs = (tok - s.x) * a.G + hq - h * a.G;
+          if (s.z > 0 && tok >= s.x && rs < s.y) {
+            n[1] = s.z;
+            rows[1] = s.y;
+            at[1] = (int64_t)(uint32_t)s.w + (int64_t)h * s.z * s.y + rs;
+          }
+        }
+      }
+    }
+  }
+  const int total = n[0] + n[1];
+  if (NW == 1 && total == 0) return;                       // written whole (with more wavefronts a row: all of a workgroup's alike)
+  if (NW > 1 && total == 0) return;
+  auto piece = [&](int i, const Partials** from) -> int64_t {
+    const int k = i < n[0] ? 0 : 1;
+    *from = k == 0 ? &own : &shared;
+    return at[k] + (int64_t)(i - (k == 0 ? 0 : n[0])) * rows[k];
+  };
+  float m = -INFINITY, z = 0.f;
+  for (int i = lane; i < total; i += 64) {
+    const Partials* f;
+    const int64_t s = piece(i, &f);
+    m = fmaxf(m, f->mz[s].x);
+  }
+  for (int x = 32; x > 0; x >>= 1) m = fmaxf(m, __shfl_xor(m, x));
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  const int sub = lane / LPP, e = (lane % LPP) * 4;
+#pragma unroll 4
+  for (int i = (wave % NW) * PPW + sub; i < total; i += NW * PPW) {
+    const Partials* f;
+    const int64_t s = piece(i, &f);
+    const float2 mz = f->mz[s];
+    const float by = m == -INFINITY ? 1.f : exp2_fast(mz.x - m);
+    acc += *(const f32x4*)(f->o + s * D + e) * by;
+    z += mz.y * by;
+  }
+  if (LPP == 64) {
+    // one piece at a time: every lane has the same sum
+  } else if (LPP == 32) {
+    z += __shfl_xor(z, 32);
+  } else {
+    z += __shfl_xor(z, 16);
+    z += __shfl_xor(z, 32);
+  }
+  *(f32x4*)&so[wave][sub][e] = acc;
+  if (lane == 0) sz[wave] = z;
+  if (NW > 1) __syncthreads(); else __builtin_amdgcn_wave_barrier();
+  if (wave % NW != 0) return;
+  z = 0.f;
+  acc = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int w = 0; w < NW; ++w) {
+    z += sz[wave + w];
+    if (lane < LPP)
+#pragma unroll
+      for (int s = 0; s < PPW; ++s) acc += *(const f32x4*)&so[wave + w][s][lane * 4];
+  }
+  if (lane * 4 < a.d) {
+    const float by = z == 0.f ? 0.f : 1.f / z;
+    typedef T Out __attribute__((ext_vector_type(4)));
+    *(Out*)((T*)a.out + (int64_t)tok * a.ot + (int64_t)hq * a.oh + lane * 4) =
+        Out{(T)(acc[0] * by), (T)(acc[1] * by), (T)(acc[2] * by), (T)(acc[3] * by)};
+  }
+  if (lane == 0 && a.lse != nullptr) a.lse[(int64_t)hq * a.total_q + tok] = z == 0.f ? -INFINITY : (m + __log2f(z)) * kLn2;
+}
+
+template <typename T, int D, int MT, bool SHARED>
+hipError_t launch_split(const AttendArgs& a, const AttendCut& cut, const Partials& pt, hipStream_t st) {
+  const int64_t items = max_items(cut, (int64_t)a.total_q * a.G, SHARED ? a.n_groups : a.n_seqs, a.Hk);
+  if (items >= (int64_t(1) << 31)) return hipErrorInvalidValue;
+  if (a.d == D)
+    hipLaunchKernelGGL((attend_split_kernel<T, D, MT, false, SHARED>), dim3((unsigned)items), dim3(kThreads), 0, st, a, cut, pt);
+  else
+    hipLaunchKernelGGL((attend_split_kernel<T, D, MT, true, SHARED>), dim3((unsigned)items), dim3(kThreads), 0, st, a, cut, pt);
+  return hipGetLastError();
+}
+
+template <typename T, int D>
+hipError_t launch_d(const PagedWorkspace& ws, const AttendArgs& args, hipStream_t st) {
+  AttendArgs a = args;
+  const int64_t rows = (int64_t)a.total_q * a.G;
+  constexpr int kTarget = 512;
+  AttendCut own = {16, kTarget, 2, 0}, shared = {16, kTarget, 2, 0};
+  const int64_t room = ws.part_rows;
+  shared.cap = max_partials(shared, rows, a.Hk);
+  // every row of a group is joined from two parts: there has to be room for them
+  if (a.n_groups > 0 && shared.cap + rows * a.Hk > room) a.n_groups = 0;
+  if (a.n_groups == 0) shared.cap = 0;
+  own.cap = room - shared.cap;
+  Partials po, ps;
+  ps.o = ws.part;
+  ps.mz = ws.part_mz;
+  ps.plan = ws.plan + kPagedMaxSeqs;
+  po.o = ws.part + shared.cap * D;
+  po.mz = ws.part_mz + shared.cap;
+  po.plan = ws.plan;
+  hipError_t e = hipSuccess;
+  if (a.n_groups > 0) e = launch_split<T, D, 1, true>(a, shared, ps, st);
+  if (e == hipSuccess) e = launch_split<T, D, 1, false>(a, own, po, st);
+  if (e != hipSuccess) return e;
+  const int64_t out_rows = (int64_t)a.total_q * a.Hq;
+  if (out_rows <= 2048)
+    hipLaunchKernelGGL((attend_join_kernel<T, D, kWaves>), dim3((unsigned)out_rows), dim3(kThreads), 0, st, a, po, ps);
+  else
+    hipLaunchKernelGGL((attend_join_kernel<T, D, 1>), dim3((unsigned)((out_rows + kWaves - 1) / kWaves)), dim3(kThreads), 0, st,
+                       a, po, ps);
+  return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_attend(const PagedWorkspace&, const AttendArgs& a, int dtype, hipStream_t st) {
+hipError_t launch_attend(const PagedWorkspace& ws, const AttendArgs& a, int dtype, hipStream_t st) {
   if (a.total_q == 0 || a.n_seqs == 0) return hipSuccess;
-  const dim3 grid((unsigned)a.total_q, (unsigned)a.Hq);
-  if (dtype == ASL_BF16)
-    hipLaunchKernelGGL((attend_simple_kernel<__bf16>), grid, dim3(kSimpleThreads), 0, st, a);
-  else
-    hipLaunchKernelGGL((attend_simple_kernel<float>), grid, dim3(kSimpleThreads), 0, st, a);
-  return hipGetLastError();
+  if (dtype == ASL_BF16) {
+    if (a.d <= 64) return launch_d<__bf16, 64>(ws, a, st);
+    if (a.d <= 128) return launch_d<__bf16, 128>(ws, a, st);
+    return launch_d<__bf16, 256>(ws, a, st);
+  }
+  if (a.d <= 64) return launch_d<float, 64>(ws, a, st);
+  if (a.d <= 128) return launch_d<float, 128>(ws, a, st);
+  return launch_d<float, 256>(ws, a, st);
 }
 
 }  // namespace asl

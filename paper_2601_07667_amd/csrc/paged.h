@@ -12,8 +12,10 @@ namespace asl {
 struct PagedWorkspace {
   void* base;
   int32_t max_seqs, max_query_rows, max_head_dim;
-  float* part;             // [part_rows][max_head_dim + 4] attention: partial results of pieces of sequences
+  float* part;             // [part_rows][max_head_dim, a power of two >= 64] attention: unnormalised results of cut rows ...
+  float2* part_mz;         // [part_rows] ... with their reference and sum
   int64_t part_rows;
+  int4* plan;              // [2][kPagedMaxSeqs] how sequences and groups were cut
   int4* forks;             // [max_seqs] what the bookkeeping launch of a fork leaves for the copying one
   int32_t* fresh;          // [kMaxFresh] the free pages that a call takes, in order
   uint32_t* fault;         // [1]

@@ -55,7 +55,13 @@ asl_status asl_paged_reserve(asl_ctx* ctx, int32_t max_seqs, int32_t max_query_r
     return at;
   };
   const size_t fault = take(sizeof(uint32_t)), forks = take((size_t)max_seqs * sizeof(int4)),
-               fresh = take((size_t)asl::kMaxFresh * sizeof(int32_t));
+               fresh = take((size_t)asl::kMaxFresh * sizeof(int32_t)),
+               plan = take((size_t)2 * asl::kPagedMaxSeqs * sizeof(int4));
+  // attention: room for every row twice (its own and its shared keys; not for the largest calls, which have no need to share),
+  // and for the pieces that long spans are cut into
+  w.part_rows = 2 * (int64_t)(max_query_rows < 131072 ? max_query_rows : 131072) + asl::kCutRows;
+  const int D = max_head_dim <= 64 ? 64 : max_head_dim <= 128 ? 128 : 256;
+  const size_t part = take((size_t)w.part_rows * D * sizeof(float)), part_mz = take((size_t)w.part_rows * sizeof(float2));
   char* base = nullptr;
   hipError_t e = hipMalloc(&base, off);
   if (e != hipSuccess) {
@@ -66,6 +72,9 @@ asl_status asl_paged_reserve(asl_ctx* ctx, int32_t max_seqs, int32_t max_query_r
   w.fault = (uint32_t*)(base + fault);
   w.forks = (int4*)(base + forks);
   w.fresh = (int32_t*)(base + fresh);
+  w.plan = (int4*)(base + plan);
+  w.part = (float*)(base + part);
+  w.part_mz = (float2*)(base + part_mz);
   w.max_seqs = max_seqs;
   w.max_query_rows = max_query_rows;
   w.max_head_dim = max_head_dim;

@@ -16,6 +16,7 @@ namespace asl {
 constexpr uint32_t kFaultPaged = 2;        // bit of the fault word: a row, length, token or page number out of range
 constexpr int kPagedMaxSeqs = 4096;        // sequences of one call
 constexpr int kMaxFresh = 65536;           // pages that one call takes
+constexpr int kCutRows = 131072;           // rows of partial results beside one for each row's own and shared keys
 constexpr int kPagedMaxDim = 256;          // head_dim of asl_paged_attention
 
 struct PageMap {
