@@ -12,6 +12,10 @@
 // probabilities are the second product's operand where they stand, if the contraction takes the keys in the order
 // slot (g, j) = key 16 (j / 4) + 4 g + j % 4.  V rows are loaded in that order, 16 bytes of a row a lane, and turned with byte
 // permutes in registers: no LDS and no barrier until the four wavefronts join their results.
+//
+// attend_tile_kernel, for many rows (bf16): bound by the products.  Each wavefront has 16 MT rows of its own, and all four take the
+// same tiles of 64 keys from LDS, which are loaded there directly, into one of two buffers while the other is worked on: K as it
+// stands as an operand (lane by lane), V by rows; so reads have no bank conflicts.
 #include "paged.h"
 
 #include "asl_internal.h"
@@ -246,42 +250,89 @@ struct Source {
   int d;
 };
 
+// A uniform address, kept in scalar registers: lanes add 32-bit offsets to it.  (Without this the compiler adds the lanes' offsets to the
+// pages' address ahead of the loop, and keeps 64-bit sums in vector registers.)
+__device__ __forceinline__ const char* uniform(const char* p) {
+  const uint64_t x = (uint64_t)p;
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)x);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(x >> 32));
+  return (const char*)(((uint64_t)hi << 32) | lo);
+}
+
+// A lane's 32-bit offset where it is used: the compiler would widen it ahead of the loop, and then add 64 bits.
+__device__ __forceinline__ uint32_t offset(uint32_t x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
+// Elements e0 .. e0 + CW - 1 of the row at base + row, zeros beyond d.
 template <typename T, int D, bool PAD>
-__device__ __forceinline__ void load_block(Block<T, D>& b, const Source& s, int key0) {
+__device__ __forceinline__ void load_value(uint32_t* to, const char* base, uint32_t row, int e0, int d) {
+  typedef uint32_t Words __attribute__((ext_vector_type(Block<T, D>::VW)));
+  const bool in = !PAD || e0 < d;
+  const Words w = *(const Words*)(base + (row + (uint32_t)(in ? e0 : 0) * (uint32_t)sizeof(T)));
+#pragma unroll
+  for (int x = 0; x < Block<T, D>::VW; ++x) to[x] = in ? w[x] : 0u;
+}
+
+// Page numbers of the blocks that a wavefront comes to, each STEP keys behind the last and of SUB subtiles: 64 of them at a time, a lane
+// each, and the 64 behind them already on their way.  (A load for each block would be waited for before the block's own
+// loads can go out: a tile took 8 us instead of 1.3.)
+template <int SUB, int STEP>
+struct PageWindow {
+  static constexpr int kBlocks = 64 / SUB;
+  int cur, nxt, key, first;    // key: of block 0; first: block of cur's first lane
+
+  __device__ __forceinline__ int fetch(const Source& s, int block) const {
+    const int lane = threadIdx.x & 63;
+    const int k = min(key + (block + lane / SUB) * STEP + 16 * (lane % SUB), s.last);
+    return s.table[k >> s.shift];
+  }
+  __device__ __forceinline__ void start(const Source& s, int key0) {
+    key = key0;
+    first = 0;
+    cur = fetch(s, 0);
+    nxt = fetch(s, kBlocks);
+  }
+  __device__ __forceinline__ void move(const Source& s, int block) {
+    if (block - first < kBlocks) return;
+    cur = nxt;
+    first += kBlocks;
+    nxt = fetch(s, first + kBlocks);
+  }
+  __device__ __forceinline__ int page(int block, int t) const {
+    const int l = (block - first) * SUB + t;
+    const int from = l < 64 ? cur : nxt;
+    return __builtin_amdgcn_readlane(from, l & 63);
+  }
+};
+
+template <typename T, int D, bool PAD, typename W>
+__device__ __forceinline__ void load_block(Block<T, D>& b, const Source& s, const W& window, int block, int key0) {
   typedef Block<T, D> B;
   const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
   const char* base[B::SUB];
 #pragma unroll
   for (int t = 0; t < B::SUB; ++t) {
     const int key = min(key0 + 16 * t, s.last);
-    const int page = __builtin_amdgcn_readfirstlane(s.table[key >> s.shift]);
+    const int page = window.page(block, t);
     b.ok[t] = (uint32_t)page < (uint32_t)s.n_pages;
     const int64_t off = (int64_t)(b.ok[t] ? page : 0) * s.page + (int64_t)(key & (s.ps - 1)) * s.tok;
-    base[t] = s.v + off;
-    const char* kp = s.k + off + (int64_t)r * s.tok + g * 16;
+    base[t] = uniform(s.v + off);
+    const char* kb = uniform(s.k + off);
+    const uint32_t ko = (uint32_t)r * (uint32_t)s.tok + (uint32_t)g * 16u;
 #pragma unroll
     for (int p = 0; p < B::KP; ++p) {
-      if (PAD) {                                           // beyond d: the first piece again, then zeros
-        const bool in = (p * 64 + g * 16) < s.d * (int)sizeof(T);
-        const Piece x = *(const Piece*)(kp + (in ? p * 64 : -g * 16));
-        b.k[t][p] = in ? x : Piece{0, 0, 0, 0};
-      } else {
-        b.k[t][p] = *(const Piece*)(kp + p * 64);
-      }
+      const bool in = !PAD || p * 64 + g * 16 < s.d * (int)sizeof(T);    // beyond d: the row's first piece, then zeros
+      const Piece x = *(const Piece*)(kb + (in ? ko + p * 64u : (uint32_t)r * (uint32_t)s.tok));
+      b.k[t][p] = in ? x : Piece{0, 0, 0, 0};
     }
   }
 #pragma unroll
   for (int j = 0; j < B::VR; ++j) {
 #pragma unroll
-    for (int hf = 0; hf < B::HN; ++hf) {
-      const int e0 = 16 * B::CW * hf + B::CW * r;
-      const char* row = base[j >> 2] + (int64_t)(4 * g + (j & 3)) * s.tok;
-      const bool in = !PAD || e0 < s.d;
-      typedef uint32_t Words __attribute__((ext_vector_type(B::VW)));
-      const Words w = *(const Words*)(row + (in ? e0 : 0) * (int)sizeof(T));
-#pragma unroll
-      for (int x = 0; x < B::VW; ++x) b.v[j][hf][x] = in ? w[x] : 0u;
-    }
+    for (int hf = 0; hf < B::HN; ++hf)
+      load_value<T, D, PAD>(b.v[j][hf], base[j >> 2], (uint32_t)(4 * g + (j & 3)) * (uint32_t)s.tok, 16 * B::CW * hf + B::CW * r, s.d);
   }
 }
 
@@ -358,8 +409,10 @@ struct Rows {
   f32x4 o[MT][B::NT];
   float m[MT], z[MT];      // reference and, of this lane's keys, sum
   int lim[MT];
+  uint32_t odd;            // values were left out
 
   __device__ __forceinline__ void clear() {
+    odd = 0;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
       m[mt] = -INFINITY;
@@ -427,64 +480,34 @@ struct Rows {
     Weights<T> w[MT];
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) w[mt].set(p[mt]);
+    add<MASKED>(b.v, b.ok[0], b.ok[B::SUB - 1], key0, least, most, w);
+  }
+
+  // out += V^T w for a block of values, whose subtiles' page numbers are in range or not (ok0, ok1).
+  template <bool MASKED>
+  __device__ __forceinline__ void add(uint32_t (&v)[B::VR][B::HN][B::VW], bool ok0, bool ok1, int key0, int least, int most,
+                                      const Weights<T> (&w)[MT]) {
+    const int g = (threadIdx.x & 63) >> 4;
     if (MASKED) {
       // Probability 0 does not keep a value that is no number out of the sum.  Behind the last key that any row sees, and in pages out
-      // of range, values are replaced by zero; where rows differ in what they see, infinities and NaN are taken out and
-      // counted by class for the rows that see them (a product of zeros and ones), and each class added as itself.
-      uint32_t odd = 0;
+      // of range, values are replaced by zero; where rows differ in what they see, infinities and NaN are too, and add_odd
+      // brings them back for the rows that see them.
+      const bool differ = least < most;
 #pragma unroll
       for (int j = 0; j < B::VR; ++j) {
-        const uint32_t seen = b.ok[j >> 2] && key0 + B::v_key(j, g) < most ? ~0u : 0u;
+        const uint32_t seen = ((j >> 2) == 0 ? ok0 : ok1) && key0 + B::v_key(j, g) < most ? ~0u : 0u;
 #pragma unroll
         for (int hf = 0; hf < B::HN; ++hf)
 #pragma unroll
           for (int x2 = 0; x2 < B::VW; ++x2) {
-            b.v[j][hf][x2] &= seen;
-            odd |= not_finite<T>(b.v[j][hf][x2]);
-          }
-      }
-      if (least < most && __any(odd != 0)) {
-        Weights<T> see[MT];
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-          float one[B::SUB][4];
-#pragma unroll
-          for (int t = 0; t < B::SUB; ++t)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) one[t][i] = b.ok[t] && key0 + 16 * t + 4 * g + i < lim[mt] ? 1.f : 0.f;
-          see[mt].set(one);
-        }
-#pragma unroll 1
-        for (int c = 0; c < 3; ++c) {
-          const float what = c == 0 ? INFINITY : c == 1 ? -INFINITY : __uint_as_float(0x7fc00000u);
-#pragma unroll
-          for (int hf = 0; hf < B::HN; ++hf)
-#pragma unroll
-            for (int e = 0; e < B::CW; ++e) {
-              f32x4 n[MT];
-              f32x4* to[MT];
-#pragma unroll
-              for (int mt = 0; mt < MT; ++mt) {
-                n[mt] = f32x4{0.f, 0.f, 0.f, 0.f};
-                to[mt] = &n[mt];
-              }
-              add_values<T, MT>(to, see, hf, e, [&](int j, int hf2, int x2) {
-                uint32_t word = b.v[j][hf2][x2];
-                asm volatile("" : "+v"(word));             // or every word's classes are worked out and kept before the loop
-                return word_class<T>(word, c);
-              });
-#pragma unroll
-              for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) o[mt][hf * B::CW + e][i] += n[mt][i] > 0.f ? what : 0.f;
+            uint32_t y = v[j][hf][x2] & seen;
+            if (differ) {
+              const uint32_t bits = not_finite<T>(y);
+              odd |= bits;
+              y &= ~whole_elements<T>(bits);
             }
-        }
-#pragma unroll
-        for (int j = 0; j < B::VR; ++j)
-#pragma unroll
-          for (int hf = 0; hf < B::HN; ++hf)
-#pragma unroll
-            for (int x2 = 0; x2 < B::VW; ++x2) b.v[j][hf][x2] &= ~whole_elements<T>(not_finite<T>(b.v[j][hf][x2]));
+            v[j][hf][x2] = y;
+          }
       }
     }
 #pragma unroll
@@ -494,8 +517,78 @@ struct Rows {
         f32x4* to[MT];
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) to[mt] = &o[mt][hf * B::CW + e];
-        add_values<T, MT>(to, w, hf, e, [&](int j, int hf2, int x2) { return b.v[j][hf2][x2]; });
+        add_values<T, MT>(to, w, hf, e, [&](int j, int hf2, int x2) { return v[j][hf2][x2]; });
       }
+  }
+
+  // Infinite values and NaN of the blocks at key0, key0 + step, ... before end, which add<true> left out: counted by class for the rows
+  // that see them, as a product of zeros and ones, and each class added as itself.  (Rare, and apart from the steps: within them
+  // it would take their registers.)
+  template <bool PAD>
+  __device__ __forceinline__ void add_odd(const Source& s, int key0, int step, int end, int most) {
+    const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+#pragma unroll 1
+    for (; key0 < end; key0 += step) {
+      uint32_t v[B::VR][B::HN][B::VW], any = 0;
+      bool ok[B::SUB];
+      const char* base[B::SUB];
+#pragma unroll
+      for (int t = 0; t < B::SUB; ++t) {
+        const int key = min(key0 + 16 * t, s.last);
+        const int page = __builtin_amdgcn_readfirstlane(s.table[key >> s.shift]);
+        ok[t] = (uint32_t)page < (uint32_t)s.n_pages;
+        base[t] = s.v + (int64_t)(ok[t] ? page : 0) * s.page + (int64_t)(key & (s.ps - 1)) * s.tok;
+      }
+#pragma unroll
+      for (int j = 0; j < B::VR; ++j) {
+        const uint32_t seen = ok[j >> 2] && key0 + B::v_key(j, g) < most ? ~0u : 0u;
+#pragma unroll
+        for (int hf = 0; hf < B::HN; ++hf) {
+          load_value<T, D, PAD>(v[j][hf], base[j >> 2], (uint32_t)(4 * g + (j & 3)) * (uint32_t)s.tok, 16 * B::CW * hf + B::CW * r, s.d);
+#pragma unroll
+          for (int x2 = 0; x2 < B::VW; ++x2) {
+            v[j][hf][x2] &= seen;
+            any |= not_finite<T>(v[j][hf][x2]);
+          }
+        }
+      }
+      if (!__any(any != 0)) continue;
+      Weights<T> see[MT];
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) {
+        float one[B::SUB][4];
+#pragma unroll
+        for (int t = 0; t < B::SUB; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) one[t][i] = ok[t] && key0 + 16 * t + 4 * g + i < lim[mt] ? 1.f : 0.f;
+        see[mt].set(one);
+      }
+#pragma unroll 1
+      for (int c = 0; c < 3; ++c) {
+        const float what = c == 0 ? INFINITY : c == 1 ? -INFINITY : __uint_as_float(0x7fc00000u);
+#pragma unroll
+        for (int hf = 0; hf < B::HN; ++hf)
+#pragma unroll
+          for (int e = 0; e < B::CW; ++e) {
+            f32x4 n[MT];
+            f32x4* to[MT];
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+              n[mt] = f32x4{0.f, 0.f, 0.f, 0.f};
+              to[mt] = &n[mt];
+            }
+            add_values<T, MT>(to, see, hf, e, [&](int j, int hf2, int x2) {
+              uint32_t word = v[j][hf2][x2];
+              asm volatile("" : "+v"(word));               // or every word's classes are worked out and kept before the loop
+              return word_class<T>(word, c);
+            });
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) o[mt][hf * B::CW + e][i] += n[mt][i] > 0.f ? what : 0.f;
+          }
+      }
+    }
   }
 };
 
@@ -580,26 +673,34 @@ attend_split_kernel(AttendArgs a, AttendCut cut, Partials pt) {
   const float scale = a.scale * kLog2e;
   bool bad = false;
   auto whole = [&](const Block<T, D>& b) { return b.ok[0] && b.ok[B::SUB - 1]; };
+  PageWindow<B::SUB, STEP> window;
+  int block = 0;
+  if (key < end) window.start(src, key);
   // blocks that every row sees, the next one on its way while one is worked on
   if (key + B::KEYS <= min(end, (int)least)) {
     Block<T, D> cur, nxt;
-    load_block<T, D, PAD>(cur, src, key);
+    load_block<T, D, PAD>(cur, src, window, block, key);
     while (whole(cur)) {
       const bool more = key + STEP + B::KEYS <= min(end, (int)least);
-      if (more) load_block<T, D, PAD>(nxt, src, key + STEP);
+      if (more) load_block<T, D, PAD>(nxt, src, window, block + 1, key + STEP);
       rows.template step<false>(cur, key, (int)least, (int)most, scale);
       key += STEP;
+      window.move(src, ++block);
       if (!more) break;
       cur = nxt;
     }
   }
   // the last ones, and all from a page number out of range on
-  for (; key < end; key += STEP) {
+  const int from = key;
+  while (key < end) {
     Block<T, D> b;
-    load_block<T, D, PAD>(b, src, key);
+    load_block<T, D, PAD>(b, src, window, block, key);
     bad = bad || !whole(b);
     rows.template step<true>(b, key, (int)least, (int)most, scale);
+    key += STEP;
+    window.move(src, ++block);
   }
+  if (__any(rows.odd != 0)) rows.template add_odd<PAD>(src, from, STEP, end, (int)most);
   if (bad && lane == 0) atomicOr(a.map.fault, kFaultPaged);
   // the wavefronts' results are joined, 16 threads a row
 #pragma unroll
@@ -645,6 +746,221 @@ attend_split_kernel(AttendArgs a, AttendCut cut, Partials pt) {
         write_row<T, CNT>(a, it, pt, D, r, at, v, m, total);
       }
     }
+  }
+}
+
+// ------------------------------------------------------------------------------------------------------------------
+// Many rows.  bf16.  A tile of 64 keys in LDS: of K the operands (subtile t, piece p, lane), of V the rows.
+
+template <int D>
+struct TileBuffer {
+  Piece k[kKeyTile / 16][D / 32][64];
+  Piece v[kKeyTile][D / 8];
+};
+
+// Sends for a tile, straight to LDS: wavefront w has the 16 keys of subtile w.  (The hardware puts lane i's 16 bytes at the given
+// place + 16 i.)  Bit t of the result: subtile t's page number is in range; page 0 stands in for one that is not.
+template <int D, bool PAD>
+__device__ __forceinline__ uint32_t fetch_tile(TileBuffer<D>& to, const Source& s, const PageWindow<4, kKeyTile>& window, int block,
+                                               int key0) {
+  typedef const __attribute__((address_space(1))) void* Global;
+  typedef __attribute__((address_space(3))) void* Lds;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
+  uint32_t ok = 0;
+#pragma unroll
+  for (int t = 0; t < 4; ++t) ok |= ((uint32_t)window.page(block, t) < (uint32_t)s.n_pages ? 1u : 0u) << t;
+  const int page = ((ok >> wave) & 1u) != 0 ? window.page(block, wave) : 0;
+  const int64_t off = (int64_t)page * s.page + (int64_t)(min(key0 + 16 * wave, s.last) & (s.ps - 1)) * s.tok;
+  const char* kb = uniform(s.k + off);
+  const uint32_t ko = (uint32_t)r * (uint32_t)s.tok + (uint32_t)g * 16u;
+#pragma unroll
+  for (int p = 0; p < D / 32; ++p) {
+    const bool in = !PAD || p * 64 + g * 16 < s.d * 2;     // beyond d: the row's first piece (read as zeros)
+    __builtin_amdgcn_global_load_lds((Global)(kb + offset(in ? ko + p * 64u : ko - g * 16u)), (Lds)&to.k[wave][p][0], 16, 0, 0);
+  }
+  constexpr int PR = D / 8, RPI = 64 / PR;                 // pieces of a row, rows of an instruction
+  const int piece = !PAD || (lane % PR) * 8 < s.d ? lane % PR : 0;
+  const uint32_t vo = (uint32_t)(lane / PR) * (uint32_t)s.tok + (uint32_t)piece * 16u;
+#pragma unroll
+  for (int i = 0; i < 16 / RPI; ++i)
+    __builtin_amdgcn_global_load_lds((Global)(uniform(s.v + off + (int64_t)i * RPI * s.tok) + offset(vo)), (Lds)&to.v[16 * wave + i * RPI][0], 16, 0, 0);
+  return ok;
+}
+
+// A wavefront's step over a tile in LDS.
+template <int D, int MT, bool PAD, bool MASKED>
+__device__ __forceinline__ void tile_step(Rows<__bf16, D, MT>& R, const TileBuffer<D>& b, int key0, uint32_t ok, int least, int most,
+                                          int d, float scale) {
+  typedef Block<__bf16, D> B;
+  const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+  f32x4 x[MT][4];
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) x[mt][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int p = 0; p < B::KP; ++p) {
+      Piece k = b.k[t][p][lane];
+      if (PAD && p * 32 + g * 8 >= d) k = Piece{0, 0, 0, 0};
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+        x[mt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, R.q[mt][p]),
+                                                           x[mt][t], 0, 0, 0);
+    }
+  }
+  Weights<__bf16> w[2][MT];
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    float top = -INFINITY;
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float y = x[mt][t][i] * scale;
+        if (MASKED) y = ((ok >> t) & 1u) != 0 && key0 + 16 * t + 4 * g + i < R.lim[mt] ? y : -INFINITY;
+        x[mt][t][i] = y;
+        top = fmaxf(top, y);
+      }
+    if (__any(top > R.m[mt] + kSlack)) {
+      const float to = fmaxf(R.m[mt], max_over_g(top));
+      const float by = to == -INFINITY ? 1.f : exp2_fast(R.m[mt] - to);
+      R.m[mt] = to;
+      R.z[mt] *= by;
+#pragma unroll
+      for (int t = 0; t < B::NT; ++t) R.o[mt][t] *= by;
+    }
+    const float base = R.m[mt] == -INFINITY ? 0.f : R.m[mt];
+#pragma unroll
+    for (int hb = 0; hb < 2; ++hb) {
+      float p[2][4];
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          p[t][i] = exp2_fast(x[mt][2 * hb + t][i] - base);
+          R.z[mt] += p[t][i];
+        }
+      w[hb][mt].set(p);
+    }
+  }
+#pragma unroll
+  for (int hb = 0; hb < 2; ++hb) {
+    if (MASKED) asm volatile("" ::: "memory");             // the reads stay here: earlier there is no register for them
+    uint32_t v[B::VR][B::HN][B::VW];
+#pragma unroll
+    for (int j = 0; j < B::VR; ++j)
+#pragma unroll
+      for (int hf = 0; hf < B::HN; ++hf) {
+        typedef uint32_t Words __attribute__((ext_vector_type(B::VW)));
+        const Words y = *(const Words*)((const char*)&b.v[32 * hb + B::v_key(j, g)][0] + (16 * B::CW * hf + B::CW * r) * 2);
+#pragma unroll
+        for (int x2 = 0; x2 < B::VW; ++x2) v[j][hf][x2] = y[x2];
+      }
+    R.template add<MASKED>(v, ((ok >> (2 * hb)) & 1u) != 0, ((ok >> (2 * hb + 1)) & 1u) != 0, key0 + 32 * hb, least, most, w[hb]);
+  }
+}
+
+template <int D, int MT, bool PAD, bool SHARED>
+__global__ void __launch_bounds__(kThreads, 2) attend_tile_kernel(AttendArgs a, AttendCut cut, Partials pt) {
+  typedef Block<__bf16, D> B;
+  __shared__ TileBuffer<D> buf[2];
+  __shared__ int lims[2][kWaves];
+  Item it;
+  if (!find_item<SHARED>(a, cut, (int)blockIdx.x, pt.plan, &it)) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r16 = lane & 15, g = lane >> 4;
+  const int row0 = it.tile * cut.rows + wave * 16 * MT;
+  Rows<__bf16, D, MT> rows;
+  rows.clear();
+  uint32_t least = 0x7fffffffu, most = 0;
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    const int r = row0 + 16 * mt + r16;
+    const bool in = r < it.seg.rows;
+    rows.lim[mt] = in ? row_limit<SHARED>(a, it.seg, r) : 0;
+    least = min(least, in ? (uint32_t)rows.lim[mt] : 0x7fffffffu);
+    most = max(most, (uint32_t)rows.lim[mt]);
+    const int i = (int)((uint32_t)r / (uint32_t)a.G);
+    const __bf16* q = (const __bf16*)a.q + (int64_t)(it.seg.c0 + i) * a.qt + (int64_t)(it.h * a.G + (r - i * a.G)) * a.qh;
+#pragma unroll
+    for (int p = 0; p < B::KP; ++p) {
+      const int e = p * 32 + g * 8;
+      rows.q[mt][p] = in && e < a.d ? *(const Piece*)(q + e) : Piece{0, 0, 0, 0};
+    }
+  }
+  least = wave_min(least);
+  most = wave_max(most);
+  // keys that all rows of the workgroup see, that any does
+  if (lane == 0) {
+    lims[0][wave] = (int)least;
+    lims[1][wave] = (int)most;
+  }
+  __syncthreads();
+  const int all_see = __builtin_amdgcn_readfirstlane(min(min(lims[0][0], lims[0][1]), min(lims[0][2], lims[0][3])));
+  const int any_sees = __builtin_amdgcn_readfirstlane(max(max(lims[1][0], lims[1][1]), max(lims[1][2], lims[1][3])));
+  Source src;
+  src.k = (const char*)a.k + (int64_t)it.h * a.map.head;
+  src.v = (const char*)a.v + (int64_t)it.h * a.map.head;
+  src.table = a.map.table + (int64_t)it.seg.row * a.map.row_stride;
+  src.page = a.map.page;
+  src.tok = a.map.tok;
+  src.n_pages = a.map.n_pages;
+  src.ps = a.map.ps;
+  src.shift = a.map.ps_shift;
+  src.last = (it.seg.len - 1) & ~15;
+  src.d = a.d;
+  int t0, t1;
+  split_range(min(it.seg.span, max(0, (any_sees + kKeyTile - 1) / kKeyTile - it.seg.t0)), it.splits, it.split, &t0, &t1);
+  const float scale = a.scale * kLog2e;
+  bool bad = false;
+  if (t0 < t1) {
+    PageWindow<4, kKeyTile> window;
+    window.start(src, (it.seg.t0 + t0) * kKeyTile);
+    uint32_t ok = fetch_tile<D, PAD>(buf[0], src, window, 0, (it.seg.t0 + t0) * kKeyTile);
+    int t = t0;
+    // tile t's pieces have landed, everybody's after the barrier, behind which nobody reads the other buffer any more: the next go there
+    auto next = [&]() {
+      __builtin_amdgcn_s_waitcnt(0x0070);                  // vmcnt 0, lgkmcnt 0
+      __syncthreads();
+      const uint32_t here = ok;
+      if (t + 1 < t1) ok = fetch_tile<D, PAD>(buf[(t + 1 - t0) & 1], src, window, t + 1 - t0, (it.seg.t0 + t + 1) * kKeyTile);
+      return here;
+    };
+    // tiles that every row sees
+    while (t < t1 && ok == 15u && (it.seg.t0 + t + 1) * kKeyTile <= all_see) {
+      next();
+      tile_step<D, MT, PAD, false>(rows, buf[(t - t0) & 1], (it.seg.t0 + t) * kKeyTile, 15u, (int)least, (int)most, a.d, scale);
+      ++t;
+      window.move(src, t - t0);
+    }
+    // the last ones, and all from a page number out of range on
+    const int from = (it.seg.t0 + t) * kKeyTile;
+    while (t < t1) {
+      const uint32_t here = next();
+      const int key0 = (it.seg.t0 + t) * kKeyTile;
+      bad = bad || here != 15u;
+      if (key0 < (int)most)
+        tile_step<D, MT, PAD, true>(rows, buf[(t - t0) & 1], key0, here, (int)least, (int)most, a.d, scale);
+      ++t;
+      window.move(src, t - t0);
+    }
+    if (__any(rows.odd != 0))
+      rows.template add_odd<PAD>(src, from, B::KEYS, min((it.seg.t0 + t1) * kKeyTile, (int)most), (int)most);
+  }
+  if (bad && lane == 0) atomicOr(a.map.fault, kFaultPaged);
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    const int r = row0 + 16 * mt + r16;
+    const float z = sum_over_g(rows.z[mt]);
+    if (r >= it.seg.rows) continue;
+#pragma unroll
+    for (int hf = 0; hf < B::HN; ++hf)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float v[B::CW];
+#pragma unroll
+        for (int e = 0; e < B::CW; ++e) v[e] = rows.o[mt][hf * B::CW + e][i];
+        write_row<__bf16, B::CW>(a, it, pt, D, r, 16 * B::CW * hf + B::CW * (4 * g + i), v, rows.m[mt], z);
+      }
   }
 }
 
@@ -742,27 +1058,47 @@ __global__ void __launch_bounds__(kThreads) attend_join_kernel(AttendArgs a, Par
   if (lane == 0 && a.lse != nullptr) a.lse[(int64_t)hq * a.total_q + tok] = z == 0.f ? -INFINITY : (m + __log2f(z)) * kLn2;
 }
 
-template <typename T, int D, int MT, bool SHARED>
-hipError_t launch_split(const AttendArgs& a, const AttendCut& cut, const Partials& pt, hipStream_t st) {
+// A launch over one kind of segments: the tile kernel from 33 rows of a segment on (bf16, d <= 128), else the split one.
+template <typename T, int D, bool SHARED, bool PAD>
+hipError_t launch_cut(const AttendArgs& a, const AttendCut& cut, const Partials& pt, hipStream_t st) {
   const int64_t items = max_items(cut, (int64_t)a.total_q * a.G, SHARED ? a.n_groups : a.n_seqs, a.Hk);
   if (items >= (int64_t(1) << 31)) return hipErrorInvalidValue;
-  if (a.d == D)
-    hipLaunchKernelGGL((attend_split_kernel<T, D, MT, false, SHARED>), dim3((unsigned)items), dim3(kThreads), 0, st, a, cut, pt);
-  else
-    hipLaunchKernelGGL((attend_split_kernel<T, D, MT, true, SHARED>), dim3((unsigned)items), dim3(kThreads), 0, st, a, cut, pt);
+  const dim3 grid((unsigned)items), block(kThreads);
+  if constexpr (sizeof(T) == 2 && D <= 128) {
+    if (cut.rows == 128) {
+      hipLaunchKernelGGL((attend_tile_kernel<D, 2, PAD, SHARED>), grid, block, 0, st, a, cut, pt);
+      return hipGetLastError();
+    }
+    if (cut.rows == 64) {
+      hipLaunchKernelGGL((attend_tile_kernel<D, 1, PAD, SHARED>), grid, block, 0, st, a, cut, pt);
+      return hipGetLastError();
+    }
+  }
+  hipLaunchKernelGGL((attend_split_kernel<T, D, 1, PAD, SHARED>), grid, block, 0, st, a, cut, pt);
   return hipGetLastError();
+}
+
+AttendCut cut_for(bool tiles, int64_t rows) {
+  AttendCut c = {16, 512, 2, 0};
+  if (tiles && rows > 32) {
+    c.rows = rows > 64 ? 128 : 64;
+    c.min_tiles = 4;
+  }
+  return c;
 }
 
 template <typename T, int D>
 hipError_t launch_d(const PagedWorkspace& ws, const AttendArgs& args, hipStream_t st) {
   AttendArgs a = args;
-  const int64_t rows = (int64_t)a.total_q * a.G;
-  constexpr int kTarget = 512;
-  AttendCut own = {16, kTarget, 2, 0}, shared = {16, kTarget, 2, 0};
+  constexpr bool kTiles = sizeof(T) == 2 && D <= 128;
+  const int64_t rows = (int64_t)a.total_q * a.G;           // of a KV head
+  const int64_t most = (int64_t)a.max_q_len * a.G < rows ? (int64_t)a.max_q_len * a.G : rows;
+  AttendCut own = cut_for(kTiles, most), shared = cut_for(kTiles, a.n_groups > 0 ? rows / a.n_groups : 0);
   const int64_t room = ws.part_rows;
   shared.cap = max_partials(shared, rows, a.Hk);
-  // every row of a group is joined from two parts: there has to be room for them
-  if (a.n_groups > 0 && shared.cap + rows * a.Hk > room) a.n_groups = 0;
+  // a sequence whose own rows fill a tile gains nothing; and every row of a group is joined from two parts, for which there has to be
+  // room
+  if (a.n_groups > 0 && (most > 64 || shared.cap + rows * a.Hk > room)) a.n_groups = 0;
   if (a.n_groups == 0) shared.cap = 0;
   own.cap = room - shared.cap;
   Partials po, ps;
@@ -773,8 +1109,8 @@ hipError_t launch_d(const PagedWorkspace& ws, const AttendArgs& args, hipStream_
   po.mz = ws.part_mz + shared.cap;
   po.plan = ws.plan;
   hipError_t e = hipSuccess;
-  if (a.n_groups > 0) e = launch_split<T, D, 1, true>(a, shared, ps, st);
-  if (e == hipSuccess) e = launch_split<T, D, 1, false>(a, own, po, st);
+  if (a.n_groups > 0) e = a.d == D ? launch_cut<T, D, true, false>(a, shared, ps, st) : launch_cut<T, D, true, true>(a, shared, ps, st);
+  if (e == hipSuccess) e = a.d == D ? launch_cut<T, D, false, false>(a, own, po, st) : launch_cut<T, D, false, true>(a, own, po, st);
   if (e != hipSuccess) return e;
   const int64_t out_rows = (int64_t)a.total_q * a.Hq;
   if (out_rows <= 2048)

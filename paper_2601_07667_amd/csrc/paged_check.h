@@ -40,6 +40,7 @@ inline asl_status pages_status(const asl_pages* p, const char** why) {
   if (!whole_pieces(p->head_dim, p->dtype) || !whole_pieces(p->stride_tok, p->dtype) ||
       !whole_pieces(p->stride_head, p->dtype) || !whole_pieces(p->stride_page, p->dtype))
     return no(ASL_EUNSUPPORTED, "rows and strides of pages must be multiples of 16 bytes");
+  if (p->stride_tok > (int64_t(1) << 24)) return no(ASL_EUNSUPPORTED, "a token stride of more than 2^24 elements");
   return ASL_OK;
 }
 
