@@ -15,7 +15,8 @@
 //
 // attend_tile_kernel, for many rows (bf16): bound by the products.  Each wavefront has 16 MT rows of its own, and all four take the
 // same tiles of 64 keys from LDS, which are loaded there directly, into one of two buffers while the other is worked on: K as it
-// stands as an operand (lane by lane), V by rows; so reads have no bank conflicts.
+// stands as an operand (lane by lane), V by rows with their 16-byte pieces exchanged, so that the transposing reads that
+// make operands of it (ds_read_b64_tr_b16) have no bank conflicts either.
 #include "paged.h"
 
 #include "asl_internal.h"
@@ -36,6 +37,9 @@ constexpr float kLn2 = 0.6931471805599453f;
 // A row's reference moves when a logit exceeds it by more than this (in units of log 2): probabilities stay below 2^8 and most
 // blocks need no maximum over lanes and no rescaling.
 constexpr float kSlack = 8.f;
+// The same where a row's reference cannot move in place: probabilities up to 2^60 lose nothing in fp32 and bf16 (a result is a
+// quotient of two such sums), and only a row whose first tile was that much lower than a later one needs the step that moves it.
+constexpr float kWideSlack = 60.f;
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -521,17 +525,17 @@ struct Rows {
       }
   }
 
-  // Infinite values and NaN of the blocks at key0, key0 + step, ... before end, which add<true> left out: counted by class for the rows
-  // that see them, as a product of zeros and ones, and each class added as itself.  (Rare, and apart from the steps: within them
-  // it would take their registers.)
-  template <bool PAD>
+  // Infinite values and NaN of the blocks at key0, key0 + step, ... before end, which the masked steps left out: counted by class for the
+  // rows that see them, as a product of zeros and ones, and each class added as itself.  (Rare, and apart from the steps:
+  // within them it would take their registers.)  ROWWISE: accumulator t has elements 16 t .. 16 t + 15 of out.
+  template <bool ROWWISE>
   __device__ __forceinline__ void add_odd(const Source& s, int key0, int step, int end, int most) {
     const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
 #pragma unroll 1
     for (; key0 < end; key0 += step) {
-      uint32_t v[B::VR][B::HN][B::VW], any = 0;
       bool ok[B::SUB];
       const char* base[B::SUB];
+      Weights<T> see[MT];
 #pragma unroll
       for (int t = 0; t < B::SUB; ++t) {
         const int key = min(key0 + 16 * t, s.last);
@@ -539,21 +543,6 @@ struct Rows {
         ok[t] = (uint32_t)page < (uint32_t)s.n_pages;
         base[t] = s.v + (int64_t)(ok[t] ? page : 0) * s.page + (int64_t)(key & (s.ps - 1)) * s.tok;
       }
-#pragma unroll
-      for (int j = 0; j < B::VR; ++j) {
-        const uint32_t seen = ok[j >> 2] && key0 + B::v_key(j, g) < most ? ~0u : 0u;
-#pragma unroll
-        for (int hf = 0; hf < B::HN; ++hf) {
-          load_value<T, D, PAD>(v[j][hf], base[j >> 2], (uint32_t)(4 * g + (j & 3)) * (uint32_t)s.tok, 16 * B::CW * hf + B::CW * r, s.d);
-#pragma unroll
-          for (int x2 = 0; x2 < B::VW; ++x2) {
-            v[j][hf][x2] &= seen;
-            any |= not_finite<T>(v[j][hf][x2]);
-          }
-        }
-      }
-      if (!__any(any != 0)) continue;
-      Weights<T> see[MT];
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) {
         float one[B::SUB][4];
@@ -563,30 +552,37 @@ struct Rows {
           for (int i = 0; i < 4; ++i) one[t][i] = ok[t] && key0 + 16 * t + 4 * g + i < lim[mt] ? 1.f : 0.f;
         see[mt].set(one);
       }
-#pragma unroll 1
-      for (int c = 0; c < 3; ++c) {
-        const float what = c == 0 ? INFINITY : c == 1 ? -INFINITY : __uint_as_float(0x7fc00000u);
 #pragma unroll
-        for (int hf = 0; hf < B::HN; ++hf)
+      for (int t = 0; t < B::NT; ++t) {
+        const int e = ROWWISE ? 16 * t + r : 16 * B::CW * (t / B::CW) + B::CW * r + t % B::CW;
+        uint32_t v[B::VR], any = 0;                        // the element of each key's row, alone in a word
 #pragma unroll
-          for (int e = 0; e < B::CW; ++e) {
-            f32x4 n[MT];
-            f32x4* to[MT];
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-              n[mt] = f32x4{0.f, 0.f, 0.f, 0.f};
-              to[mt] = &n[mt];
-            }
-            add_values<T, MT>(to, see, hf, e, [&](int j, int hf2, int x2) {
-              uint32_t word = v[j][hf2][x2];
-              asm volatile("" : "+v"(word));               // or every word's classes are worked out and kept before the loop
-              return word_class<T>(word, c);
-            });
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-              for (int i = 0; i < 4; ++i) o[mt][hf * B::CW + e][i] += n[mt][i] > 0.f ? what : 0.f;
+        for (int j = 0; j < B::VR; ++j) {
+          v[j] = 0;
+          if (ok[j >> 2] && key0 + B::v_key(j, g) < most && e < s.d) {
+            const char* at = base[j >> 2] + (int64_t)(4 * g + (j & 3)) * s.tok + (int64_t)e * (int)sizeof(T);
+            v[j] = B::kBf16 ? (uint32_t)*(const uint16_t*)at : *(const uint32_t*)at;
           }
+          any |= not_finite<T>(v[j]);
+        }
+        if (!__any(any != 0)) continue;
+#pragma unroll 1
+        for (int c = 0; c < 3; ++c) {
+          const float what = c == 0 ? INFINITY : c == 1 ? -INFINITY : __uint_as_float(0x7fc00000u);
+          f32x4 n[MT];
+          f32x4* to[MT];
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt) {
+            n[mt] = f32x4{0.f, 0.f, 0.f, 0.f};
+            to[mt] = &n[mt];
+          }
+          // (turn(): the even element of each word)
+          add_values<T, MT>(to, see, 0, 0, [&](int j, int, int) { return word_class<T>(v[j], c); });
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[mt][t][i] += n[mt][i] > 0.f ? what : 0.f;
+        }
       }
     }
   }
@@ -700,7 +696,7 @@ attend_split_kernel(AttendArgs a, AttendCut cut, Partials pt) {
     key += STEP;
     window.move(src, ++block);
   }
-  if (__any(rows.odd != 0)) rows.template add_odd<PAD>(src, from, STEP, end, (int)most);
+  if (__any(rows.odd != 0)) rows.template add_odd<false>(src, from, STEP, end, (int)most);
   if (bad && lane == 0) atomicOr(a.map.fault, kFaultPaged);
   // the wavefronts' results are joined, 16 threads a row
 #pragma unroll
@@ -750,13 +746,18 @@ attend_split_kernel(AttendArgs a, AttendCut cut, Partials pt) {
 }
 
 // ------------------------------------------------------------------------------------------------------------------
-// Many rows.  bf16.  A tile of 64 keys in LDS: of K the operands (subtile t, piece p, lane), of V the rows.
+// Many rows.  bf16.  A tile of 64 keys in LDS: of K the operands (subtile t, piece p, lane), of V the rows, piece c of key k at
+// c ^ v_swap(k).  A transposing read takes 32 bytes of each of 16 keys' rows, four keys at a time; the exchange puts those of
+// four neighbouring keys into different quarters of 128 bytes.
 
 template <int D>
 struct TileBuffer {
   Piece k[kKeyTile / 16][D / 32][64];
   Piece v[kKeyTile][D / 8];
 };
+
+template <int D>
+__device__ __forceinline__ int v_swap(int key) { return 2 * (key & (D >= 128 ? 7 : 3)); }
 
 // Sends for a tile, straight to LDS: wavefront w has the 16 keys of subtile w.  (The hardware puts lane i's 16 bytes at the given
 // place + 16 i.)  Bit t of the result: subtile t's page number is in range; page 0 stands in for one that is not.
@@ -776,39 +777,70 @@ __device__ __forceinline__ uint32_t fetch_tile(TileBuffer<D>& to, const Source& 
 #pragma unroll
   for (int p = 0; p < D / 32; ++p) {
     const bool in = !PAD || p * 64 + g * 16 < s.d * 2;     // beyond d: the row's first piece (read as zeros)
-    __builtin_amdgcn_global_load_lds((Global)(kb + offset(in ? ko + p * 64u : ko - g * 16u)), (Lds)&to.k[wave][p][0], 16, 0, 0);
+    __builtin_amdgcn_global_load_lds((Global)(uniform(kb + (PAD ? 0 : p * 64)) + offset(!PAD ? ko : in ? ko + p * 64u : ko - g * 16u)),
+                                     (Lds)&to.k[wave][p][0], 16, 0, 0);
   }
   constexpr int PR = D / 8, RPI = 64 / PR;                 // pieces of a row, rows of an instruction
-  const int piece = !PAD || (lane % PR) * 8 < s.d ? lane % PR : 0;
-  const uint32_t vo = (uint32_t)(lane / PR) * (uint32_t)s.tok + (uint32_t)piece * 16u;
 #pragma unroll
-  for (int i = 0; i < 16 / RPI; ++i)
+  for (int i = 0; i < 16 / RPI; ++i) {
+    const int piece = (lane % PR) ^ v_swap<D>(i * RPI + lane / PR);
+    const uint32_t vo = (uint32_t)(lane / PR) * (uint32_t)s.tok + (!PAD || piece * 8 < s.d ? (uint32_t)piece * 16u : 0u);
     __builtin_amdgcn_global_load_lds((Global)(uniform(s.v + off + (int64_t)i * RPI * s.tok) + offset(vo)), (Lds)&to.v[16 * wave + i * RPI][0], 16, 0, 0);
+  }
   return ok;
 }
 
-// A wavefront's step over a tile in LDS.
+// A wavefront's step over a tile in LDS.  MASKED: some row may not see some key, or its reference may have to move.  Else every row
+// sees every key and no reference moves; returns false, nothing done, if one has to.  (A branch that rescales the accumulators
+// makes the compiler keep them twice, which does not fit: a tile of 128 rows took 4.6 us with it.)
 template <int D, int MT, bool PAD, bool MASKED>
-__device__ __forceinline__ void tile_step(Rows<__bf16, D, MT>& R, const TileBuffer<D>& b, int key0, uint32_t ok, int least, int most,
+__device__ __forceinline__ bool tile_step(Rows<__bf16, D, MT>& R, const TileBuffer<D>& b, int key0, uint32_t ok, int least, int most,
                                           int d, float scale) {
   typedef Block<__bf16, D> B;
   const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+  // Reads from LDS are a step ahead of the products that take them, and held there: left alone the scheduler gathers more of them
+  // than there are registers for.
   f32x4 x[MT][4];
+  Piece kf[2][B::KP];
+  auto read_k = [&](int t) {
+#pragma unroll
+    for (int p = 0; p < B::KP; ++p) kf[t & 1][p] = b.k[t][p][lane];
+  };
+  read_k(0);
 #pragma unroll
   for (int t = 0; t < 4; ++t) {
+    if (t < 3) read_k(t + 1);
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) x[mt][t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int p = 0; p < B::KP; ++p) {
-      Piece k = b.k[t][p][lane];
+      Piece k = kf[t & 1][p];
       if (PAD && p * 32 + g * 8 >= d) k = Piece{0, 0, 0, 0};
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt)
         x[mt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, R.q[mt][p]),
                                                            x[mt][t], 0, 0, 0);
     }
+    __builtin_amdgcn_sched_barrier(0);
   }
+  // V: lanes 4 j + c of 16 name columns 4 c .. 4 c + 3 of key j, lane i gets column i of the four keys
+  typedef short Half4 __attribute__((ext_vector_type(4)));
+  typedef __attribute__((address_space(3))) Half4* LdsHalf4;
+  union Values { Half4 h[2]; uint32_t u[4]; bf16x8 v; };
+  constexpr int STEPS = 2 * B::NT, AHEAD = 2;
+  Values vf[AHEAD + 1];
+  const uint32_t swap = offset((uint32_t)(v_swap<D>(4 * g + (r >> 2)) ^ ((r >> 1) & 1)) << 4);
+  const char* vrow = (const char*)&b.v[4 * g + (r >> 2)][0] + (r & 1) * 8;
+  auto read_v = [&](int i) {
+    const int hb = i / B::NT, nt = i % B::NT;
+    const char* at = vrow + ((uint32_t)(nt << 5) ^ swap);
+    vf[i % (AHEAD + 1)].h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsHalf4)(at + (32 * hb) * (D * 2)));
+    vf[i % (AHEAD + 1)].h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsHalf4)(at + (32 * hb + 16) * (D * 2)));
+  };
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) read_v(i);
   Weights<__bf16> w[2][MT];
+  float tops[MT];
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
     float top = -INFINITY;
@@ -816,19 +848,30 @@ __device__ __forceinline__ void tile_step(Rows<__bf16, D, MT>& R, const TileBuff
     for (int t = 0; t < 4; ++t)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        float y = x[mt][t][i] * scale;
-        if (MASKED) y = ((ok >> t) & 1u) != 0 && key0 + 16 * t + 4 * g + i < R.lim[mt] ? y : -INFINITY;
-        x[mt][t][i] = y;
-        top = fmaxf(top, y);
+        if (MASKED) x[mt][t][i] = ((ok >> t) & 1u) != 0 && key0 + 16 * t + 4 * g + i < R.lim[mt] ? x[mt][t][i] : -INFINITY;
+        top = fmaxf(top, x[mt][t][i]);
       }
-    if (__any(top > R.m[mt] + kSlack)) {
-      const float to = fmaxf(R.m[mt], max_over_g(top));
-      const float by = to == -INFINITY ? 1.f : exp2_fast(R.m[mt] - to);
-      R.m[mt] = to;
-      R.z[mt] *= by;
+    tops[mt] = top * scale;
+  }
+  if (MASKED) {
 #pragma unroll
-      for (int t = 0; t < B::NT; ++t) R.o[mt][t] *= by;
-    }
+    for (int mt = 0; mt < MT; ++mt)
+      if (__any(tops[mt] > R.m[mt] + kSlack)) {
+        const float to = fmaxf(R.m[mt], max_over_g(tops[mt]));
+        const float by = to == -INFINITY ? 1.f : exp2_fast(R.m[mt] - to);
+        R.m[mt] = to;
+        R.z[mt] *= by;
+#pragma unroll
+        for (int t = 0; t < B::NT; ++t) R.o[mt][t] *= by;
+      }
+  } else {
+    bool rises = false;
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) rises = rises || tops[mt] > R.m[mt] + kWideSlack;
+    if (__any(rises)) return false;
+  }
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
     const float base = R.m[mt] == -INFINITY ? 0.f : R.m[mt];
 #pragma unroll
     for (int hb = 0; hb < 2; ++hb) {
@@ -837,27 +880,46 @@ __device__ __forceinline__ void tile_step(Rows<__bf16, D, MT>& R, const TileBuff
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          p[t][i] = exp2_fast(x[mt][2 * hb + t][i] - base);
+          p[t][i] = exp2_fast(__builtin_fmaf(x[mt][2 * hb + t][i], scale, -base));
           R.z[mt] += p[t][i];
         }
       w[hb][mt].set(p);
     }
   }
+  uint32_t seen[2][4];                                     // of the two keys of each word, those that any of the rows sees
+  if (MASKED) {
 #pragma unroll
-  for (int hb = 0; hb < 2; ++hb) {
-    if (MASKED) asm volatile("" ::: "memory");             // the reads stay here: earlier there is no register for them
-    uint32_t v[B::VR][B::HN][B::VW];
+    for (int hb = 0; hb < 2; ++hb)
 #pragma unroll
-    for (int j = 0; j < B::VR; ++j)
-#pragma unroll
-      for (int hf = 0; hf < B::HN; ++hf) {
-        typedef uint32_t Words __attribute__((ext_vector_type(B::VW)));
-        const Words y = *(const Words*)((const char*)&b.v[32 * hb + B::v_key(j, g)][0] + (16 * B::CW * hf + B::CW * r) * 2);
-#pragma unroll
-        for (int x2 = 0; x2 < B::VW; ++x2) v[j][hf][x2] = y[x2];
+      for (int p = 0; p < 4; ++p) {
+        const int key = key0 + 32 * hb + B::v_key(2 * p, g);
+        const bool in = ((ok >> (2 * hb + (p >> 1))) & 1u) != 0;
+        seen[hb][p] = (in && key < most ? 0xffffu : 0u) | (in && key + 1 < most ? 0xffff0000u : 0u);
       }
-    R.template add<MASKED>(v, ((ok >> (2 * hb)) & 1u) != 0, ((ok >> (2 * hb + 1)) & 1u) != 0, key0 + 32 * hb, least, most, w[hb]);
   }
+#pragma unroll
+  for (int i = 0; i < STEPS; ++i) {
+    const int hb = i / B::NT, nt = i % B::NT;
+    if (i + AHEAD < STEPS) read_v(i + AHEAD);
+    Values& y = vf[i % (AHEAD + 1)];
+    if (MASKED) {                                          // as in Rows::add
+      const bool differ = least < most;
+#pragma unroll
+      for (int p = 0; p < 4; ++p) {
+        y.u[p] &= seen[hb][p];
+        if (differ) {
+          const uint32_t bits = not_finite<__bf16>(y.u[p]);
+          R.odd |= bits;
+          y.u[p] &= ~whole_elements<__bf16>(bits);
+        }
+      }
+    }
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+      R.o[mt][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y.v, w[hb][mt].w, R.o[mt][nt], 0, 0, 0);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  return true;
 }
 
 template <int D, int MT, bool PAD, bool SHARED>
@@ -925,26 +987,30 @@ __global__ void __launch_bounds__(kThreads, 2) attend_tile_kernel(AttendArgs a, 
       if (t + 1 < t1) ok = fetch_tile<D, PAD>(buf[(t + 1 - t0) & 1], src, window, t + 1 - t0, (it.seg.t0 + t + 1) * kKeyTile);
       return here;
     };
-    // tiles that every row sees
-    while (t < t1 && ok == 15u && (it.seg.t0 + t + 1) * kKeyTile <= all_see) {
-      next();
-      tile_step<D, MT, PAD, false>(rows, buf[(t - t0) & 1], (it.seg.t0 + t) * kKeyTile, 15u, (int)least, (int)most, a.d, scale);
-      ++t;
-      window.move(src, t - t0);
-    }
-    // the last ones, and all from a page number out of range on
-    const int from = (it.seg.t0 + t) * kKeyTile;
+    bool fetched = false;                                  // tile t has been waited for
+    uint32_t here = 0;
+    const int from = (it.seg.t0 + t0) * kKeyTile;
     while (t < t1) {
-      const uint32_t here = next();
+      if (!fetched) here = next();
       const int key0 = (it.seg.t0 + t) * kKeyTile;
       bad = bad || here != 15u;
       if (key0 < (int)most)
         tile_step<D, MT, PAD, true>(rows, buf[(t - t0) & 1], key0, here, (int)least, (int)most, a.d, scale);
+      fetched = false;
       ++t;
       window.move(src, t - t0);
+      // tiles that every row sees, as long as no reference has to move.  (Wavefronts may leave at different tiles: next() has the barriers,
+      // one a tile.)
+      while (t < t1 && ok == 15u && (it.seg.t0 + t + 1) * kKeyTile <= all_see) {
+        here = next();
+        fetched = !tile_step<D, MT, PAD, false>(rows, buf[(t - t0) & 1], (it.seg.t0 + t) * kKeyTile, 15u, (int)least, (int)most, a.d, scale);
+        if (fetched) break;
+        ++t;
+        window.move(src, t - t0);
+      }
     }
     if (__any(rows.odd != 0))
-      rows.template add_odd<PAD>(src, from, B::KEYS, min((it.seg.t0 + t1) * kKeyTile, (int)most), (int)most);
+      rows.template add_odd<true>(src, from, B::KEYS, min((it.seg.t0 + t1) * kKeyTile, (int)most), (int)most);
   }
   if (bad && lane == 0) atomicOr(a.map.fault, kFaultPaged);
 #pragma unroll
@@ -953,14 +1019,10 @@ __global__ void __launch_bounds__(kThreads, 2) attend_tile_kernel(AttendArgs a, 
     const float z = sum_over_g(rows.z[mt]);
     if (r >= it.seg.rows) continue;
 #pragma unroll
-    for (int hf = 0; hf < B::HN; ++hf)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        float v[B::CW];
-#pragma unroll
-        for (int e = 0; e < B::CW; ++e) v[e] = rows.o[mt][hf * B::CW + e][i];
-        write_row<__bf16, B::CW>(a, it, pt, D, r, 16 * B::CW * hf + B::CW * (4 * g + i), v, rows.m[mt], z);
-      }
+    for (int nt = 0; nt < B::NT; ++nt) {
+      const float v[4] = {rows.o[mt][nt][0], rows.o[mt][nt][1], rows.o[mt][nt][2], rows.o[mt][nt][3]};
+      write_row<__bf16, 4>(a, it, pt, D, r, 16 * nt + 4 * g, v, rows.m[mt], z);
+    }
   }
 }
 
