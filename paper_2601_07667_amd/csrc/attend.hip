@@ -57,6 +57,18 @@ __device__ __forceinline__ float sum_over_g(float x) {
   return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
+// sequence_of by a whole wavefront: a load for up to 64 sequences, two for up to 4096, where a binary search waits for one after another.
+__device__ __forceinline__ int sequence_by_wave(const int32_t* cu, int n, int j) {
+  const int lane = threadIdx.x & 63, step = (n + 63) / 64;
+  int first = 0;
+  if (step > 1) {
+    const int i = lane * step;
+    first = step * max(0, (int)__popcll(__ballot(i < n && cu[min(i, n - 1)] <= j)) - 1);
+  }
+  const int i = first + lane;
+  return min(n - 1, first + max(0, (int)__popcll(__ballot(i < n && lane < step + (step == 1 ? 63 : 0) && cu[min(i, n - 1)] <= j)) - 1));
+}
+
 // ------------------------------------------------------------------------------------------------------------------
 // The cut, found by every wavefront for itself.
 
@@ -113,6 +125,13 @@ __device__ __forceinline__ Segment segment_of(const AttendArgs& a, int i, bool* 
   return s;
 }
 
+struct Partials {
+  float* o;                // [cap][D]
+  float2* mz;              // [cap]
+  int4* plan;              // of the segments
+  int32_t* group;          // [n_seqs] own segments: the sequence's group or -1
+};
+
 struct Item {
   Segment seg;
   int tile, h, split, splits;
@@ -125,7 +144,7 @@ __device__ __forceinline__ int4 plan_entry(const Segment& s, int splits, bool pa
 }
 
 template <bool SHARED>
-__device__ __forceinline__ bool find_item(const AttendArgs& a, const AttendCut& cut, int item, int4* plan, Item* out) {
+__device__ __forceinline__ bool find_item(const AttendArgs& a, const AttendCut& cut, int item, const Partials& pt, Item* out) {
   const int lane = threadIdx.x & 63;
   const int n = SHARED ? a.n_groups : a.n_seqs, per = (n + 63) / 64;
   const bool writes = blockIdx.x == 0 && threadIdx.x < 64;
@@ -166,7 +185,8 @@ __device__ __forceinline__ bool find_item(const AttendArgs& a, const AttendCut& 
       if (per > 1) own = segment_of<SHARED>(a, i, &bad);
       const int k = splits_of(own.span, per_item);
       const bool partial = is_partial(own, k);
-      plan[i] = plan_entry(own, k, partial && own.rows > 0, at);
+      pt.plan[i] = plan_entry(own, k, partial && own.rows > 0, at);
+      if (!SHARED && a.n_groups > 0) pt.group[i] = group_of(a, i);
       if (partial) at += (uint32_t)own.rows * (uint32_t)a.Hk * (uint32_t)k;
     }
   }
@@ -590,11 +610,6 @@ struct Rows {
 
 // ------------------------------------------------------------------------------------------------------------------
 
-struct Partials {
-  float* o;                // [cap][D]
-  float2* mz;              // [cap]
-  int4* plan;              // of the segments
-};
 
 // Writes row r of an item: to out and lse if its results are whole, else to its slot.  v: CNT elements from e0 on.
 template <typename T, int CNT>
@@ -628,7 +643,7 @@ attend_split_kernel(AttendArgs a, AttendCut cut, Partials pt) {
   __shared__ __attribute__((aligned(16))) float so[kWaves][16][LD];
   __shared__ float sm[kWaves][16], sz[kWaves][16];
   Item it;
-  if (!find_item<SHARED>(a, cut, (int)blockIdx.x, pt.plan, &it)) return;
+  if (!find_item<SHARED>(a, cut, (int)blockIdx.x, pt, &it)) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r16 = lane & 15, g = lane >> 4;
   Rows<T, D, MT> rows;
   rows.clear();
@@ -928,7 +943,7 @@ __global__ void __launch_bounds__(kThreads, 2) attend_tile_kernel(AttendArgs a, 
   __shared__ TileBuffer<D> buf[2];
   __shared__ int lims[2][kWaves];
   Item it;
-  if (!find_item<SHARED>(a, cut, (int)blockIdx.x, pt.plan, &it)) return;
+  if (!find_item<SHARED>(a, cut, (int)blockIdx.x, pt, &it)) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r16 = lane & 15, g = lane >> 4;
   const int row0 = it.tile * cut.rows + wave * 16 * MT;
   Rows<__bf16, D, MT> rows;
@@ -1027,94 +1042,104 @@ __global__ void __launch_bounds__(kThreads, 2) attend_tile_kernel(AttendArgs a, 
 }
 
 // ------------------------------------------------------------------------------------------------------------------
-// Joins the pieces of rows that were cut: NW wavefronts a row, each lane four elements of every so many-th piece.
+// Joins the pieces of rows that were cut: NW wavefronts a row, each 4 D bytes' lanes of them every so many-th piece, four at a time,
+// with a running maximum of their references; then lanes and wavefronts are joined.  One pass: what it costs is the latency of the
+// loads that depend on each other (the sequence, its plan, the pieces).
 template <typename T, int D, int NW>
-__global__ void __launch_bounds__(kThreads) attend_join_kernel(AttendArgs a, Partials own, Partials shared) {
-  constexpr int LPP = D / 4;                               // lanes of a piece
-  constexpr int PPW = 64 / LPP;                            // pieces a wavefront takes at once
-  constexpr int RPB = kWaves / NW;
-  __shared__ __attribute__((aligned(16))) float so[kWaves][PPW][D];
-  __shared__ float sz[kWaves];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+__global__ void __launch_bounds__(NW > kWaves ? NW * 64 : kThreads) attend_join_kernel(AttendArgs a, Partials own, Partials shared) {
+  constexpr int LPP = D / 4;                               // lanes of a piece, four elements each
+  constexpr int PPW = 64 / LPP;                            // pieces that a wavefront takes at once
+  constexpr int WAVES = NW > kWaves ? NW : kWaves;
+  constexpr int RPB = WAVES / NW;
+  __shared__ __attribute__((aligned(16))) float so[WAVES][D];
+  __shared__ float sm[WAVES], sz[WAVES];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t row = (int64_t)blockIdx.x * RPB + wave / NW;
-  const bool live = row < (int64_t)a.total_q * a.Hq;
-  const int tok = live ? (int)(row / a.Hq) : 0, hq = (int)(row - (int64_t)tok * a.Hq), h = hq / a.G;
-  int n[2] = {0, 0};                                       // pieces of the sequence's own keys, of the shared ones
-  int64_t at[2] = {0, 0};
-  int rows[2] = {0, 0};
-  if (live) {
-    const int b = sequence_of(a.cu_q, a.n_seqs, tok);
-    const int4 p = own.plan[b];
-    const int r = (tok - p.x) * a.G + hq - h * a.G;
-    if (p.z > 0 && tok >= p.x && r < p.y) {
-      n[0] = p.z;
-      rows[0] = p.y;
-      at[0] = (int64_t)(uint32_t)p.w + (int64_t)h * p.z * p.y + r;
-      if (a.n_groups > 0) {
-        const int g = group_of(a, b);
-        if (g >= 0) {
-          const int4 s = shared.plan[g];
-          const int rs = (tok - s.x) * a.G + hq - h * a.G;
-          if (s.z > 0 && tok >= s.x && rs < s.y) {
-            n[1] = s.z;
-            rows[1] = s.y;
-            at[1] = (int64_t)(uint32_t)s.w + (int64_t)h * s.z * s.y + rs;
-          }
-        }
-      }
+  if (row >= (int64_t)a.total_q * a.Hq) return;            // all of a workgroup, or it has a row for each wavefront and no barrier
+  const int tok = (int)(row / a.Hq), hq = (int)(row - (int64_t)tok * a.Hq), h = hq / a.G;
+  const int b = sequence_by_wave(a.cu_q, a.n_seqs, tok);
+  const int4 p = own.plan[b];
+  const int g = a.n_groups > 0 ? own.group[b] : -1;
+  const int r = (tok - p.x) * a.G + hq - h * a.G;
+  if (p.z <= 0 || tok < p.x || r >= p.y) return;           // written whole
+  int n1 = 0;
+  int64_t at1 = 0;
+  int rows1 = 0;
+  if (g >= 0) {
+    const int4 q = shared.plan[g];
+    const int rs = (tok - q.x) * a.G + hq - h * a.G;
+    if (q.z > 0 && tok >= q.x && rs < q.y) {
+      n1 = q.z;
+      rows1 = q.y;
+      at1 = (int64_t)(uint32_t)q.w + (int64_t)h * q.z * q.y + rs;
     }
   }
-  const int total = n[0] + n[1];
-  if (NW == 1 && total == 0) return;                       // written whole (with more wavefronts a row: all of a workgroup's alike)
-  if (NW > 1 && total == 0) return;
-  auto piece = [&](int i, const Partials** from) -> int64_t {
-    const int k = i < n[0] ? 0 : 1;
-    *from = k == 0 ? &own : &shared;
-    return at[k] + (int64_t)(i - (k == 0 ? 0 : n[0])) * rows[k];
-  };
-  float m = -INFINITY, z = 0.f;
-  for (int i = lane; i < total; i += 64) {
-    const Partials* f;
-    const int64_t s = piece(i, &f);
-    m = fmaxf(m, f->mz[s].x);
-  }
-  for (int x = 32; x > 0; x >>= 1) m = fmaxf(m, __shfl_xor(m, x));
-  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  const int n0 = p.z, total = n0 + n1;
+  const int64_t at0 = (int64_t)(uint32_t)p.w + (int64_t)h * p.z * p.y + r;
   const int sub = lane / LPP, e = (lane % LPP) * 4;
-#pragma unroll 4
-  for (int i = (wave % NW) * PPW + sub; i < total; i += NW * PPW) {
-    const Partials* f;
-    const int64_t s = piece(i, &f);
-    const float2 mz = f->mz[s];
-    const float by = m == -INFINITY ? 1.f : exp2_fast(mz.x - m);
-    acc += *(const f32x4*)(f->o + s * D + e) * by;
-    z += mz.y * by;
-  }
-  if (LPP == 64) {
-    // one piece at a time: every lane has the same sum
-  } else if (LPP == 32) {
-    z += __shfl_xor(z, 32);
-  } else {
-    z += __shfl_xor(z, 16);
-    z += __shfl_xor(z, 32);
-  }
-  *(f32x4*)&so[wave][sub][e] = acc;
-  if (lane == 0) sz[wave] = z;
-  if (NW > 1) __syncthreads(); else __builtin_amdgcn_wave_barrier();
-  if (wave % NW != 0) return;
-  z = 0.f;
-  acc = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, z = 0.f;
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  for (int i0 = (wave % NW) * PPW + sub; i0 < total; i0 += 4 * NW * PPW) {
+    float2 mz[4];
+    f32x4 o[4];
 #pragma unroll
-  for (int w = 0; w < NW; ++w) {
-    z += sz[wave + w];
-    if (lane < LPP)
+    for (int u = 0; u < 4; ++u) {
+      const int i = min(i0 + u * NW * PPW, total - 1);     // past the end: the last one again, not counted
+      const Partials& f = i < n0 ? own : shared;
+      const int64_t s = i < n0 ? at0 + (int64_t)i * p.y : at1 + (int64_t)(i - n0) * rows1;
+      mz[u] = f.mz[s];
+      o[u] = *(const f32x4*)(f.o + s * D + e);
+    }
+    float top = m;
 #pragma unroll
-      for (int s = 0; s < PPW; ++s) acc += *(const f32x4*)&so[wave + w][s][lane * 4];
+    for (int u = 0; u < 4; ++u)
+      if (i0 + u * NW * PPW < total) top = fmaxf(top, mz[u].x);
+    const float by = top == -INFINITY ? 1.f : exp2_fast(m - top);
+    m = top;
+    z *= by;
+    acc *= by;
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (i0 + u * NW * PPW < total) {
+        const float w = m == -INFINITY ? 1.f : exp2_fast(mz[u].x - m);
+        z += mz[u].y * w;
+        acc += o[u] * w;
+      }
   }
-  if (lane * 4 < a.d) {
+#pragma unroll
+  for (int x = LPP; x < 64; x *= 2) {                      // the wavefront's lanes that have the same elements
+    const float m2 = __shfl_xor(m, x), z2 = __shfl_xor(z, x);
+    const float top = fmaxf(m, m2), by = top == -INFINITY ? 1.f : exp2_fast(m - top), by2 = top == -INFINITY ? 1.f : exp2_fast(m2 - top);
+    m = top;
+    z = z * by + z2 * by2;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) acc[c] = acc[c] * by + __shfl_xor(acc[c], x) * by2;
+  }
+  if (NW > 1) {
+    if (lane < LPP) *(f32x4*)&so[wave][e] = acc;
+    if (lane == 0) {
+      sm[wave] = m;
+      sz[wave] = z;
+    }
+    __syncthreads();
+    if (wave % NW != 0) return;
+    float top = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) top = fmaxf(top, sm[wave + w]);
+    m = top;
+    z = 0.f;
+    acc = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      const float by = m == -INFINITY ? 1.f : exp2_fast(sm[wave + w] - m);
+      z += sz[wave + w] * by;
+      acc += *(const f32x4*)&so[wave + w][e] * by;
+    }
+  }
+  if (lane < LPP && e < a.d) {
     const float by = z == 0.f ? 0.f : 1.f / z;
     typedef T Out __attribute__((ext_vector_type(4)));
-    *(Out*)((T*)a.out + (int64_t)tok * a.ot + (int64_t)hq * a.oh + lane * 4) =
+    *(Out*)((T*)a.out + (int64_t)tok * a.ot + (int64_t)hq * a.oh + e) =
         Out{(T)(acc[0] * by), (T)(acc[1] * by), (T)(acc[2] * by), (T)(acc[3] * by)};
   }
   if (lane == 0 && a.lse != nullptr) a.lse[(int64_t)hq * a.total_q + tok] = z == 0.f ? -INFINITY : (m + __log2f(z)) * kLn2;
@@ -1170,12 +1195,17 @@ hipError_t launch_d(const PagedWorkspace& ws, const AttendArgs& args, hipStream_
   po.o = ws.part + shared.cap * D;
   po.mz = ws.part_mz + shared.cap;
   po.plan = ws.plan;
+  po.group = ws.group;
+  ps.group = nullptr;
   hipError_t e = hipSuccess;
   if (a.n_groups > 0) e = a.d == D ? launch_cut<T, D, true, false>(a, shared, ps, st) : launch_cut<T, D, true, true>(a, shared, ps, st);
   if (e == hipSuccess) e = a.d == D ? launch_cut<T, D, false, false>(a, own, po, st) : launch_cut<T, D, false, true>(a, own, po, st);
   if (e != hipSuccess) return e;
   const int64_t out_rows = (int64_t)a.total_q * a.Hq;
-  if (out_rows <= 2048)
+  // few rows are cut into many pieces each
+  if (out_rows <= 256)
+    hipLaunchKernelGGL((attend_join_kernel<T, D, 16>), dim3((unsigned)out_rows), dim3(1024), 0, st, a, po, ps);
+  else if (out_rows <= 2048)
     hipLaunchKernelGGL((attend_join_kernel<T, D, kWaves>), dim3((unsigned)out_rows), dim3(kThreads), 0, st, a, po, ps);
   else
     hipLaunchKernelGGL((attend_join_kernel<T, D, 1>), dim3((unsigned)((out_rows + kWaves - 1) / kWaves)), dim3(kThreads), 0, st,

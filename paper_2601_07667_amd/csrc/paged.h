@@ -16,6 +16,7 @@ struct PagedWorkspace {
   float2* part_mz;         // [part_rows] ... with their reference and sum
   int64_t part_rows;
   int4* plan;              // [2][kPagedMaxSeqs] how sequences and groups were cut
+  int32_t* group;          // [kPagedMaxSeqs] the sequences' groups
   int4* forks;             // [max_seqs] what the bookkeeping launch of a fork leaves for the copying one
   int32_t* fresh;          // [kMaxFresh] the free pages that a call takes, in order
   uint32_t* fault;         // [1]
@@ -34,6 +35,7 @@ struct PagesWriteArgs {
   int64_t ksh, kst, vsh, vst;  // strides of a dense source in bytes
   int32_t n, total, n_src, idx_rows;
   int32_t cpr, cpr_shift;  // 16-byte pieces of a row; the shift is -1 where that is no power of two
+  int32_t tokens;          // of a workgroup (set by launch_pages_write)
 };
 hipError_t launch_pages_write(const PagesWriteArgs& a, int Hk, hipStream_t st);
 

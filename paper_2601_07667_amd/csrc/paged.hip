@@ -16,57 +16,97 @@ constexpr int kBookThreads = 1024;
 
 __device__ __forceinline__ void paged_fault(const PageMap& m) { atomicOr(m.fault, kFaultPaged); }
 
+typedef uint32_t Piece __attribute__((ext_vector_type(4)));              // 16 bytes
+typedef const Piece __attribute__((address_space(1))) * PieceSrc;
+typedef Piece __attribute__((address_space(1))) * PieceDst;
+
+// STREAM: past the caches (transfers that do not fit them anyway).
+template <bool STREAM>
+__device__ __forceinline__ Piece load_piece(const char* p) {
+  return STREAM ? __builtin_nontemporal_load((PieceSrc)p) : *(PieceSrc)p;
+}
+template <bool STREAM>
+__device__ __forceinline__ void store_piece(char* p, Piece x) {
+  if (STREAM) __builtin_nontemporal_store(x, (PieceDst)p); else *(PieceDst)p = x;
+}
+
+constexpr int kWriteUnroll = 4;            // pieces of K, and as many of V, that a thread has on their way
+constexpr int kWriteTokens = kWriteThreads;   // most tokens of a workgroup
+
 // Rows of head_dim elements into the last cu[i + 1] - cu[i] positions of table row rows[i], for every i: a copy, bound by memory.
-// Each thread moves U pieces of 16 bytes; the pieces of a (head, tensor) are numbered token * cpr + c, so a wavefront reads and
-// writes whole rows.  PAGED: the source is a row's pages too.  grid: x = blocks of pieces, y = KV head, z = K or V.
-template <bool PAGED, int U>
+// A workgroup has some neighbouring tokens of a KV head: first a thread for each finds where it stands and where it goes (sequence,
+// row, length, page: loads that depend on each other), then all move the tokens' pieces of 16 bytes, K and V, numbered
+// token * cpr + c, so that a wavefront reads and writes whole rows.  PAGED: the source is a row's pages too.
+// grid: x = blocks of a.tokens tokens, y = KV head.
+template <bool PAGED, bool STREAM>
 __global__ void __launch_bounds__(kWriteThreads) pages_write_kernel(PagesWriteArgs a) {
-  typedef uint32_t Piece __attribute__((ext_vector_type(4)));
-  extern __shared__ int32_t cu[];
-  for (int i = threadIdx.x; i <= a.n; i += kWriteThreads) cu[i] = a.cu[i];
-  __syncthreads();
-  const int h = blockIdx.y, which = blockIdx.z;
-  const char* src = which == 0 ? a.k : a.v;
-  char* dst = (which == 0 ? a.k_pages : a.v_pages) + (int64_t)h * a.map.head;
-  const int64_t sh = which == 0 ? a.ksh : a.vsh, stt = which == 0 ? a.kst : a.vst;
-  src += PAGED ? (int64_t)h * a.map.head : (int64_t)h * sh;
+  extern __shared__ int32_t lds[];         // cu [n + 1]; rows [n], lengths [n]: of the rows written to, then of those read
+  __shared__ int64_t from[kWriteTokens], to[kWriteTokens];               // byte offsets within the head's source and pages; to -1: none
+  int32_t* cu = lds;
+  int32_t* row = lds + a.n + 1;
+  int32_t* len = row + a.n;
+  int32_t* src_row = len + a.n;
+  int32_t* src_len = src_row + a.n;
+  const int h = blockIdx.y, tid = threadIdx.x;
+  const int j0 = (int)blockIdx.x * a.tokens, n_tok = min(a.tokens, a.total - j0);
   const int32_t* idx = a.idx != nullptr ? a.idx + (a.idx_rows == 1 ? 0 : (int64_t)h * a.total) : nullptr;
-  const int64_t total = (int64_t)a.total * a.cpr;
-  const int64_t q0 = (int64_t)blockIdx.x * (kWriteThreads * U) + threadIdx.x;
-  Piece val[U];
-  int64_t to[U];
+  const int t = tid < n_tok ? (idx != nullptr ? idx[j0 + tid] : j0 + tid) : 0;
   bool bad = false;
-#pragma unroll
-  for (int u = 0; u < U; ++u) {
-    to[u] = -1;
-    const int64_t q = q0 + u * kWriteThreads;
-    if (q >= total) continue;
-    const int j = a.cpr_shift >= 0 ? (int)(q >> a.cpr_shift) : (int)(q / a.cpr);
-    const int c = (int)(q - (int64_t)j * a.cpr);
-    const int i = sequence_of(cu, a.n, j);
-    const int t = idx != nullptr ? idx[j] : j;
-    const int r = a.rows[i];
-    int64_t from = -1;
-    if (PAGED) {
-      const int rs = a.src_rows[i];
-      int len;
-      if (row_length(a.map, rs, &len) && t < len) from = token_offset(a.map, rs, t);
-    } else if ((uint32_t)t < (uint32_t)a.n_src) {
-      from = (int64_t)t * stt;
+  for (int i = tid; i <= a.n; i += kWriteThreads) {
+    cu[i] = a.cu[i];
+    if (i < a.n) {
+      const int r = a.rows[i];
+      int L;
+      row[i] = row_length(a.map, r, &L) ? r : -1;
+      len[i] = L;
+      if (PAGED) {
+        const int rs = a.src_rows[i];
+        src_row[i] = row_length(a.map, rs, &L) ? rs : -1;
+        src_len[i] = L;
+      }
     }
-    int64_t at = -1;
-    int len;
-    if (cu[i] <= j && j < cu[i + 1] && row_length(a.map, r, &len)) at = token_offset(a.map, r, len - (cu[i + 1] - j));
-    if (from < 0 || at < 0) {
-      bad = true;
-      continue;
-    }
-    to[u] = at + c * 16;
-    val[u] = *(const Piece*)(src + from + c * 16);
   }
+  __syncthreads();
+  if (tid < n_tok) {
+    const int j = j0 + tid, i = sequence_of(cu, a.n, j);
+    int64_t f = -1, w = -1;
+    if (PAGED) {
+      if (t < src_len[i]) f = token_offset(a.map, src_row[i], t);        // t < 0: -1 as well
+    } else if ((uint32_t)t < (uint32_t)a.n_src) {
+      f = t;
+    }
+    if (cu[i] <= j && j < cu[i + 1]) w = token_offset(a.map, row[i], len[i] - (cu[i + 1] - j));
+    bad = f < 0 || w < 0;
+    from[tid] = f;
+    to[tid] = bad ? -1 : w;
+  }
+  __syncthreads();
+  const int64_t head = (int64_t)h * a.map.head;
+  const char* ks = a.k + (PAGED ? head : (int64_t)h * a.ksh);
+  const char* vs = a.v + (PAGED ? head : (int64_t)h * a.vsh);
+  const int pieces = n_tok * a.cpr;
+  for (int q0 = tid; q0 < pieces; q0 += kWriteThreads * kWriteUnroll) {
+    Piece k[kWriteUnroll], v[kWriteUnroll];
+    int64_t at[kWriteUnroll];
 #pragma unroll
-  for (int u = 0; u < U; ++u)
-    if (to[u] >= 0) *(Piece*)(dst + to[u]) = val[u];
+    for (int u = 0; u < kWriteUnroll; ++u) {
+      const int q = q0 + u * kWriteThreads;
+      at[u] = -1;
+      if (q >= pieces) continue;
+      const int j = a.cpr_shift >= 0 ? q >> a.cpr_shift : (int)((uint32_t)q / (uint32_t)a.cpr);
+      const int c = (q - j * a.cpr) * 16;
+      if (to[j] < 0) continue;
+      at[u] = head + to[j] + c;
+      k[u] = load_piece<STREAM>(ks + (PAGED ? from[j] : from[j] * a.kst) + c);
+      v[u] = load_piece<STREAM>(vs + (PAGED ? from[j] : from[j] * a.vst) + c);
+    }
+#pragma unroll
+    for (int u = 0; u < kWriteUnroll; ++u)
+      if (at[u] >= 0) {
+        store_piece<STREAM>(a.k_pages + at[u], k[u]);
+        store_piece<STREAM>(a.v_pages + at[u], v[u]);
+      }
+  }
   if (bad) paged_fault(a.map);
 }
 
@@ -236,7 +276,6 @@ __global__ void __launch_bounds__(kBookThreads) pages_fork_kernel(PagesForkArgs 
 
 // The continuations' rows and counts (slice 0), and the filled tokens of their last pages (slices from 1: layer, K or V).
 __global__ void __launch_bounds__(kWriteThreads) pages_fork_copy_kernel(PagesForkArgs a) {
-  typedef uint32_t Piece __attribute__((ext_vector_type(4)));
   const PageMap& m = a.map;
   const int4 f = a.forks[blockIdx.x];
   if (f.z <= 0) return;
@@ -262,12 +301,23 @@ __global__ void __launch_bounds__(kWriteThreads) pages_fork_copy_kernel(PagesFor
     if (threadIdx.x == 0) paged_fault(m);
     return;
   }
-  const int per_head = part * a.cpr, total = per_head * a.Hk;
-  for (int q = threadIdx.x; q < total; q += kWriteThreads) {
-    const int h = q / per_head, e = q - h * per_head;
-    const int t = a.cpr_shift >= 0 ? e >> a.cpr_shift : e / a.cpr;
-    const int64_t off = (int64_t)h * m.head + (int64_t)t * m.tok + (int64_t)(e - t * a.cpr) * 16;
-    *(Piece*)(base + (int64_t)f.w * m.page + off) = *(const Piece*)(base + (int64_t)page * m.page + off);
+  const uint32_t per_head = (uint32_t)(part * a.cpr), total = per_head * (uint32_t)a.Hk;
+  const char* src = base + (int64_t)page * m.page;
+  char* dst = base + (int64_t)f.w * m.page;
+  constexpr int U = 8;                     // pieces that a thread has on their way
+  for (uint32_t q0 = threadIdx.x; q0 < total; q0 += kWriteThreads * U) {
+    Piece x[U];
+    int64_t off[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const uint32_t q = min(q0 + u * kWriteThreads, total - 1u), h = q / per_head, e = q - h * per_head;
+      const uint32_t t = a.cpr_shift >= 0 ? e >> a.cpr_shift : e / (uint32_t)a.cpr;
+      off[u] = (int64_t)h * m.head + (int64_t)t * m.tok + (int64_t)(e - t * (uint32_t)a.cpr) * 16;
+      x[u] = load_piece<false>(src + off[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (q0 + u * kWriteThreads < total) store_piece<false>(dst + off[u], x[u]);
   }
 }
 
@@ -302,17 +352,28 @@ pages_free_kernel(PageMap m, int32_t* kv_len, int32_t* refs, const int32_t* rows
 
 }  // namespace
 
-hipError_t launch_pages_write(const PagesWriteArgs& a, int Hk, hipStream_t st) {
+// Bytes read and written from which pages are written past the caches (gather.hip has the measurement of the same copy).
+constexpr int64_t kWriteStreamBytes = int64_t(100) << 20;
+
+hipError_t launch_pages_write(const PagesWriteArgs& args, int Hk, hipStream_t st) {
+  PagesWriteArgs a = args;
   if (a.n == 0 || a.total == 0) return hipSuccess;
-  const size_t lds = (size_t)(a.n + 1) * sizeof(int32_t);
-  const int64_t pieces = (int64_t)a.total * a.cpr;
-  const int64_t blocks = (pieces + kWriteThreads * 4 - 1) / (kWriteThreads * 4);
-  if (blocks >= (int64_t(1) << 31)) return hipErrorInvalidValue;
-  const dim3 grid((unsigned)blocks, (unsigned)Hk, 2);
-  if (a.src_rows != nullptr)
-    hipLaunchKernelGGL((pages_write_kernel<true, 4>), grid, dim3(kWriteThreads), lds, st, a);
+  // a workgroup has pieces for one round of its threads; fewer tokens where the call does not fill the card
+  const int round = kWriteThreads * kWriteUnroll / a.cpr;
+  a.tokens = round < 1 ? 1 : round > kWriteTokens ? kWriteTokens : round;
+  while (a.tokens > 8 && (int64_t)(a.total / a.tokens + 1) * Hk < 256) a.tokens /= 2;
+  const int64_t blocks = ((int64_t)a.total + a.tokens - 1) / a.tokens;
+  const size_t lds = (size_t)((a.src_rows != nullptr ? 5 : 3) * a.n + 1) * sizeof(int32_t);
+  const bool stream = 4 * (int64_t)a.total * a.cpr * 16 * Hk >= kWriteStreamBytes;
+  const dim3 grid((unsigned)blocks, (unsigned)Hk), block(kWriteThreads);
+  if (a.src_rows != nullptr && stream)
+    hipLaunchKernelGGL((pages_write_kernel<true, true>), grid, block, lds, st, a);
+  else if (a.src_rows != nullptr)
+    hipLaunchKernelGGL((pages_write_kernel<true, false>), grid, block, lds, st, a);
+  else if (stream)
+    hipLaunchKernelGGL((pages_write_kernel<false, true>), grid, block, lds, st, a);
   else
-    hipLaunchKernelGGL((pages_write_kernel<false, 4>), grid, dim3(kWriteThreads), lds, st, a);
+    hipLaunchKernelGGL((pages_write_kernel<false, false>), grid, block, lds, st, a);
   return hipGetLastError();
 }
 
