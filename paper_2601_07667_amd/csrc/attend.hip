@@ -4,7 +4,7 @@
 // Keys are taken once, in pieces: a piece's (m, z, unnormalised out) are joined by m = max m_p, z = sum z_p 2^(m_p - m) and the
 // same for out (attend_plan.h: how the work is cut).  Logits are kept in units of log 2.
 //
-// attend_split_kernel, for few rows: bound by reading K and V.  Each wavefront takes every fourth block of 32 keys (16 in fp32) of
+// Split items, for few rows: bound by reading K and V.  Each wavefront of the workgroup takes every fourth block of 32 keys (16 in fp32) of
 // the item, for all rows of its tile, straight from memory into registers in the layout of the matrix instruction's operand:
 //   x^T = K Q^T  (v_mfma_f32_16x16x32_bf16; lane (r = lane % 16, g = lane / 16) holds K[r][8 g ..]),
 //   out^T += V^T P^T.
@@ -13,7 +13,7 @@
 // slot (g, j) = key 16 (j / 4) + 4 g + j % 4.  V rows are loaded in that order, 16 bytes of a row a lane, and turned with byte
 // permutes in registers: no LDS and no barrier until the four wavefronts join their results.
 //
-// attend_tile_kernel, for many rows (bf16): bound by the products.  Each wavefront has 16 MT rows of its own, and all four take the
+// Tile items, for many rows (bf16, d <= 128): bound by the products.  Each wavefront has 16 MT rows of its own, and all four take the
 // same tiles of 64 keys from LDS, which are loaded there directly, into one of two buffers while the other is worked on: K as it
 // stands as an operand (lane by lane), V by rows with their 16-byte pieces exchanged, so that the transposing reads that
 // make operands of it (ds_read_b64_tr_b16) have no bank conflicts either.
@@ -147,7 +147,7 @@ template <bool SHARED>
 __device__ __forceinline__ bool find_item(const AttendArgs& a, const AttendCut& cut, int item, const Partials& pt, Item* out) {
   const int lane = threadIdx.x & 63;
   const int n = SHARED ? a.n_groups : a.n_seqs, per = (n + 63) / 64;
-  const bool writes = blockIdx.x == 0 && threadIdx.x < 64;
+  const bool writes = item == 0 && threadIdx.x < 64;
   bool bad = false;
   auto row_tiles = [&](const Segment& s) { return (uint32_t)((s.rows + cut.rows - 1) / cut.rows) * (uint32_t)a.Hk; };
   auto is_partial = [&](const Segment& s, int splits) { return SHARED || splits > 1 || s.shared > 0; };
@@ -290,11 +290,12 @@ __device__ __forceinline__ uint32_t offset(uint32_t x) {
 }
 
 // Elements e0 .. e0 + CW - 1 of the row at base + row, zeros beyond d.
-template <typename T, int D, bool PAD>
+template <typename T, int D, bool PAD, bool STREAM>
 __device__ __forceinline__ void load_value(uint32_t* to, const char* base, uint32_t row, int e0, int d) {
   typedef uint32_t Words __attribute__((ext_vector_type(Block<T, D>::VW)));
   const bool in = !PAD || e0 < d;
-  const Words w = *(const Words*)(base + (row + (uint32_t)(in ? e0 : 0) * (uint32_t)sizeof(T)));
+  const Words* from = (const Words*)(base + (row + (uint32_t)(in ? e0 : 0) * (uint32_t)sizeof(T)));
+  const Words w = STREAM ? __builtin_nontemporal_load(from) : *from;
 #pragma unroll
   for (int x = 0; x < Block<T, D>::VW; ++x) to[x] = in ? w[x] : 0u;
 }
@@ -331,7 +332,8 @@ struct PageWindow {
   }
 };
 
-template <typename T, int D, bool PAD, typename W>
+// STREAM: past the caches, for keys that one tile of rows takes (decode of 128K keys 58.7 us, so 53.2; a pruned batch 95.9, 87.8).
+template <typename T, int D, bool PAD, bool STREAM, typename W>
 __device__ __forceinline__ void load_block(Block<T, D>& b, const Source& s, const W& window, int block, int key0) {
   typedef Block<T, D> B;
   const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
@@ -348,7 +350,8 @@ __device__ __forceinline__ void load_block(Block<T, D>& b, const Source& s, cons
 #pragma unroll
     for (int p = 0; p < B::KP; ++p) {
       const bool in = !PAD || p * 64 + g * 16 < s.d * (int)sizeof(T);    // beyond d: the row's first piece, then zeros
-      const Piece x = *(const Piece*)(kb + (in ? ko + p * 64u : (uint32_t)r * (uint32_t)s.tok));
+      const Piece* from = (const Piece*)(kb + (in ? ko + p * 64u : (uint32_t)r * (uint32_t)s.tok));
+      const Piece x = STREAM ? __builtin_nontemporal_load(from) : *from;
       b.k[t][p] = in ? x : Piece{0, 0, 0, 0};
     }
   }
@@ -356,7 +359,7 @@ __device__ __forceinline__ void load_block(Block<T, D>& b, const Source& s, cons
   for (int j = 0; j < B::VR; ++j) {
 #pragma unroll
     for (int hf = 0; hf < B::HN; ++hf)
-      load_value<T, D, PAD>(b.v[j][hf], base[j >> 2], (uint32_t)(4 * g + (j & 3)) * (uint32_t)s.tok, 16 * B::CW * hf + B::CW * r, s.d);
+      load_value<T, D, PAD, STREAM>(b.v[j][hf], base[j >> 2], (uint32_t)(4 * g + (j & 3)) * (uint32_t)s.tok, 16 * B::CW * hf + B::CW * r, s.d);
   }
 }
 
@@ -635,15 +638,19 @@ __device__ __forceinline__ void write_row(const AttendArgs& a, const Item& it, c
   if (e0 == 0 && a.lse != nullptr) a.lse[(int64_t)hq * a.total_q + tok] = z == 0.f ? -INFINITY : (m + __log2f(z)) * kLn2;
 }
 
-template <typename T, int D, int MT, bool PAD, bool SHARED>
-__global__ void __launch_bounds__(kThreads, D * MT > 128 ? 1 : 2)
-attend_split_kernel(AttendArgs a, AttendCut cut, Partials pt) {
+// What the wavefronts of a split item leave for each other.
+template <int D>
+struct SplitLds {
+  float o[kWaves][16][D + 4];              // padded rows
+  float m[kWaves][16], z[kWaves][16];
+};
+
+template <typename T, int D, int MT, bool PAD, bool SHARED, bool STREAM>
+__device__ __forceinline__ void split_item(const AttendArgs& a, const AttendCut& cut, const Partials& pt, int item, char* lds) {
   typedef Block<T, D> B;
-  constexpr int LD = D + 4;                                // padded row of the joining buffer
-  __shared__ __attribute__((aligned(16))) float so[kWaves][16][LD];
-  __shared__ float sm[kWaves][16], sz[kWaves][16];
+  SplitLds<D>& l = *(SplitLds<D>*)lds;
   Item it;
-  if (!find_item<SHARED>(a, cut, (int)blockIdx.x, pt, &it)) return;
+  if (!find_item<SHARED>(a, cut, item, pt, &it)) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r16 = lane & 15, g = lane >> 4;
   Rows<T, D, MT> rows;
   rows.clear();
@@ -690,10 +697,10 @@ attend_split_kernel(AttendArgs a, AttendCut cut, Partials pt) {
   // blocks that every row sees, the next one on its way while one is worked on
   if (key + B::KEYS <= min(end, (int)least)) {
     Block<T, D> cur, nxt;
-    load_block<T, D, PAD>(cur, src, window, block, key);
+    load_block<T, D, PAD, STREAM>(cur, src, window, block, key);
     while (whole(cur)) {
       const bool more = key + STEP + B::KEYS <= min(end, (int)least);
-      if (more) load_block<T, D, PAD>(nxt, src, window, block + 1, key + STEP);
+      if (more) load_block<T, D, PAD, STREAM>(nxt, src, window, block + 1, key + STEP);
       rows.template step<false>(cur, key, (int)least, (int)most, scale);
       key += STEP;
       window.move(src, ++block);
@@ -705,7 +712,7 @@ attend_split_kernel(AttendArgs a, AttendCut cut, Partials pt) {
   const int from = key;
   while (key < end) {
     Block<T, D> b;
-    load_block<T, D, PAD>(b, src, window, block, key);
+    load_block<T, D, PAD, STREAM>(b, src, window, block, key);
     bad = bad || !whole(b);
     rows.template step<true>(b, key, (int)least, (int)most, scale);
     key += STEP;
@@ -719,8 +726,8 @@ attend_split_kernel(AttendArgs a, AttendCut cut, Partials pt) {
     if (mt > 0) __syncthreads();
     const float z = sum_over_g(rows.z[mt]);
     if (g == 0) {
-      sm[wave][r16] = rows.m[mt];
-      sz[wave][r16] = z;
+      l.m[wave][r16] = rows.m[mt];
+      l.z[wave][r16] = z;
     }
 #pragma unroll
     for (int hf = 0; hf < B::HN; ++hf)
@@ -728,20 +735,20 @@ attend_split_kernel(AttendArgs a, AttendCut cut, Partials pt) {
       for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int e = 0; e < B::CW; e += 4)
-          *(f32x4*)&so[wave][r16][16 * B::CW * hf + B::CW * (4 * g + i) + e] =
+          *(f32x4*)&l.o[wave][r16][16 * B::CW * hf + B::CW * (4 * g + i) + e] =
               f32x4{rows.o[mt][hf * B::CW + e][i], rows.o[mt][hf * B::CW + e + 1][i], rows.o[mt][hf * B::CW + e + 2][i],
                     rows.o[mt][hf * B::CW + e + 3][i]};
     __syncthreads();
     const int row = threadIdx.x >> 4, part = threadIdx.x & 15, r = it.tile * cut.rows + 16 * mt + row;
     if (r < it.seg.rows) {
-      float m = sm[0][row];
+      float m = l.m[0][row];
 #pragma unroll
-      for (int w = 1; w < kWaves; ++w) m = fmaxf(m, sm[w][row]);
+      for (int w = 1; w < kWaves; ++w) m = fmaxf(m, l.m[w][row]);
       float by[kWaves], total = 0.f;
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) {
-        by[w] = m == -INFINITY ? 1.f : exp2_fast(sm[w][row] - m);
-        total += sz[w][row] * by[w];
+        by[w] = m == -INFINITY ? 1.f : exp2_fast(l.m[w][row] - m);
+        total += l.z[w][row] * by[w];
       }
       constexpr int CNT = D / 16 >= 8 ? 8 : 4;
 #pragma unroll
@@ -752,7 +759,7 @@ attend_split_kernel(AttendArgs a, AttendCut cut, Partials pt) {
         for (int x = 0; x < CNT; ++x) {
           v[x] = 0.f;
 #pragma unroll
-          for (int w = 0; w < kWaves; ++w) v[x] += so[w][row][at + x] * by[w];
+          for (int w = 0; w < kWaves; ++w) v[x] += l.o[w][row][at + x] * by[w];
         }
         write_row<T, CNT>(a, it, pt, D, r, at, v, m, total);
       }
@@ -822,6 +829,7 @@ __device__ __forceinline__ bool tile_step(Rows<__bf16, D, MT>& R, const TileBuff
     for (int p = 0; p < B::KP; ++p) kf[t & 1][p] = b.k[t][p][lane];
   };
   read_k(0);
+  __builtin_amdgcn_s_setprio(1);                           // products before the other wavefronts' softmax: 1106 us, 1084 so
 #pragma unroll
   for (int t = 0; t < 4; ++t) {
     if (t < 3) read_k(t + 1);
@@ -838,6 +846,7 @@ __device__ __forceinline__ bool tile_step(Rows<__bf16, D, MT>& R, const TileBuff
     }
     __builtin_amdgcn_sched_barrier(0);
   }
+  __builtin_amdgcn_s_setprio(0);
   // V: lanes 4 j + c of 16 name columns 4 c .. 4 c + 3 of key j, lane i gets column i of the four keys
   typedef short Half4 __attribute__((ext_vector_type(4)));
   typedef __attribute__((address_space(3))) Half4* LdsHalf4;
@@ -912,6 +921,7 @@ __device__ __forceinline__ bool tile_step(Rows<__bf16, D, MT>& R, const TileBuff
         seen[hb][p] = (in && key < most ? 0xffffu : 0u) | (in && key + 1 < most ? 0xffff0000u : 0u);
       }
   }
+  __builtin_amdgcn_s_setprio(1);
 #pragma unroll
   for (int i = 0; i < STEPS; ++i) {
     const int hb = i / B::NT, nt = i % B::NT;
@@ -934,16 +944,23 @@ __device__ __forceinline__ bool tile_step(Rows<__bf16, D, MT>& R, const TileBuff
       R.o[mt][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y.v, w[hb][mt].w, R.o[mt][nt], 0, 0, 0);
     __builtin_amdgcn_sched_barrier(0);
   }
+  __builtin_amdgcn_s_setprio(0);
   return true;
 }
 
+template <int D>
+struct TileLds {
+  TileBuffer<D> buf[2];
+  int lims[2][kWaves];
+};
+
 template <int D, int MT, bool PAD, bool SHARED>
-__global__ void __launch_bounds__(kThreads, 2) attend_tile_kernel(AttendArgs a, AttendCut cut, Partials pt) {
+__device__ __forceinline__ void tile_item(const AttendArgs& a, const AttendCut& cut, const Partials& pt, int item, char* lds) {
   typedef Block<__bf16, D> B;
-  __shared__ TileBuffer<D> buf[2];
-  __shared__ int lims[2][kWaves];
+  TileBuffer<D>* buf = ((TileLds<D>*)lds)->buf;
+  int (&lims)[2][kWaves] = ((TileLds<D>*)lds)->lims;
   Item it;
-  if (!find_item<SHARED>(a, cut, (int)blockIdx.x, pt, &it)) return;
+  if (!find_item<SHARED>(a, cut, item, pt, &it)) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r16 = lane & 15, g = lane >> 4;
   const int row0 = it.tile * cut.rows + wave * 16 * MT;
   Rows<__bf16, D, MT> rows;
@@ -1145,33 +1162,58 @@ __global__ void __launch_bounds__(NW > kWaves ? NW * 64 : kThreads) attend_join_
   if (lane == 0 && a.lse != nullptr) a.lse[(int64_t)hq * a.total_q + tok] = z == 0.f ? -INFINITY : (m + __log2f(z)) * kLn2;
 }
 
-// A launch over one kind of segments: the tile kernel from 33 rows of a segment on (bf16, d <= 128), else the split one.
-template <typename T, int D, bool SHARED, bool PAD>
-hipError_t launch_cut(const AttendArgs& a, const AttendCut& cut, const Partials& pt, hipStream_t st) {
-  const int64_t items = max_items(cut, (int64_t)a.total_q * a.G, SHARED ? a.n_groups : a.n_seqs, a.Hk);
-  if (items >= (int64_t(1) << 31)) return hipErrorInvalidValue;
-  const dim3 grid((unsigned)items), block(kThreads);
-  if constexpr (sizeof(T) == 2 && D <= 128) {
-    if (cut.rows == 128) {
-      hipLaunchKernelGGL((attend_tile_kernel<D, 2, PAD, SHARED>), grid, block, 0, st, a, cut, pt);
-      return hipGetLastError();
+// ------------------------------------------------------------------------------------------------------------------
+// How a kind of segments is worked on: by split items of 16 rows, or tiles of 64 or 128 (0: there are none).
+constexpr int kNone = 0, kSplit = 16, kTile1 = 64, kTile2 = 128;
+
+template <typename T, int D, int KIND, bool PAD, bool SHARED, bool STREAM>
+__device__ __forceinline__ void run_item(const AttendArgs& a, const AttendCut& cut, const Partials& pt, int item, char* lds) {
+  if constexpr (KIND == kSplit) split_item<T, D, 1, PAD, SHARED, STREAM>(a, cut, pt, item, lds);
+  if constexpr (KIND == kTile1) tile_item<D, 1, PAD, SHARED>(a, cut, pt, item, lds);
+  if constexpr (KIND == kTile2) tile_item<D, 2, PAD, SHARED>(a, cut, pt, item, lds);
+}
+template <int D, int KIND>
+constexpr size_t lds_of() {
+  return KIND == kNone ? 0 : KIND == kSplit ? sizeof(SplitLds<D>) : sizeof(TileLds<D>);
+}
+
+// One launch has the items of both kinds, the shared ones first: those are the longer ones, and the own ones fill the units as they
+// come free.  (In turn, eight of each, some units end up with more of the long ones: shared prompt 121 us, 93 so.)
+template <typename T, int D, int OWN, int SHARED, bool PAD, bool STREAM>
+__global__ void __launch_bounds__(kThreads, D > 128 ? 1 : 2)
+attend_kernel(AttendArgs a, AttendCut own, AttendCut shared, Partials po, Partials ps, int n_shared) {
+  constexpr size_t LDS = lds_of<D, OWN>() > lds_of<D, SHARED>() ? lds_of<D, OWN>() : lds_of<D, SHARED>();
+  __shared__ __attribute__((aligned(16))) char lds[LDS];
+  int i = (int)blockIdx.x;
+  if constexpr (SHARED != kNone) {
+    if (i < n_shared) {
+      run_item<T, D, SHARED, PAD, true, STREAM>(a, shared, ps, i, lds);
+      return;
     }
-    if (cut.rows == 64) {
-      hipLaunchKernelGGL((attend_tile_kernel<D, 1, PAD, SHARED>), grid, block, 0, st, a, cut, pt);
-      return hipGetLastError();
-    }
+    i -= n_shared;                                         // a multiple of 8: an item's die is its head's
   }
-  hipLaunchKernelGGL((attend_split_kernel<T, D, 1, PAD, SHARED>), grid, block, 0, st, a, cut, pt);
+  run_item<T, D, OWN, PAD, false, STREAM>(a, own, po, i, lds);
+}
+
+template <typename T, int D, int OWN, int SHARED, bool STREAM>
+hipError_t launch_kinds(const AttendArgs& a, const AttendCut& own, const AttendCut& shared, const Partials& po, const Partials& ps,
+                        hipStream_t st) {
+  const int64_t rows = (int64_t)a.total_q * a.G;
+  const int64_t n_own = (max_items(own, rows, a.n_seqs, a.Hk) + 7) & ~int64_t(7);
+  const int64_t n_shared = SHARED == kNone ? 0 : (max_items(shared, rows, a.n_groups, a.Hk) + 7) & ~int64_t(7);
+  if (n_own + n_shared >= (int64_t(1) << 31)) return hipErrorInvalidValue;
+  const dim3 grid((unsigned)(n_own + n_shared)), block(kThreads);
+  if (a.d == D)
+    hipLaunchKernelGGL((attend_kernel<T, D, OWN, SHARED, false, STREAM>), grid, block, 0, st, a, own, shared, po, ps, (int)n_shared);
+  else
+    hipLaunchKernelGGL((attend_kernel<T, D, OWN, SHARED, true, STREAM>), grid, block, 0, st, a, own, shared, po, ps, (int)n_shared);
   return hipGetLastError();
 }
 
+// The kind for segments of about `rows` rows.
 AttendCut cut_for(bool tiles, int64_t rows) {
-  AttendCut c = {16, 512, 2, 0};
-  if (tiles && rows > 32) {
-    c.rows = rows > 64 ? 128 : 64;
-    c.min_tiles = 4;
-  }
-  return c;
+  if (tiles && rows > 16) return AttendCut{rows > 64 ? kTile2 : kTile1, 512, 4, 0};
+  return AttendCut{kSplit, 512, 2, 0};
 }
 
 template <typename T, int D>
@@ -1185,21 +1227,40 @@ hipError_t launch_d(const PagedWorkspace& ws, const AttendArgs& args, hipStream_
   shared.cap = max_partials(shared, rows, a.Hk);
   // a sequence whose own rows fill a tile gains nothing; and every row of a group is joined from two parts, for which there has to be
   // room
-  if (a.n_groups > 0 && (most > 64 || shared.cap + rows * a.Hk > room)) a.n_groups = 0;
+  if (a.n_groups > 0 && (own.rows == kTile2 || shared.cap + rows * a.Hk > room)) a.n_groups = 0;
   if (a.n_groups == 0) shared.cap = 0;
   own.cap = room - shared.cap;
   Partials po, ps;
   ps.o = ws.part;
   ps.mz = ws.part_mz;
   ps.plan = ws.plan + kPagedMaxSeqs;
+  ps.group = nullptr;
   po.o = ws.part + shared.cap * D;
   po.mz = ws.part_mz + shared.cap;
   po.plan = ws.plan;
   po.group = ws.group;
-  ps.group = nullptr;
-  hipError_t e = hipSuccess;
-  if (a.n_groups > 0) e = a.d == D ? launch_cut<T, D, true, false>(a, shared, ps, st) : launch_cut<T, D, true, true>(a, shared, ps, st);
-  if (e == hipSuccess) e = a.d == D ? launch_cut<T, D, false, false>(a, own, po, st) : launch_cut<T, D, false, true>(a, own, po, st);
+  hipError_t e = hipErrorInvalidValue;
+  const int ks = a.n_groups > 0 ? shared.rows : kNone;
+  if constexpr (kTiles) {
+    if (ks == kNone) {
+      e = own.rows == kTile2   ? launch_kinds<T, D, kTile2, kNone, true>(a, own, shared, po, ps, st)
+          : own.rows == kTile1 ? launch_kinds<T, D, kTile1, kNone, true>(a, own, shared, po, ps, st)
+                               : launch_kinds<T, D, kSplit, kNone, true>(a, own, shared, po, ps, st);
+    } else if (own.rows == kTile1) {
+      e = ks == kTile2   ? launch_kinds<T, D, kTile1, kTile2, true>(a, own, shared, po, ps, st)
+          : ks == kTile1 ? launch_kinds<T, D, kTile1, kTile1, true>(a, own, shared, po, ps, st)
+                         : launch_kinds<T, D, kTile1, kSplit, true>(a, own, shared, po, ps, st);
+    } else {
+      e = ks == kTile2   ? launch_kinds<T, D, kSplit, kTile2, true>(a, own, shared, po, ps, st)
+          : ks == kTile1 ? launch_kinds<T, D, kSplit, kTile1, true>(a, own, shared, po, ps, st)
+                         : launch_kinds<T, D, kSplit, kSplit, true>(a, own, shared, po, ps, st);
+    }
+  } else if (ks == kNone) {
+    e = most <= kSplit ? launch_kinds<T, D, kSplit, kNone, true>(a, own, shared, po, ps, st)
+                       : launch_kinds<T, D, kSplit, kNone, false>(a, own, shared, po, ps, st);
+  } else {
+    e = launch_kinds<T, D, kSplit, kSplit, false>(a, own, shared, po, ps, st);
+  }
   if (e != hipSuccess) return e;
   const int64_t out_rows = (int64_t)a.total_q * a.Hq;
   // few rows are cut into many pieces each

@@ -32,6 +32,7 @@ __device__ __forceinline__ void store_piece(char* p, Piece x) {
 
 constexpr int kWriteUnroll = 4;            // pieces of K, and as many of V, that a thread has on their way
 constexpr int kWriteTokens = kWriteThreads;   // most tokens of a workgroup
+constexpr int kWriteStaged = 1024;         // sequences whose rows and lengths a workgroup takes to LDS (at most 20 KB) rather than look them up
 
 // Rows of head_dim elements into the last cu[i + 1] - cu[i] positions of table row rows[i], for every i: a copy, bound by memory.
 // A workgroup has some neighbouring tokens of a KV head: first a thread for each finds where it stands and where it goes (sequence,
@@ -40,7 +41,7 @@ constexpr int kWriteTokens = kWriteThreads;   // most tokens of a workgroup
 // grid: x = blocks of a.tokens tokens, y = KV head.
 template <bool PAGED, bool STREAM>
 __global__ void __launch_bounds__(kWriteThreads) pages_write_kernel(PagesWriteArgs a) {
-  extern __shared__ int32_t lds[];         // cu [n + 1]; rows [n], lengths [n]: of the rows written to, then of those read
+  extern __shared__ int32_t lds[];         // cu [n + 1]; staged: rows [n], lengths [n] of the rows written to, then of those read
   __shared__ int64_t from[kWriteTokens], to[kWriteTokens];               // byte offsets within the head's source and pages; to -1: none
   int32_t* cu = lds;
   int32_t* row = lds + a.n + 1;
@@ -52,9 +53,10 @@ __global__ void __launch_bounds__(kWriteThreads) pages_write_kernel(PagesWriteAr
   const int32_t* idx = a.idx != nullptr ? a.idx + (a.idx_rows == 1 ? 0 : (int64_t)h * a.total) : nullptr;
   const int t = tid < n_tok ? (idx != nullptr ? idx[j0 + tid] : j0 + tid) : 0;
   bool bad = false;
+  const bool staged = a.n <= kWriteStaged;
   for (int i = tid; i <= a.n; i += kWriteThreads) {
     cu[i] = a.cu[i];
-    if (i < a.n) {
+    if (staged && i < a.n) {
       const int r = a.rows[i];
       int L;
       row[i] = row_length(a.map, r, &L) ? r : -1;
@@ -70,12 +72,24 @@ __global__ void __launch_bounds__(kWriteThreads) pages_write_kernel(PagesWriteAr
   if (tid < n_tok) {
     const int j = j0 + tid, i = sequence_of(cu, a.n, j);
     int64_t f = -1, w = -1;
+    int r, L, rs = -1, Ls = 0;
+    if (staged) {
+      r = row[i];
+      L = len[i];
+      if (PAGED) {
+        rs = src_row[i];
+        Ls = src_len[i];
+      }
+    } else {
+      r = row_length(a.map, a.rows[i], &L) ? a.rows[i] : -1;
+      if (PAGED) rs = row_length(a.map, a.src_rows[i], &Ls) ? a.src_rows[i] : -1;
+    }
     if (PAGED) {
-      if (t < src_len[i]) f = token_offset(a.map, src_row[i], t);        // t < 0: -1 as well
+      if (t < Ls) f = token_offset(a.map, rs, t);          // t < 0: -1 as well
     } else if ((uint32_t)t < (uint32_t)a.n_src) {
       f = t;
     }
-    if (cu[i] <= j && j < cu[i + 1]) w = token_offset(a.map, row[i], len[i] - (cu[i + 1] - j));
+    if (cu[i] <= j && j < cu[i + 1]) w = token_offset(a.map, r, L - (cu[i + 1] - j));
     bad = f < 0 || w < 0;
     from[tid] = f;
     to[tid] = bad ? -1 : w;
@@ -155,7 +169,7 @@ __device__ __forceinline__ int scan_needs(const int (&need)[kPagedMaxSeqs / kBoo
 
 // The first `want` pages whose count is 0, in order, to fresh[]; returns how many there are (at most `want`).
 __device__ __forceinline__ int find_free(const int32_t* refs, int n_pages, int want, int32_t* fresh, BookLds& l) {
-  constexpr int PER = 8;
+  constexpr int PER = 16;                  // pages of a thread and round: 64K pages take four
   int base = 0;
   for (int64_t p0 = 0; p0 < n_pages && base < want; p0 += kBookThreads * PER) {
     const int64_t p = p0 + (int64_t)threadIdx.x * PER;
@@ -274,50 +288,77 @@ __global__ void __launch_bounds__(kBookThreads) pages_fork_kernel(PagesForkArgs 
   }
 }
 
-// The continuations' rows and counts (slice 0), and the filled tokens of their last pages (slices from 1: layer, K or V).
+// The continuations' rows and counts (slice 0), and the filled tokens of their last pages (slices from 1: layer, K or V), kForkGroup
+// neighbouring continuations a workgroup.  grid: x = groups, y = slices, z = blocks of kForkPieces pieces of the page.  Neighbours mostly
+// have one parent: its pieces are read once and stored for each of them (24 parents continued 8 times, 16 layers: 136 us with a
+// workgroup for each continuation).
+constexpr int kForkGroup = 8;
+constexpr int kForkUnroll = 8;             // pieces of a thread
+constexpr int kForkPieces = kWriteThreads * kForkUnroll;
 __global__ void __launch_bounds__(kWriteThreads) pages_fork_copy_kernel(PagesForkArgs a) {
   const PageMap& m = a.map;
-  const int4 f = a.forks[blockIdx.x];
-  if (f.z <= 0) return;
-  const int full = f.z >> m.ps_shift, part = f.z & (m.ps - 1);
-  const int32_t* from = m.table + (int64_t)f.x * m.row_stride;
-  if (blockIdx.y == 0) {
-    int32_t* to = a.table + (int64_t)f.y * m.row_stride;
-    bool bad = false;
-    for (int t = threadIdx.x; t < full; t += kWriteThreads) {
-      const int page = from[t];
-      to[t] = page;
-      if ((uint32_t)page < (uint32_t)m.n_pages) atomicAdd(&a.refs[page], 1); else bad = true;
+  const int i0 = (int)blockIdx.x * kForkGroup, count = min(kForkGroup, a.n - i0);
+  __shared__ int4 forks[kForkGroup];
+  __shared__ int32_t last[kForkGroup];     // the parent's last, partly filled page, or -1
+  if ((int)threadIdx.x < count) {
+    const int4 f = a.forks[i0 + threadIdx.x];
+    forks[threadIdx.x] = f;
+    int page = -1;
+    if (f.z > 0 && f.w >= 0) {
+      page = m.table[(int64_t)f.x * m.row_stride + (f.z >> m.ps_shift)];
+      if ((uint32_t)page >= (uint32_t)m.n_pages) {
+        page = -1;
+        paged_fault(m);
+      }
     }
-    if (threadIdx.x == 0 && part != 0) to[full] = f.w;
+    last[threadIdx.x] = page;
+  }
+  __syncthreads();
+  if (blockIdx.y == 0) {
+    if (blockIdx.z != 0) return;
+    bool bad = false;
+    for (int i = 0; i < count; ++i) {
+      const int4 f = forks[i];
+      if (f.z <= 0) continue;
+      const int full = f.z >> m.ps_shift;
+      const int32_t* from = m.table + (int64_t)f.x * m.row_stride;
+      int32_t* to = a.table + (int64_t)f.y * m.row_stride;
+      for (int t = threadIdx.x; t < full; t += kWriteThreads) {
+        const int page = from[t];
+        to[t] = page;
+        if ((uint32_t)page < (uint32_t)m.n_pages) atomicAdd(&a.refs[page], 1); else bad = true;
+      }
+      if (threadIdx.x == 0 && f.w >= 0) to[full] = f.w;
+    }
     if (bad) paged_fault(m);
     return;
   }
-  if (part == 0) return;
   const int slice = (int)blockIdx.y - 1, layer = slice >> 1;
   char* base = (char*)((slice & 1) == 0 ? a.k_ptrs[layer] : a.v_ptrs[layer]);
-  const int page = from[full];
-  if ((uint32_t)page >= (uint32_t)m.n_pages) {
-    if (threadIdx.x == 0) paged_fault(m);
-    return;
-  }
-  const uint32_t per_head = (uint32_t)(part * a.cpr), total = per_head * (uint32_t)a.Hk;
-  const char* src = base + (int64_t)page * m.page;
-  char* dst = base + (int64_t)f.w * m.page;
-  constexpr int U = 8;                     // pieces that a thread has on their way
-  for (uint32_t q0 = threadIdx.x; q0 < total; q0 += kWriteThreads * U) {
-    Piece x[U];
-    int64_t off[U];
+  const uint32_t q0 = blockIdx.z * (uint32_t)kForkPieces + threadIdx.x;
+  Piece x[kForkUnroll];
+  int64_t off[kForkUnroll];
+  int parent = -1;
+  for (int i = 0; i < count; ++i) {
+    const int4 f = forks[i];
+    const int page = last[i];
+    if (page < 0) continue;
+    const uint32_t per_head = (uint32_t)(f.z & (m.ps - 1)) * (uint32_t)a.cpr, total = per_head * (uint32_t)a.Hk;
+    if (f.x != parent) {
+      parent = f.x;
+      const char* src = base + (int64_t)page * m.page;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const uint32_t q = min(q0 + u * kWriteThreads, total - 1u), h = q / per_head, e = q - h * per_head;
-      const uint32_t t = a.cpr_shift >= 0 ? e >> a.cpr_shift : e / (uint32_t)a.cpr;
-      off[u] = (int64_t)h * m.head + (int64_t)t * m.tok + (int64_t)(e - t * (uint32_t)a.cpr) * 16;
-      x[u] = load_piece<false>(src + off[u]);
+      for (int u = 0; u < kForkUnroll; ++u) {
+        const uint32_t q = min(q0 + u * kWriteThreads, total - 1u), h = q / per_head, e = q - h * per_head;
+        const uint32_t t = a.cpr_shift >= 0 ? e >> a.cpr_shift : e / (uint32_t)a.cpr;
+        off[u] = (int64_t)h * m.head + (int64_t)t * m.tok + (int64_t)(e - t * (uint32_t)a.cpr) * 16;
+        x[u] = load_piece<false>(src + off[u]);
+      }
     }
+    char* dst = base + (int64_t)f.w * m.page;
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (q0 + u * kWriteThreads < total) store_piece<false>(dst + off[u], x[u]);
+    for (int u = 0; u < kForkUnroll; ++u)
+      if (q0 + u * kWriteThreads < total) store_piece<true>(dst + off[u], x[u]);
   }
 }
 
@@ -363,7 +404,7 @@ hipError_t launch_pages_write(const PagesWriteArgs& args, int Hk, hipStream_t st
   a.tokens = round < 1 ? 1 : round > kWriteTokens ? kWriteTokens : round;
   while (a.tokens > 8 && (int64_t)(a.total / a.tokens + 1) * Hk < 256) a.tokens /= 2;
   const int64_t blocks = ((int64_t)a.total + a.tokens - 1) / a.tokens;
-  const size_t lds = (size_t)((a.src_rows != nullptr ? 5 : 3) * a.n + 1) * sizeof(int32_t);
+  const size_t lds = (size_t)(a.n + 1 + (a.n > kWriteStaged ? 0 : (a.src_rows != nullptr ? 4 : 2) * a.n)) * sizeof(int32_t);
   const bool stream = 4 * (int64_t)a.total * a.cpr * 16 * Hk >= kWriteStreamBytes;
   const dim3 grid((unsigned)blocks, (unsigned)Hk), block(kWriteThreads);
   if (a.src_rows != nullptr && stream)
@@ -380,7 +421,11 @@ hipError_t launch_pages_write(const PagesWriteArgs& args, int Hk, hipStream_t st
 hipError_t launch_pages_fork(const PagesForkArgs& a, int32_t* fresh, hipStream_t st) {
   if (a.n == 0) return hipSuccess;
   hipLaunchKernelGGL(pages_fork_kernel, dim3(1), dim3(kBookThreads), 0, st, a, fresh);
-  hipLaunchKernelGGL(pages_fork_copy_kernel, dim3((unsigned)a.n, (unsigned)(1 + 2 * a.n_layers)), dim3(kWriteThreads), 0, st, a);
+  const int64_t pieces = (int64_t)(a.map.ps - 1) * a.cpr * a.Hk;
+  const dim3 grid((unsigned)((a.n + kForkGroup - 1) / kForkGroup), (unsigned)(1 + 2 * a.n_layers),
+                  (unsigned)((pieces + kForkPieces - 1) / kForkPieces));
+  if (grid.z > 65535u) return hipErrorInvalidValue;
+  hipLaunchKernelGGL(pages_fork_copy_kernel, grid, dim3(kWriteThreads), 0, st, a);
   return hipGetLastError();
 }
 

@@ -116,8 +116,8 @@ asl_status asl_pages_fork(asl_ctx* ctx, const asl_pages* p, void* const* k_ptrs,
   if (n_layers > 16384) return fail(ctx, ASL_EUNSUPPORTED, "more than 16384 layers per call");
   if (n_layers > 0 && (!k_ptrs || !v_ptrs)) return fail(ctx, ASL_EINVAL, "null tensor pointer");
   const int64_t row_bytes = (int64_t)p->head_dim * elem_bytes(p->dtype);
-  if (row_bytes / 16 * p->page_size * p->n_kv_heads >= (int64_t(1) << 31))
-    return fail(ctx, ASL_EUNSUPPORTED, "pages of 2^35 bytes or more");
+  if (row_bytes / 16 * p->page_size * p->n_kv_heads > (int64_t(1) << 26))
+    return fail(ctx, ASL_EUNSUPPORTED, "pages of more than 2^30 bytes");
   a.table = table;
   a.kv_len = kv_len;
   a.refs = refs;

@@ -140,11 +140,12 @@ def _attend(ctx, c, q, n_q, Hq, causal=True, groups=None, rows=None, scale=0.0, 
 
 
 def _oracle(c, q, n_q, scale=0.0, causal=True, rows=None):
-    q = q.double().cpu().numpy()
+    q, k, v = (x.double().cpu().numpy() for x in (q, c.k, c.v))
+    row = lambda x, r: po.gather(x, c.host_table[r], c.lens[r])
     parts, at = [], 0
     for b, n in enumerate(n_q):
         r = b if rows is None else rows[b]
-        parts.append(po.attention(q[at:at + n], c.row(c.k, r), c.row(c.v, r), scale or c.d ** -0.5, causal))
+        parts.append(po.attention(q[at:at + n], row(k, r), row(v, r), scale or c.d ** -0.5, causal))
         at += n
     return (np.concatenate([p[0] for p in parts]), np.concatenate([p[1] for p in parts], axis=1),
             np.concatenate([p[2] for p in parts]), np.concatenate([p[3] for p in parts]))
@@ -690,4 +691,101 @@ def test_a_prompt_is_pruned_continued_and_decoded(ctx, gpu_device):
     assert kv.tolist() == [keep] + [keep + 21] * 4 + [0]
     ctx.asl_pages_free(p, i(0, 1, 2, 3, 4), 5, table, kv, refs)
     assert int(refs.abs().sum()) == 0 and int(kv.sum()) == 0
+    assert ctx.asl_device_fault() == 0
+
+
+# ----------------------------------------------------------------------------------------- more sequences, rows, jumps
+@pytest.fixture(scope="module")
+def wide(gpu_device):
+    c = asl.Asl(2, 1, 1)
+    c.asl_paged_reserve(4096, 1 << 17, 128)
+    yield c
+    assert c.asl_device_fault() == 0
+    c.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,groups", [(65, None), (130, [(64, 200), (66, 130)]), (700, None), (4096, None), (1500, [(3, 140)] * 500)])
+def test_attention_of_many_sequences(wide, gpu_device, n, groups, dtype):
+    """More sequences than a wavefront has lanes: each lane plans for several."""
+    rng = np.random.default_rng(n)
+    own = rng.integers(0 if groups is None else 3, 40, n)
+    lens = [int(x) + (0 if groups is None else p) for x, p in
+            zip(own, [0] * n if groups is None else [p for m, p in groups for _ in range(m)])]
+    n_q = [int(x) for x in rng.integers(0 if groups is None else 1, 3, n)]
+    _case(wide, gpu_device, lens, n_q, 4, 2, 64, 16, dtype, groups=groups, what="many sequences")
+
+
+@pytest.mark.parametrize("n", [1024, 1025, 4096])
+def test_pages_of_many_sequences(wide, gpu_device, n):
+    """The most rows of a call, grown, written, compacted, continued and freed."""
+    torch = _torch()
+    rng = np.random.default_rng(n)
+    dev, Hk, d, ps, half = gpu_device, 1, 8, 16, n // 2
+    lens = [int(x) for x in rng.integers(0, 30, half)] + [0] * (n - half)
+    c = Cache(dev, lens, Hk, d, ps, "bf16", 7, row_stride=6, spare=3 * n)
+    table, kv, refs = _books(c)
+    add = [int(x) for x in rng.integers(0, 20, n)]
+    rows = rng.permutation(n)
+    po.grow(table, kv, refs, rows, [add[r] for r in rows], ps)
+    wide.asl_pages_grow(c.desc(), _ints(rows, dev), _ints([add[r] for r in rows], dev), n, c.table, c.kv_len, c.refs)
+    _same_books(c, table, kv, refs, "grow")
+    counts = [add[r] for r in rows]
+    total = sum(counts)
+    k = torch.randn((Hk, total, d)).to(torch.bfloat16).to(dev)
+    want = c.k.double().cpu().numpy()
+    po.write(want, table, kv, rows, counts, np.split(k.double().cpu().numpy(), np.cumsum(counts)[:-1], axis=1))
+    cu = _ints(np.concatenate([[0], np.cumsum(counts)]), dev)
+    wide.asl_pages_write(c.desc(), k, k, _ints(rows, dev), cu, n, total, c.table, c.kv_len, c.k, c.v)
+    _same_pages(c.k, want, "write")
+    wide.asl_pages_free(c.desc(), _ints(rows[:n - half], dev), n - half, c.table, c.kv_len, c.refs)
+    po.free(table, kv, refs, rows[:n - half], ps)
+    _same_books(c, table, kv, refs, "free")
+    held = rows[n - half:]
+    parents = held[rng.integers(0, half, n - half)]
+    host = [(want, c.v.double().cpu().numpy())]
+    po.fork(table, kv, refs, host, parents, rows[:n - half])
+    ptr = lambda x: torch.tensor([x.data_ptr()], dtype=torch.int64, device=dev)
+    wide.asl_pages_fork(c.desc(), ptr(c.k), ptr(c.v), 1, _ints(parents, dev), _ints(rows[:n - half], dev), n - half, c.table, c.kv_len,
+                        c.refs)
+    _same_books(c, table, kv, refs, "fork")
+    _same_pages(c.k, host[0][0], "fork")
+    # the last token of each held row into the last place of another, which is emptied and grown first
+    m = min(half, n - half)
+    dst = rows[:m]
+    po.free(table, kv, refs, dst, ps)
+    po.grow(table, kv, refs, dst, [1] * m, ps)
+    wide.asl_pages_free(c.desc(), _ints(dst, dev), m, c.table, c.kv_len, c.refs)
+    wide.asl_pages_grow(c.desc(), _ints(dst, dev), _ints([1] * m, dev), m, c.table, c.kv_len, c.refs)
+    _same_books(c, table, kv, refs, "again")
+    src = held[np.argsort(-kv[held], kind="stable")][:m]
+    keep = [i for i in range(m) if kv[src[i]] > 0]
+    src, dst = src[keep], dst[keep]
+    pick = [int(kv[r]) - 1 for r in src]
+    want = c.k.double().cpu().numpy()
+    vals = [po.gather(want, table[r], int(kv[r]))[:, p:p + 1] for r, p in zip(src, pick)]
+    po.write(want, table, kv, dst, [1] * len(dst), vals)
+    wide.asl_pages_compact(c.desc(), _ints(src, dev), _ints(dst, dev), _ints(np.arange(len(dst) + 1), dev), len(dst), len(dst),
+                           _ints([pick], dev), c.table, c.kv_len, c.k, c.v)
+    _same_pages(c.k, want, "compact")
+    assert wide.asl_device_fault() == 0
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n_q", [8, 40])
+@pytest.mark.parametrize("shared", [False, True])
+def test_attention_logits_that_rise_by_leaps(ctx, gpu_device, shared, n_q, d):
+    """The largest logit of a row grows by 100 nats and more from tile to tile, several times over the keys, for some rows."""
+    torch = _torch()
+    L = 700
+    c = Cache(gpu_device, [L, L] if shared else [L], 1, d, 16, "bf16", 3, shared=[(0, 2, 640)] if shared else ())
+    for r in range(len(c.lens)):
+        for t, size in ((130, 4.0), (200, 8.0), (420, 16.0), (641, 24.0), (690, 32.0)):
+            c.k[c.host_table[r, t // 16], 0, t % 16] = size
+    G = 4
+    q = _queries(n_q * len(c.lens), G, d, "bf16", gpu_device, 5, spread=0.5)
+    q[::3] = q[::3].abs() * 2 + 1                             # these rows climb; the others see the same keys with logits of any sign
+    n = [n_q] * len(c.lens)
+    out, lse = _attend(ctx, c, q, n, G, groups=[(2, 640)] if shared else None)
+    _check(out, lse, _oracle(c, q, n), d, L, "bf16", "leaps")
     assert ctx.asl_device_fault() == 0
