@@ -130,6 +130,7 @@ struct Partials {
   float2* mz;              // [cap]
   int4* plan;              // of the segments
   int32_t* group;          // [n_seqs] own segments: the sequence's group or -1
+  uint32_t* arrived;       // [cap] zeros: pieces of a row tile that are there, counted at its first slot; null: a launch joins them
 };
 
 struct Item {
@@ -614,12 +615,28 @@ struct Rows {
 // ------------------------------------------------------------------------------------------------------------------
 
 
+// Two floats written through, and read past, this die's caches (device-scope atomic accesses).
+__device__ __forceinline__ void store_through(float* p, float x, float y) {
+  const unsigned long long w = ((unsigned long long)__float_as_uint(y) << 32) | __float_as_uint(x);
+  __hip_atomic_store((unsigned long long*)p, w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 load_through(const float* p) {
+  const unsigned long long w = __hip_atomic_load((const unsigned long long*)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return make_float2(__uint_as_float((uint32_t)w), __uint_as_float((uint32_t)(w >> 32)));
+}
+
 // Writes row r of an item: to out and lse if its results are whole, else to its slot.  v: CNT elements from e0 on.
 template <typename T, int CNT>
 __device__ __forceinline__ void write_row(const AttendArgs& a, const Item& it, const Partials& pt, int D, int r, int e0,
                                           const float (&v)[CNT], float m, float z) {
   if (it.slot >= 0) {
     const int64_t slot = it.slot + ((int64_t)it.h * it.splits + it.split) * it.seg.rows + r;
+    if (pt.arrived != nullptr) {                           // for another workgroup of this launch: see join_last
+#pragma unroll
+      for (int x = 0; x < CNT; x += 2) store_through(pt.o + slot * D + e0 + x, v[x], v[x + 1]);
+      if (e0 == 0) store_through((float*)(pt.mz + slot), m, z);
+      return;
+    }
 #pragma unroll
     for (int x = 0; x < CNT; x += 4) *(f32x4*)(pt.o + slot * D + e0 + x) = f32x4{v[x], v[x + 1], v[x + 2], v[x + 3]};
     if (e0 == 0) pt.mz[slot] = make_float2(m, z);
@@ -636,6 +653,66 @@ __device__ __forceinline__ void write_row(const AttendArgs& a, const Item& it, c
     *(Out*)to = w;
   }
   if (e0 == 0 && a.lse != nullptr) a.lse[(int64_t)hq * a.total_q + tok] = z == 0.f ? -INFINITY : (m + __log2f(z)) * kLn2;
+}
+
+// The workgroup that brings the last piece of a tile of 16 rows joins them, 16 threads a row (few pieces: the launch that joins many
+// would take longer to begin than this takes).  Pieces are written through to memory, every wavefront waits until its own are
+// there, then one thread counts the workgroup's in; whoever counts the last one reads them past its caches.  (With
+// fences instead, which write a die's whole cache back, 8 sequences of 1024 keys took 40 us instead of 12.)  The
+// count is put back to 0 for the next call.
+template <typename T, int D>
+__device__ __forceinline__ void join_last(const AttendArgs& a, const AttendCut& cut, const Partials& pt, const Item& it, uint32_t* lds) {
+  const int64_t first = it.slot + (int64_t)it.h * it.splits * it.seg.rows + it.tile * cut.rows;
+  __builtin_amdgcn_s_waitcnt(0);                           // this wavefront's pieces are in memory
+  __syncthreads();
+  if (threadIdx.x == 0) *lds = __hip_atomic_fetch_add(&pt.arrived[first], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __syncthreads();
+  if (*lds + 1u != (uint32_t)it.splits) return;
+  const int row = threadIdx.x >> 4, part = threadIdx.x & 15, r = it.tile * cut.rows + row;
+  if (threadIdx.x == 0) __hip_atomic_store(&pt.arrived[first], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  if (r >= it.seg.rows) return;
+  constexpr int PER = D / 16, BATCH = 4;                   // elements of a thread, pieces at once
+  float v[PER], m = -INFINITY, z = 0.f;
+#pragma unroll
+  for (int x = 0; x < PER; ++x) v[x] = 0.f;
+  for (int s0 = 0; s0 < it.splits; s0 += BATCH) {
+    float2 mz[BATCH];
+    float2 o[BATCH][PER / 2];
+#pragma unroll
+    for (int u = 0; u < BATCH; ++u) {
+      const int64_t slot = first + row + (int64_t)min(s0 + u, it.splits - 1) * it.seg.rows;
+      mz[u] = load_through((const float*)(pt.mz + slot));
+#pragma unroll
+      for (int x = 0; x < PER / 2; ++x) o[u][x] = load_through(pt.o + slot * D + part * PER + 2 * x);
+    }
+    float top = m;
+#pragma unroll
+    for (int u = 0; u < BATCH; ++u)
+      if (s0 + u < it.splits) top = fmaxf(top, mz[u].x);
+    const float by = top == -INFINITY ? 1.f : exp2_fast(m - top);
+    m = top;
+    z *= by;
+#pragma unroll
+    for (int x = 0; x < PER; ++x) v[x] *= by;
+#pragma unroll
+    for (int u = 0; u < BATCH; ++u) {
+      if (s0 + u >= it.splits) continue;
+      const float w = m == -INFINITY ? 1.f : exp2_fast(mz[u].x - m);
+      z += mz[u].y * w;
+#pragma unroll
+      for (int x = 0; x < PER; ++x) v[x] += (x % 2 == 0 ? o[u][x / 2].x : o[u][x / 2].y) * w;
+    }
+  }
+  Item whole = it;
+  whole.slot = -1;
+  constexpr int CNT = PER >= 8 ? 8 : 4;
+#pragma unroll
+  for (int x0 = 0; x0 < PER; x0 += CNT) {
+    float y[CNT];
+#pragma unroll
+    for (int x = 0; x < CNT; ++x) y[x] = v[x0 + x];
+    write_row<T, CNT>(a, whole, pt, D, r, part * PER + x0, y, m, z);
+  }
 }
 
 // What the wavefronts of a split item leave for each other.
@@ -765,6 +842,7 @@ __device__ __forceinline__ void split_item(const AttendArgs& a, const AttendCut&
       }
     }
   }
+  if (!SHARED && pt.arrived != nullptr && it.slot >= 0) join_last<T, D>(a, cut, pt, it, (uint32_t*)&l.m[0][0]);
 }
 
 // ------------------------------------------------------------------------------------------------------------------
@@ -1210,6 +1288,12 @@ hipError_t launch_kinds(const AttendArgs& a, const AttendCut& own, const AttendC
   return hipGetLastError();
 }
 
+// The longest sequences whose pieces (of 128 keys or more) are joined within the launch.
+#ifndef ASL_JK
+#define ASL_JK 2048
+#endif
+constexpr int kJoinKeys = ASL_JK;
+
 // The kind for segments of about `rows` rows.
 AttendCut cut_for(bool tiles, int64_t rows) {
   if (tiles && rows > 16) return AttendCut{rows > 64 ? kTile2 : kTile1, 512, 4, 0};
@@ -1239,6 +1323,9 @@ hipError_t launch_d(const PagedWorkspace& ws, const AttendArgs& args, hipStream_
   po.mz = ws.part_mz + shared.cap;
   po.plan = ws.plan;
   po.group = ws.group;
+  ps.arrived = nullptr;
+  // Few pieces of few rows are joined by the workgroup that brings the last one.
+  po.arrived = a.n_groups == 0 && own.rows == kSplit && a.max_kv_len <= kJoinKeys ? ws.arrived + shared.cap : nullptr;
   hipError_t e = hipErrorInvalidValue;
   const int ks = a.n_groups > 0 ? shared.rows : kNone;
   if constexpr (kTiles) {
@@ -1261,7 +1348,7 @@ hipError_t launch_d(const PagedWorkspace& ws, const AttendArgs& args, hipStream_
   } else {
     e = launch_kinds<T, D, kSplit, kSplit, false>(a, own, shared, po, ps, st);
   }
-  if (e != hipSuccess) return e;
+  if (e != hipSuccess || po.arrived != nullptr) return e;
   const int64_t out_rows = (int64_t)a.total_q * a.Hq;
   // few rows are cut into many pieces each
   if (out_rows <= 256)

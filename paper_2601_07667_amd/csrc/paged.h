@@ -14,6 +14,7 @@ struct PagedWorkspace {
   int32_t max_seqs, max_query_rows, max_head_dim;
   float* part;             // [part_rows][max_head_dim, a power of two >= 64] attention: unnormalised results of cut rows ...
   float2* part_mz;         // [part_rows] ... with their reference and sum
+  uint32_t* arrived;       // [part_rows] zeros between calls
   int64_t part_rows;
   int4* plan;              // [2][kPagedMaxSeqs] how sequences and groups were cut
   int32_t* group;          // [kPagedMaxSeqs] the sequences' groups

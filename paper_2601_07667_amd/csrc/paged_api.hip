@@ -62,7 +62,8 @@ asl_status asl_paged_reserve(asl_ctx* ctx, int32_t max_seqs, int32_t max_query_r
   // and for the pieces that long spans are cut into
   w.part_rows = 2 * (int64_t)(max_query_rows < 131072 ? max_query_rows : 131072) + asl::kCutRows;
   const int D = max_head_dim <= 64 ? 64 : max_head_dim <= 128 ? 128 : 256;
-  const size_t part = take((size_t)w.part_rows * D * sizeof(float)), part_mz = take((size_t)w.part_rows * sizeof(float2));
+  const size_t part = take((size_t)w.part_rows * D * sizeof(float)), part_mz = take((size_t)w.part_rows * sizeof(float2)),
+               arrived = take((size_t)w.part_rows * sizeof(uint32_t));
   char* base = nullptr;
   hipError_t e = hipMalloc(&base, off);
   if (e != hipSuccess) {
@@ -77,6 +78,7 @@ asl_status asl_paged_reserve(asl_ctx* ctx, int32_t max_seqs, int32_t max_query_r
   w.group = (int32_t*)(base + group);
   w.part = (float*)(base + part);
   w.part_mz = (float2*)(base + part_mz);
+  w.arrived = (uint32_t*)(base + arrived);
   w.max_seqs = max_seqs;
   w.max_query_rows = max_query_rows;
   w.max_head_dim = max_head_dim;
