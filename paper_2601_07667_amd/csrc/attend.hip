@@ -43,6 +43,8 @@ constexpr float kWideSlack = 60.f;
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
+__device__ __forceinline__ void paged_fault(const PageMap& m) { atomicOr(m.fault, kFaultPaged); }
+
 // Maximum / sum over the four lanes that share lane % 16.
 __device__ __forceinline__ float max_over_g(float x) {
   auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -77,6 +79,8 @@ struct Segment {
   int row, len;            // table row and its tokens
   int t0, span;            // first key tile and number of key tiles
   int shared;              // own segments: tokens in the group's shared segment
+  int b0, b1;              // shared segments: the group's sequences
+  int group;               // own segments: the sequence's, or -1
 };
 
 __device__ __forceinline__ int seq_row(const AttendArgs& a, int b) { return a.rows != nullptr ? a.rows[b] : b; }
@@ -89,15 +93,54 @@ __device__ __forceinline__ int group_shared(const AttendArgs& a, int g) {
   row_length(a.map, seq_row(a, b0), &len);
   return shared_tokens(a.prefix_len[g], len, b1 - b0);
 }
-__device__ __forceinline__ int group_of(const AttendArgs& a, int b) {
-  const int g = sequence_of(a.group_start, a.n_groups, b);
-  return a.group_start[g] <= b && b < a.group_start[g + 1] ? g : -1;
-}
+
+// Up to 64 groups, a lane each: an own segment finds its group and the shared tokens among the lanes, where loads would wait for one
+// another (search, group, first sequence, its length).
+struct Groups {
+  int start, end, shared;
+  bool in_lanes;
+
+  __device__ __forceinline__ Groups(const AttendArgs& a, bool wanted) {
+    const int lane = threadIdx.x & 63;
+    start = end = shared = 0;
+    in_lanes = wanted && a.n_groups <= 64;
+    if (in_lanes && lane < a.n_groups) {
+      start = a.group_start[lane];
+      end = a.group_start[lane + 1];
+      shared = group_shared(a, lane);
+    }
+  }
+  // The group of sequence b, or -1; *tokens: what it shares.  (Every lane of the wavefront calls it.)
+  __device__ __forceinline__ int find(const AttendArgs& a, int b, int* tokens) const {
+    int g, first, last;
+    if (in_lanes) {
+      g = 0;
+      for (int k = 1; k < a.n_groups; ++k) g = __builtin_amdgcn_readlane(start, k) <= b ? k : g;
+      first = __shfl(start, g);
+      last = __shfl(end, g);
+      *tokens = __shfl(shared, g);
+    } else {
+      b = min(max(b, 0), a.n_seqs - 1);
+      g = sequence_of(a.group_start, a.n_groups, b);
+      first = a.group_start[g];
+      last = a.group_start[g + 1];
+      *tokens = group_shared(a, g);
+    }
+    if (first <= b && b < last) return g;
+    *tokens = 0;
+    return -1;
+  }
+};
 
 // Segment i: sequence i's own (SHARED false), or group i's shared one.  *bad: a number out of range.
+// (Every lane of the wavefront calls it; those with i out of range get an empty one.)
 template <bool SHARED>
-__device__ __forceinline__ Segment segment_of(const AttendArgs& a, int i, bool* bad) {
-  Segment s = {0, 0, 0, 0, 0, 0, 0};
+__device__ __forceinline__ Segment segment_of(const AttendArgs& a, const Groups& groups, int i, bool* bad) {
+  Segment s = {};
+  s.group = -1;
+  int tokens = 0;
+  if (!SHARED && a.n_groups > 0) s.group = groups.find(a, i, &tokens);
+  if (i >= (SHARED ? a.n_groups : a.n_seqs)) return s;
   if (SHARED) {
     const int p = group_shared(a, i);
     if (p == 0) return s;
@@ -108,6 +151,8 @@ __device__ __forceinline__ Segment segment_of(const AttendArgs& a, int i, bool* 
     s.row = seq_row(a, b0);
     s.len = p;
     s.span = p / kKeyTile;
+    s.b0 = b0;
+    s.b1 = b1;
     return s;
   }
   const int c0 = a.cu_q[i], c1 = a.cu_q[i + 1];
@@ -117,8 +162,8 @@ __device__ __forceinline__ Segment segment_of(const AttendArgs& a, int i, bool* 
   s.c0 = c0;
   s.rows = (c1 - c0) * a.G;
   if (a.n_groups > 0) {
-    const int g = group_of(a, i);
-    if (g >= 0) s.shared = group_shared(a, g); else *bad = true;
+    if (s.group < 0) *bad = true;
+    s.shared = tokens;
   }
   s.t0 = s.shared / kKeyTile;
   s.span = max(0, (s.len + kKeyTile - 1) / kKeyTile - s.t0);
@@ -152,23 +197,20 @@ __device__ __forceinline__ bool find_item(const AttendArgs& a, const AttendCut& 
   bool bad = false;
   auto row_tiles = [&](const Segment& s) { return (uint32_t)((s.rows + cut.rows - 1) / cut.rows) * (uint32_t)a.Hk; };
   auto is_partial = [&](const Segment& s, int splits) { return SHARED || splits > 1 || s.shared > 0; };
-  Segment own = {0, 0, 0, 0, 0, 0, 0};
+  Segment own = {};
+  const Groups groups(a, !SHARED && a.n_groups > 0);
   unsigned long long work = 0;
   for (int u = 0; u < per; ++u) {
-    const int i = lane * per + u;
-    if (i >= n) break;
-    own = segment_of<SHARED>(a, i, &bad);
-    work += (unsigned long long)row_tiles(own) * (uint32_t)max(own.span, 1);
+    own = segment_of<SHARED>(a, groups, lane * per + u, &bad);
+    work += (unsigned long long)row_tiles(own) * (uint32_t)max(own.span, 1);   // (no rows: 0)
   }
-  if (writes && bad) atomicOr(a.map.fault, kFaultPaged);
+  if (writes && bad) paged_fault(a.map);
   int64_t per_item = tiles_per_item(cut, wave_sum(work));
   uint32_t items, slots, upto, slots_upto;
   for (int round = 0;; ++round) {
     items = slots = 0;
     for (int u = 0; u < per; ++u) {
-      const int i = lane * per + u;
-      if (i >= n) break;
-      if (per > 1) own = segment_of<SHARED>(a, i, &bad);
+      if (per > 1) own = segment_of<SHARED>(a, groups, lane * per + u, &bad);
       const int k = splits_of(own.span, per_item);
       items += row_tiles(own) * (uint32_t)k;
       slots += is_partial(own, k) ? (uint32_t)own.rows * (uint32_t)a.Hk * (uint32_t)k : 0u;
@@ -182,12 +224,15 @@ __device__ __forceinline__ bool find_item(const AttendArgs& a, const AttendCut& 
     uint32_t at = slots_upto - slots;
     for (int u = 0; u < per; ++u) {
       const int i = lane * per + u;
-      if (i >= n) break;
-      if (per > 1) own = segment_of<SHARED>(a, i, &bad);
+      if (per > 1) own = segment_of<SHARED>(a, groups, i, &bad);
+      if (i >= n) continue;
       const int k = splits_of(own.span, per_item);
       const bool partial = is_partial(own, k);
-      pt.plan[i] = plan_entry(own, k, partial && own.rows > 0, at);
-      if (!SHARED && a.n_groups > 0) pt.group[i] = group_of(a, i);
+      // (lists that do not ascend can ask for more rows than there are: nothing of those is written or joined)
+      const bool fits = (int64_t)at + (int64_t)own.rows * a.Hk * k <= cut.cap;
+      if (partial && !fits) paged_fault(a.map);
+      pt.plan[i] = plan_entry(own, k, partial && fits && own.rows > 0, at);
+      if (!SHARED && a.n_groups > 0) pt.group[i] = own.group;
       if (partial) at += (uint32_t)own.rows * (uint32_t)a.Hk * (uint32_t)k;
     }
   }
@@ -199,10 +244,9 @@ __device__ __forceinline__ bool find_item(const AttendArgs& a, const AttendCut& 
   int from = l;
   if (per > 1) {                                           // the same among the lane's segments (per <= 64)
     const int i = l * per + lane;
-    own = Segment{0, 0, 0, 0, 0, 0, 0};
     items = slots = 0;
+    own = segment_of<SHARED>(a, groups, lane < per ? i : n, &bad);
     if (lane < per && i < n) {
-      own = segment_of<SHARED>(a, i, &bad);
       const int k = splits_of(own.span, per_item);
       items = row_tiles(own) * (uint32_t)k;
       slots = is_partial(own, k) ? (uint32_t)own.rows * (uint32_t)a.Hk * (uint32_t)k : 0u;
@@ -223,6 +267,8 @@ __device__ __forceinline__ bool find_item(const AttendArgs& a, const AttendCut& 
   s.t0 = __builtin_amdgcn_readlane(own.t0, from);
   s.span = __builtin_amdgcn_readlane(own.span, from);
   s.shared = __builtin_amdgcn_readlane(own.shared, from);
+  s.b0 = __builtin_amdgcn_readlane(own.b0, from);
+  s.b1 = __builtin_amdgcn_readlane(own.b1, from);
   out->seg = s;
   out->splits = splits_of(s.span, per_item);
   const uint32_t e = (uint32_t)item - base, tiles = (uint32_t)((s.rows + cut.rows - 1) / cut.rows);
@@ -233,11 +279,25 @@ __device__ __forceinline__ bool find_item(const AttendArgs& a, const AttendCut& 
   return out->slot < 0 || (int64_t)slot + (int64_t)s.rows * a.Hk * out->splits <= cut.cap;
 }
 
-// Keys that row r of a segment sees.
+// The fewest keys that a row of a shared segment's sequences sees, or the segment's if that is less: found by lanes over the sequences,
+// since a row's own takes a search for its sequence.
+__device__ __forceinline__ int least_limit(const AttendArgs& a, const Segment& s) {
+  uint32_t least = (uint32_t)s.len;
+  for (int b = s.b0 + (int)(threadIdx.x & 63); b < s.b1; b += 64) {
+    const int n = a.cu_q[b + 1] - a.cu_q[b];
+    int len;
+    row_length(a.map, seq_row(a, b), &len);
+    if (n > 0) least = min(least, (uint32_t)(a.causal ? max(0, len - n + 1) : len));
+  }
+  return (int)wave_min(least);
+}
+
+// Keys that row r of a segment sees.  all: as many as every row of a shared segment sees.
 template <bool SHARED>
-__device__ __forceinline__ int row_limit(const AttendArgs& a, const Segment& s, int r) {
+__device__ __forceinline__ int row_limit(const AttendArgs& a, const Segment& s, int r, int all) {
   const int i = (int)((uint32_t)r / (uint32_t)a.G);
   if (!SHARED) return a.causal ? max(0, s.len - s.rows / a.G + i + 1) : s.len;
+  if (all == s.len) return s.len;
   const int tok = s.c0 + i, b = sequence_of(a.cu_q, a.n_seqs, tok);
   int len;
   row_length(a.map, seq_row(a, b), &len);
@@ -655,6 +715,31 @@ __device__ __forceinline__ void write_row(const AttendArgs& a, const Item& it, c
   if (e0 == 0 && a.lse != nullptr) a.lse[(int64_t)hq * a.total_q + tok] = z == 0.f ? -INFINITY : (m + __log2f(z)) * kLn2;
 }
 
+__device__ __forceinline__ Source source_of(const AttendArgs& a, const Item& it) {
+  Source src;
+  src.k = (const char*)a.k + (int64_t)it.h * a.map.head;
+  src.v = (const char*)a.v + (int64_t)it.h * a.map.head;
+  src.table = a.map.table + (int64_t)it.seg.row * a.map.row_stride;
+  src.page = a.map.page;
+  src.tok = a.map.tok;
+  src.n_pages = a.map.n_pages;
+  src.ps = a.map.ps;
+  src.shift = a.map.ps_shift;
+  src.last = (it.seg.len - 1) & ~15;
+  src.d = a.d;
+  return src;
+}
+
+// Key tiles [*t0, *t1) of an item: its share of those that any of its rows sees (of a shared segment: of all).
+template <bool SHARED>
+__device__ __forceinline__ void tiles_of(const AttendArgs& a, const Item& it, int tile_rows, int* t0, int* t1) {
+  int any = it.seg.len;
+  if (!SHARED) any = row_limit<false>(a, it.seg, min(it.seg.rows, (it.tile + 1) * tile_rows) - 1, 0);
+  split_range(min(it.seg.span, max(0, (any + kKeyTile - 1) / kKeyTile - it.seg.t0)), it.splits, it.split, t0, t1);
+  *t0 += it.seg.t0;
+  *t1 += it.seg.t0;
+}
+
 // The workgroup that brings the last piece of a tile of 16 rows joins them, 16 threads a row (few pieces: the launch that joins many
 // would take longer to begin than this takes).  Pieces are written through to memory, every wavefront waits until its own are
 // there, then one thread counts the workgroup's in; whoever counts the last one reads them past its caches.  (With
@@ -729,14 +814,22 @@ __device__ __forceinline__ void split_item(const AttendArgs& a, const AttendCut&
   Item it;
   if (!find_item<SHARED>(a, cut, item, pt, &it)) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r16 = lane & 15, g = lane >> 4;
+  const Source src = source_of(a, it);
+  int t0, t1;
+  tiles_of<SHARED>(a, it, cut.rows, &t0, &t1);
+  constexpr int STEP = kWaves * B::KEYS;
+  int key = t0 * kKeyTile + wave * B::KEYS;
+  PageWindow<B::SUB, STEP> window;                         // (ahead of the queries and limits, which wait for loads of their own)
+  if (t0 < t1) window.start(src, key);
   Rows<T, D, MT> rows;
   rows.clear();
+  const int all = SHARED ? least_limit(a, it.seg) : 0;
   uint32_t least = 0x7fffffffu, most = 0;
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
     const int r = it.tile * cut.rows + 16 * mt + r16;
     const bool in = r < it.seg.rows;
-    rows.lim[mt] = in ? row_limit<SHARED>(a, it.seg, r) : 0;
+    rows.lim[mt] = in ? row_limit<SHARED>(a, it.seg, r, all) : 0;
     least = min(least, in ? (uint32_t)rows.lim[mt] : 0x7fffffffu);
     most = max(most, (uint32_t)rows.lim[mt]);
     const int i = (int)((uint32_t)r / (uint32_t)a.G);
@@ -749,28 +842,11 @@ __device__ __forceinline__ void split_item(const AttendArgs& a, const AttendCut&
   }
   least = wave_min(least);
   most = wave_max(most);
-  Source src;
-  src.k = (const char*)a.k + (int64_t)it.h * a.map.head;
-  src.v = (const char*)a.v + (int64_t)it.h * a.map.head;
-  src.table = a.map.table + (int64_t)it.seg.row * a.map.row_stride;
-  src.page = a.map.page;
-  src.tok = a.map.tok;
-  src.n_pages = a.map.n_pages;
-  src.ps = a.map.ps;
-  src.shift = a.map.ps_shift;
-  src.last = (it.seg.len - 1) & ~15;
-  src.d = a.d;
-  int t0, t1;
-  split_range(min(it.seg.span, max(0, ((int)most + kKeyTile - 1) / kKeyTile - it.seg.t0)), it.splits, it.split, &t0, &t1);
-  constexpr int STEP = kWaves * B::KEYS;
-  int key = (it.seg.t0 + t0) * kKeyTile + wave * B::KEYS;
-  const int end = min((it.seg.t0 + t1) * kKeyTile, (int)most);
+  const int end = min(t1 * kKeyTile, (int)most);
   const float scale = a.scale * kLog2e;
   bool bad = false;
   auto whole = [&](const Block<T, D>& b) { return b.ok[0] && b.ok[B::SUB - 1]; };
-  PageWindow<B::SUB, STEP> window;
   int block = 0;
-  if (key < end) window.start(src, key);
   // blocks that every row sees, the next one on its way while one is worked on
   if (key + B::KEYS <= min(end, (int)least)) {
     Block<T, D> cur, nxt;
@@ -796,7 +872,7 @@ __device__ __forceinline__ void split_item(const AttendArgs& a, const AttendCut&
     window.move(src, ++block);
   }
   if (__any(rows.odd != 0)) rows.template add_odd<false>(src, from, STEP, end, (int)most);
-  if (bad && lane == 0) atomicOr(a.map.fault, kFaultPaged);
+  if (bad && lane == 0) paged_fault(a.map);
   // the wavefronts' results are joined, 16 threads a row
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
@@ -1026,29 +1102,28 @@ __device__ __forceinline__ bool tile_step(Rows<__bf16, D, MT>& R, const TileBuff
   return true;
 }
 
-template <int D>
-struct TileLds {
-  TileBuffer<D> buf[2];
-  int lims[2][kWaves];
-};
-
 template <int D, int MT, bool PAD, bool SHARED>
 __device__ __forceinline__ void tile_item(const AttendArgs& a, const AttendCut& cut, const Partials& pt, int item, char* lds) {
   typedef Block<__bf16, D> B;
-  TileBuffer<D>* buf = ((TileLds<D>*)lds)->buf;
-  int (&lims)[2][kWaves] = ((TileLds<D>*)lds)->lims;
+  TileBuffer<D>* buf = (TileBuffer<D>*)lds;
   Item it;
   if (!find_item<SHARED>(a, cut, item, pt, &it)) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r16 = lane & 15, g = lane >> 4;
   const int row0 = it.tile * cut.rows + wave * 16 * MT;
+  const Source src = source_of(a, it);
+  int t0, t1;
+  tiles_of<SHARED>(a, it, cut.rows, &t0, &t1);
+  PageWindow<4, kKeyTile> window;                          // (ahead of the queries and limits, which wait for loads of their own)
+  if (t0 < t1) window.start(src, t0 * kKeyTile);
   Rows<__bf16, D, MT> rows;
   rows.clear();
+  const int all = SHARED ? least_limit(a, it.seg) : 0;
   uint32_t least = 0x7fffffffu, most = 0;
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
     const int r = row0 + 16 * mt + r16;
     const bool in = r < it.seg.rows;
-    rows.lim[mt] = in ? row_limit<SHARED>(a, it.seg, r) : 0;
+    rows.lim[mt] = in ? row_limit<SHARED>(a, it.seg, r, all) : 0;
     least = min(least, in ? (uint32_t)rows.lim[mt] : 0x7fffffffu);
     most = max(most, (uint32_t)rows.lim[mt]);
     const int i = (int)((uint32_t)r / (uint32_t)a.G);
@@ -1061,48 +1136,32 @@ __device__ __forceinline__ void tile_item(const AttendArgs& a, const AttendCut& 
   }
   least = wave_min(least);
   most = wave_max(most);
-  // keys that all rows of the workgroup see, that any does
-  if (lane == 0) {
-    lims[0][wave] = (int)least;
-    lims[1][wave] = (int)most;
-  }
-  __syncthreads();
-  const int all_see = __builtin_amdgcn_readfirstlane(min(min(lims[0][0], lims[0][1]), min(lims[0][2], lims[0][3])));
-  const int any_sees = __builtin_amdgcn_readfirstlane(max(max(lims[1][0], lims[1][1]), max(lims[1][2], lims[1][3])));
-  Source src;
-  src.k = (const char*)a.k + (int64_t)it.h * a.map.head;
-  src.v = (const char*)a.v + (int64_t)it.h * a.map.head;
-  src.table = a.map.table + (int64_t)it.seg.row * a.map.row_stride;
-  src.page = a.map.page;
-  src.tok = a.map.tok;
-  src.n_pages = a.map.n_pages;
-  src.ps = a.map.ps;
-  src.shift = a.map.ps_shift;
-  src.last = (it.seg.len - 1) & ~15;
-  src.d = a.d;
-  int t0, t1;
-  split_range(min(it.seg.span, max(0, (any_sees + kKeyTile - 1) / kKeyTile - it.seg.t0)), it.splits, it.split, &t0, &t1);
+  // keys that all rows of the workgroup see (an own segment's limits rise with the row)
+  const int all_see = SHARED ? all : row_limit<SHARED>(a, it.seg, it.tile * cut.rows, 0);
   const float scale = a.scale * kLog2e;
   bool bad = false;
   if (t0 < t1) {
-    PageWindow<4, kKeyTile> window;
-    window.start(src, (it.seg.t0 + t0) * kKeyTile);
-    uint32_t ok = fetch_tile<D, PAD>(buf[0], src, window, 0, (it.seg.t0 + t0) * kKeyTile);
+    uint32_t ok = fetch_tile<D, PAD>(buf[0], src, window, 0, t0 * kKeyTile);
     int t = t0;
     // tile t's pieces have landed, everybody's after the barrier, behind which nobody reads the other buffer any more: the next go there
     auto next = [&]() {
       __builtin_amdgcn_s_waitcnt(0x0070);                  // vmcnt 0, lgkmcnt 0
       __syncthreads();
       const uint32_t here = ok;
-      if (t + 1 < t1) ok = fetch_tile<D, PAD>(buf[(t + 1 - t0) & 1], src, window, t + 1 - t0, (it.seg.t0 + t + 1) * kKeyTile);
+      if (t + 1 < t1) ok = fetch_tile<D, PAD>(buf[(t + 1 - t0) & 1], src, window, t + 1 - t0, (t + 1) * kKeyTile);
       return here;
     };
     bool fetched = false;                                  // tile t has been waited for
     uint32_t here = 0;
-    const int from = (it.seg.t0 + t0) * kKeyTile;
+    const int from = t0 * kKeyTile;
+    while (most == 0 && t < t1) {                          // a wavefront without rows only fetches
+      next();
+      ++t;
+      window.move(src, t - t0);
+    }
     while (t < t1) {
       if (!fetched) here = next();
-      const int key0 = (it.seg.t0 + t) * kKeyTile;
+      const int key0 = t * kKeyTile;
       bad = bad || here != 15u;
       if (key0 < (int)most)
         tile_step<D, MT, PAD, true>(rows, buf[(t - t0) & 1], key0, here, (int)least, (int)most, a.d, scale);
@@ -1111,18 +1170,18 @@ __device__ __forceinline__ void tile_item(const AttendArgs& a, const AttendCut& 
       window.move(src, t - t0);
       // tiles that every row sees, as long as no reference has to move.  (Wavefronts may leave at different tiles: next() has the barriers,
       // one a tile.)
-      while (t < t1 && ok == 15u && (it.seg.t0 + t + 1) * kKeyTile <= all_see) {
+      while (t < t1 && ok == 15u && (t + 1) * kKeyTile <= all_see) {
         here = next();
-        fetched = !tile_step<D, MT, PAD, false>(rows, buf[(t - t0) & 1], (it.seg.t0 + t) * kKeyTile, 15u, (int)least, (int)most, a.d, scale);
+        fetched = !tile_step<D, MT, PAD, false>(rows, buf[(t - t0) & 1], t * kKeyTile, 15u, (int)least, (int)most, a.d, scale);
         if (fetched) break;
         ++t;
         window.move(src, t - t0);
       }
     }
     if (__any(rows.odd != 0))
-      rows.template add_odd<true>(src, from, B::KEYS, min((it.seg.t0 + t1) * kKeyTile, (int)most), (int)most);
+      rows.template add_odd<true>(src, from, B::KEYS, min(t1 * kKeyTile, (int)most), (int)most);
   }
-  if (bad && lane == 0) atomicOr(a.map.fault, kFaultPaged);
+  if (bad && lane == 0) paged_fault(a.map);
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
     const int r = row0 + 16 * mt + r16;
@@ -1252,7 +1311,7 @@ __device__ __forceinline__ void run_item(const AttendArgs& a, const AttendCut& c
 }
 template <int D, int KIND>
 constexpr size_t lds_of() {
-  return KIND == kNone ? 0 : KIND == kSplit ? sizeof(SplitLds<D>) : sizeof(TileLds<D>);
+  return KIND == kNone ? 0 : KIND == kSplit ? sizeof(SplitLds<D>) : 2 * sizeof(TileBuffer<D>);
 }
 
 // One launch has the items of both kinds, the shared ones first: those are the longer ones, and the own ones fill the units as they
@@ -1289,14 +1348,11 @@ hipError_t launch_kinds(const AttendArgs& a, const AttendCut& own, const AttendC
 }
 
 // The longest sequences whose pieces (of 128 keys or more) are joined within the launch.
-#ifndef ASL_JK
-#define ASL_JK 2048
-#endif
-constexpr int kJoinKeys = ASL_JK;
+constexpr int kJoinKeys = 2048;
 
 // The kind for segments of about `rows` rows.
 AttendCut cut_for(bool tiles, int64_t rows) {
-  if (tiles && rows > 16) return AttendCut{rows > 64 ? kTile2 : kTile1, 512, 4, 0};
+  if (tiles && rows > 16) return AttendCut{rows > 64 ? kTile2 : kTile1, 384, 8, 0};
   return AttendCut{kSplit, 512, 2, 0};
 }
 
