@@ -98,17 +98,22 @@ __device__ __forceinline__ int group_shared(const AttendArgs& a, int g) {
 // another (search, group, first sequence, its length).
 struct Groups {
   int start, end, shared;
-  bool in_lanes;
+  bool in_lanes, on;       // on: the groups together save enough
 
-  __device__ __forceinline__ Groups(const AttendArgs& a, bool wanted) {
+  __device__ __forceinline__ Groups(const AttendArgs& a) {
     const int lane = threadIdx.x & 63;
     start = end = shared = 0;
-    in_lanes = wanted && a.n_groups <= 64;
-    if (in_lanes && lane < a.n_groups) {
-      start = a.group_start[lane];
-      end = a.group_start[lane + 1];
-      shared = group_shared(a, lane);
+    in_lanes = a.n_groups <= 64;
+    on = false;
+    if (a.n_groups == 0) return;
+    unsigned long long saved = 0;                          // keys
+    for (int g = lane; g < a.n_groups; g += 64) {
+      start = a.group_start[g];
+      end = a.group_start[g + 1];
+      shared = group_shared(a, g);
+      saved += (unsigned long long)max(0, end - start - 1) * (uint32_t)shared;
     }
+    on = wave_sum(saved) * (unsigned long long)a.key_bytes >= kMinSaved;
   }
   // The group of sequence b, or -1; *tokens: what it shares.  (Every lane of the wavefront calls it.)
   __device__ __forceinline__ int find(const AttendArgs& a, int b, int* tokens) const {
@@ -140,6 +145,8 @@ __device__ __forceinline__ Segment segment_of(const AttendArgs& a, const Groups&
   s.group = -1;
   int tokens = 0;
   if (!SHARED && a.n_groups > 0) s.group = groups.find(a, i, &tokens);
+  if (!groups.on) tokens = 0;
+  if (SHARED && !groups.on) return s;
   if (i >= (SHARED ? a.n_groups : a.n_seqs)) return s;
   if (SHARED) {
     const int p = group_shared(a, i);
@@ -198,7 +205,7 @@ __device__ __forceinline__ bool find_item(const AttendArgs& a, const AttendCut& 
   auto row_tiles = [&](const Segment& s) { return (uint32_t)((s.rows + cut.rows - 1) / cut.rows) * (uint32_t)a.Hk; };
   auto is_partial = [&](const Segment& s, int splits) { return SHARED || splits > 1 || s.shared > 0; };
   Segment own = {};
-  const Groups groups(a, !SHARED && a.n_groups > 0);
+  const Groups groups(a);
   unsigned long long work = 0;
   for (int u = 0; u < per; ++u) {
     own = segment_of<SHARED>(a, groups, lane * per + u, &bad);
@@ -1124,6 +1131,7 @@ __device__ __forceinline__ void tile_item(const AttendArgs& a, const AttendCut& 
     const int r = row0 + 16 * mt + r16;
     const bool in = r < it.seg.rows;
     rows.lim[mt] = in ? row_limit<SHARED>(a, it.seg, r, all) : 0;
+    if (!in) rows.m[mt] = 0.f;                             // rows that are not there have logits 0: no reference to move for them
     least = min(least, in ? (uint32_t)rows.lim[mt] : 0x7fffffffu);
     most = max(most, (uint32_t)rows.lim[mt]);
     const int i = (int)((uint32_t)r / (uint32_t)a.G);
@@ -1350,9 +1358,15 @@ hipError_t launch_kinds(const AttendArgs& a, const AttendCut& own, const AttendC
 // The longest sequences whose pieces (of 128 keys or more) are joined within the launch.
 constexpr int kJoinKeys = 2048;
 
-// The kind for segments of about `rows` rows.
-AttendCut cut_for(bool tiles, int64_t rows) {
-  if (tiles && rows > 16) return AttendCut{rows > 64 ? kTile2 : kTile1, 384, 8, 0};
+// The kind for `segments` segments of up to `rows` rows and `keys` keys.  A split item has all four wavefronts' loads on their way and
+// needs no barrier, a tile reads its keys once for 64 or 128 rows: calls of little work are bound by latency and are split
+// (32 query heads, 8 KV heads, d = 128; us, split and tiles: 32 rows 512 keys 11, 23; 128 rows 512 keys 11, 27; 64 rows 4096 keys 18,
+// 25), others are not (8 sequences, 4096 keys: 32 rows 34, 36, 64 rows 50, 38; 32768 keys: 32 rows 225, 208, 64 rows 357, 214).
+// Tiles of 64 rows up to 64 (8 sequences, 32768 keys, 64 rows 214 us, with tiles of 128 228).
+constexpr double kSplitWork = 524288.;     // tiles of 16 rows x keys x KV heads
+AttendCut cut_for(bool tiles, int64_t rows, int64_t keys, int64_t segments, int Hk) {
+  const double work = (double)((rows + 15) / 16) * (double)keys * (double)segments * Hk;
+  if (tiles && rows > 16 && work >= kSplitWork) return AttendCut{rows > 64 ? kTile2 : kTile1, 384, 8, 0};
   return AttendCut{kSplit, 512, 2, 0};
 }
 
@@ -1362,7 +1376,8 @@ hipError_t launch_d(const PagedWorkspace& ws, const AttendArgs& args, hipStream_
   constexpr bool kTiles = sizeof(T) == 2 && D <= 128;
   const int64_t rows = (int64_t)a.total_q * a.G;           // of a KV head
   const int64_t most = (int64_t)a.max_q_len * a.G < rows ? (int64_t)a.max_q_len * a.G : rows;
-  AttendCut own = cut_for(kTiles, most), shared = cut_for(kTiles, a.n_groups > 0 ? rows / a.n_groups : 0);
+  AttendCut own = cut_for(kTiles, most, a.max_kv_len, a.n_seqs, a.Hk);
+  AttendCut shared = cut_for(kTiles, a.n_groups > 0 ? rows / a.n_groups : 0, a.max_kv_len, a.n_groups, a.Hk);
   const int64_t room = ws.part_rows;
   shared.cap = max_partials(shared, rows, a.Hk);
   // a sequence whose own rows fill a tile gains nothing; and every row of a group is joined from two parts, for which there has to be
@@ -1380,7 +1395,7 @@ hipError_t launch_d(const PagedWorkspace& ws, const AttendArgs& args, hipStream_
   po.plan = ws.plan;
   po.group = ws.group;
   ps.arrived = nullptr;
-  // Few pieces of few rows are joined by the workgroup that brings the last one.
+  // Few pieces are joined by the workgroup that brings the last one.
   po.arrived = a.n_groups == 0 && own.rows == kSplit && a.max_kv_len <= kJoinKeys ? ws.arrived + shared.cap : nullptr;
   hipError_t e = hipErrorInvalidValue;
   const int ks = a.n_groups > 0 ? shared.rows : kNone;
@@ -1388,7 +1403,8 @@ hipError_t launch_d(const PagedWorkspace& ws, const AttendArgs& args, hipStream_
     if (ks == kNone) {
       e = own.rows == kTile2   ? launch_kinds<T, D, kTile2, kNone, true>(a, own, shared, po, ps, st)
           : own.rows == kTile1 ? launch_kinds<T, D, kTile1, kNone, true>(a, own, shared, po, ps, st)
-                               : launch_kinds<T, D, kSplit, kNone, true>(a, own, shared, po, ps, st);
+          : most <= kSplit     ? launch_kinds<T, D, kSplit, kNone, true>(a, own, shared, po, ps, st)
+                               : launch_kinds<T, D, kSplit, kNone, false>(a, own, shared, po, ps, st);
     } else if (own.rows == kTile1) {
       e = ks == kTile2   ? launch_kinds<T, D, kTile1, kTile2, true>(a, own, shared, po, ps, st)
           : ks == kTile1 ? launch_kinds<T, D, kTile1, kTile1, true>(a, own, shared, po, ps, st)
@@ -1396,7 +1412,7 @@ hipError_t launch_d(const PagedWorkspace& ws, const AttendArgs& args, hipStream_
     } else {
       e = ks == kTile2   ? launch_kinds<T, D, kSplit, kTile2, true>(a, own, shared, po, ps, st)
           : ks == kTile1 ? launch_kinds<T, D, kSplit, kTile1, true>(a, own, shared, po, ps, st)
-                         : launch_kinds<T, D, kSplit, kSplit, true>(a, own, shared, po, ps, st);
+                         : launch_kinds<T, D, kSplit, kSplit, false>(a, own, shared, po, ps, st);
     }
   } else if (ks == kNone) {
     e = most <= kSplit ? launch_kinds<T, D, kSplit, kNone, true>(a, own, shared, po, ps, st)

@@ -44,12 +44,18 @@ ASL_HD int64_t max_items(const AttendCut& c, int64_t rows, int64_t segments, int
 // Rows of partial results that such a launch can leave at most.
 ASL_HD int64_t max_partials(const AttendCut& c, int64_t rows, int Hk) { return rows * Hk + (int64_t)c.target * c.rows; }
 
-// The shared tokens that are worth a segment of their own: whole key tiles; none for a group of one.
+// Tokens of a group that a segment of its own takes: whole key tiles of what is stated and there; none for a group of one.
 constexpr int kMinShared = 128;
 ASL_HD int shared_tokens(int stated, int first_len, int members) {
   if (members < 2) return 0;
   const int p = (stated < first_len ? stated : first_len) & ~(kKeyTile - 1);
   return p < kMinShared ? 0 : p;
 }
+
+// Bytes of K and V that a call's groups have to save for their prefixes to be read apart; read by each sequence they come from the
+// caches, and nothing has to be joined (d = 128; us, apart and by each: 32 query heads, 8 KV heads, one group of 64, prefix 512
+// (132 MB) 29, 20, 1024 (264 MB) 30, 29, 2090 32, 74; 8 groups of 6, 1024 (168 MB) 37, 39; 28 heads, 4 KV heads, 8 groups of 6,
+// 1024 (84 MB) 34, 27, 2090 (171 MB) 37, 45).
+constexpr unsigned long long kMinSaved = 128ull << 20;
 
 }  // namespace asl

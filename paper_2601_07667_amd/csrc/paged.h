@@ -71,6 +71,7 @@ struct AttendArgs {
   int64_t qt, qh, ot, oh;  // strides of q and out in elements
   int32_t Hq, Hk, G, d;
   int32_t n_seqs, total_q, max_q_len, max_kv_len, n_groups, causal;
+  int32_t key_bytes;       // of K and V of a token
   float scale;
 };
 hipError_t launch_attend(const PagedWorkspace& ws, const AttendArgs& a, int dtype, hipStream_t st);

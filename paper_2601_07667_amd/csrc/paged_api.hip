@@ -251,6 +251,7 @@ asl_status asl_paged_attention(asl_ctx* ctx, const asl_pages* p, const asl_attn*
   a.Hk = p->n_kv_heads;
   a.G = a.Hq / a.Hk;
   a.d = p->head_dim;
+  a.key_bytes = 2 * p->head_dim * elem_bytes(p->dtype) * p->n_kv_heads;
   a.n_seqs = at->n_seqs;
   a.total_q = at->total_q;
   a.max_q_len = at->max_q_len;
