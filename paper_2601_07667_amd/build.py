@@ -11,7 +11,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libasl.so")
 SOURCES = ["api.hip", "score.hip", "pool.hip", "rank.hip", "rankvar.hip", "select.hip", "gather.hip", "tail.hip",
-           "paged_api.hip", "paged.hip", "attend.hip"]
+           "paged_api.hip", "paged.hip", "attend.hip", "attend_64.hip", "attend_128.hip"]
 # packed-fp32 instructions are switched off for all device code
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -20,11 +20,11 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hi
 
 # score.hip never produces NaNs from finite inputs (masked logits are -inf, never inf - inf); telling
 # the compiler so lets max() compile to bare v_max_f32 / v_max3_f32 without NaN-quieting moves.
-# attend.hip takes NaN as they come, so without the first of the two.
+# The attention kernels take NaN as they come, so without the first of the two.
 # MFMA results are kept in ordinary VGPRs: the softmax arithmetic reads every accumulator, and
 # copies out of accumulation registers would cost one vector instruction per element.
 PER_FILE_FLAGS = {"score.hip": ["-fno-honor-nans", "-mllvm", "-amdgpu-mfma-vgpr-form"],
-                  "attend.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+                  **{f: ["-mllvm", "-amdgpu-mfma-vgpr-form"] for f in ("attend.hip", "attend_64.hip", "attend_128.hip")}}
 
 
 def _hipcc() -> str:

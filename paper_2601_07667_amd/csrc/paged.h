@@ -75,5 +75,7 @@ struct AttendArgs {
   float scale;
 };
 hipError_t launch_attend(const PagedWorkspace& ws, const AttendArgs& a, int dtype, hipStream_t st);
+hipError_t launch_attend_bf16_64(const PagedWorkspace& ws, const AttendArgs& a, hipStream_t st);
+hipError_t launch_attend_bf16_128(const PagedWorkspace& ws, const AttendArgs& a, hipStream_t st);
 
 }  // namespace asl

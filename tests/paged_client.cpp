@@ -5,6 +5,7 @@
 #include <string>
 #include <vector>
 
+#include "attend_plan.h"
 #include "paged_check.h"
 
 static long long num() {
@@ -63,6 +64,42 @@ int main() {
       int L = -7;
       const bool ok = asl::row_length(m, r, &L);
       std::printf("%d %d %lld\n", ok ? 1 : 0, L, (long long)asl::token_offset(m, r, pos));
+    } else if (!std::strcmp(what, "cut")) {
+      // rows of a tile, target, least tiles, KV heads, the segments' rows and spans: whether every share is whole, the items and partial
+      // rows that the cut gives and the most that a launch makes room for
+      asl::AttendCut c = {};
+      c.rows = (int)num(); c.target = (int)num(); c.min_tiles = (int)num();
+      const int Hk = (int)num(), n = (int)num();
+      std::vector<long long> rows(n), span(n);
+      unsigned long long work = 0;
+      long long all_rows = 0;
+      for (int i = 0; i < n; ++i) {
+        rows[i] = num();
+        span[i] = num();
+        all_rows += rows[i];
+        work += (unsigned long long)((rows[i] + c.rows - 1) / c.rows) * Hk * (span[i] < 1 ? 1 : span[i]);
+      }
+      const long long per = asl::tiles_per_item(c, work);
+      long long items = 0, partial = 0;
+      bool ok = true;
+      for (int i = 0; i < n; ++i) {
+        const int k = asl::splits_of((int)span[i], per);
+        items += (rows[i] + c.rows - 1) / c.rows * Hk * k;
+        partial += rows[i] * Hk * k;
+        int at = 0;
+        for (int s = 0; s < k; ++s) {
+          int t0, t1;
+          asl::split_range((int)span[i], k, s, &t0, &t1);
+          ok = ok && t0 == at && t1 >= t0 && t1 - t0 <= per;
+          at = t1;
+        }
+        ok = ok && at == span[i];
+      }
+      std::printf("%d %lld %lld %lld %lld\n", ok ? 1 : 0, items, (long long)asl::max_items(c, all_rows, n, Hk), partial,
+                  (long long)asl::max_partials(c, all_rows, Hk));
+    } else if (!std::strcmp(what, "shared")) {
+      const int stated = (int)num(), first = (int)num(), members = (int)num();
+      std::printf("%d\n", asl::shared_tokens(stated, first, members));
     } else if (!std::strcmp(what, "seq")) {
       const int n = (int)num();
       std::vector<int32_t> cu(n + 1);

@@ -789,3 +789,32 @@ def test_attention_logits_that_rise_by_leaps(ctx, gpu_device, shared, n_q, d):
     out, lse = _attend(ctx, c, q, n, G, groups=[(2, 640)] if shared else None)
     _check(out, lse, _oracle(c, q, n), d, L, "bf16", "leaps")
     assert ctx.asl_device_fault() == 0
+
+
+def test_the_example_from_prefill_to_decoding(gpu_device):
+    """examples/serve_pruned.py: its attention and normalisers against the oracle, the scores it got from them against the
+    scoring's own, its decoding steps over what it kept."""
+    import importlib.util
+    import os
+    import gpu_util as gu
+    from oracle import asl_oracle as orc
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "serve_pruned.py")
+    spec = importlib.util.spec_from_file_location("serve_pruned", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    Hq, Hk, d, N, W, n = 8, 2, 64, 1000, 16, 3
+    r = example.run(Hq=Hq, Hk=Hk, d=d, N=N, W=W, budget=200, continuations=n, steps=6, page_size=16)
+    assert r["fault"] == 0 and r["left"] == 0 and r["lengths"] == [0, 200] + [206] * n
+    f = lambda x: x.double().cpu().numpy()
+    q, k, v = f(r["q"]), f(r["k"]), f(r["v"])
+    _check(r["out"], r["lse"], po.attention(q, k, v, d ** -0.5, True), d, N, "bf16", "window")
+    ref = orc.get_ranks(q.transpose(1, 0, 2), k, v, W, 7, 200)
+    gu.assert_scores_close(f(r["scores"][:Hk]), ref["P"], "scores by the attention's normalisers")
+    idx = r["idx"].cpu().numpy()
+    for b in range(n):
+        for t, ((q1, _, _), out) in enumerate(zip(r["history"], r["outputs"])):
+            K, V = (np.stack([np.concatenate([x[h][idx[h]], np.stack([f(step[1 + j][b])[h] for step in r["history"][:t + 1]])])
+                              for h in range(Hk)]) for j, x in enumerate((k, v)))
+            ref = po.attention(f(q1[b:b + 1]), K, V, d ** -0.5, True)
+            tol, _ = _bounds(d, K.shape[1], "bf16", ref)
+            assert np.all(np.abs(f(out[b:b + 1]) - ref[0]) <= tol), (b, t)

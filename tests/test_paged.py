@@ -125,6 +125,27 @@ def test_the_sequence_of_a_token(client):
         assert w is None or got == w
 
 
+def test_the_cut_of_an_attention_call(client):
+    """Every key tile of a segment falls to one item, and no cut gives more items or partial rows than a launch makes room for."""
+    rng = random.Random(5)
+    lines = []
+    for _ in range(400):
+        n, Hk = rng.choice([1, 2, 5, 64, 300]), rng.choice([1, 2, 4, 8])
+        longest = rng.choice([1, 3, 40, 2000, 16384])
+        segments = [(rng.choice([0, 1, 4, 7, 16, 17, 128, 129, 1000]), rng.randint(0, longest)) for _ in range(n)]
+        lines.append("cut %d %d %d %d %d %s" % (rng.choice([16, 64, 128]), rng.choice([1, 384, 512]), rng.choice([1, 2, 8]), Hk, n,
+                                                " ".join("%d %d" % s for s in segments)))
+    for line, got in zip(lines, client(lines)):
+        ok, items, most_items, partial, most_partial = map(int, got.split())
+        assert ok and items <= most_items and partial <= most_partial, (line, got)
+
+
+def test_shared_tokens(client):
+    for (stated, first, members), want in {(1000, 1000, 2): 960, (1000, 500, 2): 448, (10 ** 9, 191, 3): 128, (127, 1000, 9): 0,
+                                           (1000, 1000, 1): 0, (-5, 1000, 4): 0, (1000, 0, 4): 0, (128, 128, 2): 128}.items():
+        assert client(["shared %d %d %d" % (stated, first, members)]) == [str(want)]
+
+
 # ------------------------------------------------------------------------------------------------- the oracle's pins
 def test_oracle_attention_closed_forms():
     rng = np.random.default_rng(0)
