@@ -1365,9 +1365,12 @@ constexpr int kJoinKeys = 2048;
 // 25), others are not (8 sequences, 4096 keys: 32 rows 34, 36, 64 rows 50, 38; 32768 keys: 32 rows 225, 208, 64 rows 357, 214).
 // Tiles of 64 rows up to 64 (8 sequences, 32768 keys, 64 rows 214 us, with tiles of 128 228).
 constexpr double kSplitWork = 524288.;     // tiles of 16 rows x keys x KV heads
-AttendCut cut_for(bool tiles, int64_t rows, int64_t keys, int64_t segments, int Hk) {
+// Pieces of tiles: about 512 of own keys, two a compute unit (one chunk of 512 tokens over 4096 keys 63 us, with 384 74), 384 of
+// shared ones, beside which there are others (shared prompt of 32768 keys 88 us, with 512 93.5); at least 8 key tiles each
+// (shared drafts 36 us, with 4 47).
+AttendCut cut_for(bool tiles, int64_t rows, int64_t keys, int64_t segments, int Hk, bool shared) {
   const double work = (double)((rows + 15) / 16) * (double)keys * (double)segments * Hk;
-  if (tiles && rows > 16 && work >= kSplitWork) return AttendCut{rows > 64 ? kTile2 : kTile1, 384, 8, 0};
+  if (tiles && rows > 16 && work >= kSplitWork) return AttendCut{rows > 64 ? kTile2 : kTile1, shared ? 384 : 512, 8, 0};
   return AttendCut{kSplit, 512, 2, 0};
 }
 
@@ -1377,8 +1380,8 @@ hipError_t launch_d(const PagedWorkspace& ws, const AttendArgs& args, hipStream_
   constexpr bool kTiles = sizeof(T) == 2 && D <= 128;
   const int64_t rows = (int64_t)a.total_q * a.G;           // of a KV head
   const int64_t most = (int64_t)a.max_q_len * a.G < rows ? (int64_t)a.max_q_len * a.G : rows;
-  AttendCut own = cut_for(kTiles, most, a.max_kv_len, a.n_seqs, a.Hk);
-  AttendCut shared = cut_for(kTiles, a.n_groups > 0 ? rows / a.n_groups : 0, a.max_kv_len, a.n_groups, a.Hk);
+  AttendCut own = cut_for(kTiles, most, a.max_kv_len, a.n_seqs, a.Hk, false);
+  AttendCut shared = cut_for(kTiles, a.n_groups > 0 ? rows / a.n_groups : 0, a.max_kv_len, a.n_groups, a.Hk, true);
   const int64_t room = ws.part_rows;
   shared.cap = max_partials(shared, rows, a.Hk);
   // a sequence whose own rows fill a tile gains nothing; and every row of a group is joined from two parts, for which there has to be
