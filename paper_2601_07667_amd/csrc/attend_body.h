@@ -38,9 +38,10 @@ constexpr float kLn2 = 0.6931471805599453f;
 // A row's reference moves when a logit exceeds it by more than this (in units of log 2): probabilities stay below 2^8 and most
 // blocks need no maximum over lanes and no rescaling.
 constexpr float kSlack = 8.f;
-// The same where a row's reference cannot move in place: probabilities up to 2^60 lose nothing in fp32 and bf16 (a result is a
-// quotient of two such sums), and only a row whose first tile was that much lower than a later one needs the step that moves it.
-constexpr float kWideSlack = 60.f;
+// The same where a row's reference cannot move in place: probabilities up to 2^24 lose nothing in fp32 and bf16 (a result is a
+// quotient of two such sums; it is values beyond 2^100 whose sums overflow), and only rows whose first tile was that much lower
+// than a later one need the step that moves it.
+constexpr float kWideSlack = 24.f;
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -1384,9 +1385,10 @@ hipError_t launch_d(const PagedWorkspace& ws, const AttendArgs& args, hipStream_
   AttendCut shared = cut_for(kTiles, a.n_groups > 0 ? rows / a.n_groups : 0, a.max_kv_len, a.n_groups, a.Hk, true);
   const int64_t room = ws.part_rows;
   shared.cap = max_partials(shared, rows, a.Hk);
-  // a sequence whose own rows fill a tile gains nothing; and every row of a group is joined from two parts, for which there has to be
-  // room
-  if (a.n_groups > 0 && (own.rows == kTile2 || shared.cap + rows * a.Hk > room)) a.n_groups = 0;
+  // a sequence whose own rows fill a tile gains nothing, and groups cannot save more than all sequences' keys but one each (kMinSaved);
+  // every row of a group is joined from two parts, for which there has to be room
+  const double most_saved = (double)(a.n_seqs - a.n_groups) * (double)a.max_kv_len * (double)a.key_bytes;
+  if (a.n_groups > 0 && (own.rows == kTile2 || most_saved < (double)kMinSaved || shared.cap + rows * a.Hk > room)) a.n_groups = 0;
   if (a.n_groups == 0) shared.cap = 0;
   own.cap = room - shared.cap;
   Partials po, ps;
