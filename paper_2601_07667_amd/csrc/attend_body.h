@@ -184,6 +184,7 @@ struct Partials {
   float2* mz;              // [cap]
   int4* plan;              // of the segments
   int32_t* group;          // [n_seqs] own segments: the sequence's group or -1
+  int32_t* cut;            // own segments: whether any row is in pieces
   uint32_t* arrived;       // [cap] zeros: pieces of a row tile that are there, counted at its first slot; null: a launch joins them
 };
 
@@ -208,12 +209,23 @@ __device__ __forceinline__ bool find_item(const AttendArgs& a, const AttendCut& 
   auto is_partial = [&](const Segment& s, int splits) { return SHARED || splits > 1 || s.shared > 0; };
   Segment own = {};
   const Groups groups(a);
-  unsigned long long work = 0;
+  unsigned long long work = 0, all_rows = 0;
   for (int u = 0; u < per; ++u) {
     own = segment_of<SHARED>(a, groups, lane * per + u, &bad);
+    all_rows += (unsigned long long)own.rows;
     work += (unsigned long long)row_tiles(own) * (uint32_t)max(own.span, 1);   // (no rows: 0)
   }
-  if (writes && bad) paged_fault(a.map);
+  // Lists that do not ascend can have a token in several sequences: more rows than the launch, the pieces' room and their counts are
+  // made for.  Nothing is done then.
+  const bool sound = wave_sum(all_rows) <= (unsigned long long)a.total_q * (unsigned long long)a.G;
+  if (writes && (bad || !sound)) paged_fault(a.map);
+  if (!sound) {
+    if (writes) {
+      for (int i = lane; i < n; i += 64) pt.plan[i] = make_int4(0, 0, 0, 0);
+      if (!SHARED && lane == 0) *pt.cut = 0;
+    }
+    return false;
+  }
   int64_t per_item = tiles_per_item(cut, wave_sum(work));
   uint32_t items, slots, upto, slots_upto;
   for (int round = 0;; ++round) {
@@ -230,6 +242,7 @@ __device__ __forceinline__ bool find_item(const AttendArgs& a, const AttendCut& 
     per_item = int64_t(1) << 40;                           // no room for the pieces: whole spans
   }
   if (writes) {
+    if (!SHARED && lane == 63) *pt.cut = slots_upto != 0 ? 1 : 0;
     uint32_t at = slots_upto - slots;
     for (int u = 0; u < per; ++u) {
       const int i = lane * per + u;
@@ -237,10 +250,7 @@ __device__ __forceinline__ bool find_item(const AttendArgs& a, const AttendCut& 
       if (i >= n) continue;
       const int k = splits_of(own.span, per_item);
       const bool partial = is_partial(own, k);
-      // (lists that do not ascend can ask for more rows than there are: nothing of those is written or joined)
-      const bool fits = (int64_t)at + (int64_t)own.rows * a.Hk * k <= cut.cap;
-      if (partial && !fits) paged_fault(a.map);
-      pt.plan[i] = plan_entry(own, k, partial && fits && own.rows > 0, at);
+      pt.plan[i] = plan_entry(own, k, partial && own.rows > 0, at);
       if (!SHARED && a.n_groups > 0) pt.group[i] = own.group;
       if (partial) at += (uint32_t)own.rows * (uint32_t)a.Hk * (uint32_t)k;
     }
@@ -1210,16 +1220,12 @@ __device__ __forceinline__ void tile_item(const AttendArgs& a, const AttendCut& 
 // with a running maximum of their references; then lanes and wavefronts are joined.  One pass: what it costs is the latency of the
 // loads that depend on each other (the sequence, its plan, the pieces).
 template <typename T, int D, int NW>
-__global__ void __launch_bounds__(NW > kWaves ? NW * 64 : kThreads) attend_join_kernel(AttendArgs a, Partials own, Partials shared) {
+__device__ __forceinline__ void join_row(const AttendArgs& a, const Partials& own, const Partials& shared, int64_t row, float* so_, float* sm,
+                                         float* sz) {
   constexpr int LPP = D / 4;                               // lanes of a piece, four elements each
   constexpr int PPW = 64 / LPP;                            // pieces that a wavefront takes at once
-  constexpr int WAVES = NW > kWaves ? NW : kWaves;
-  constexpr int RPB = WAVES / NW;
-  __shared__ __attribute__((aligned(16))) float so[WAVES][D];
-  __shared__ float sm[WAVES], sz[WAVES];
+  float (*so)[D] = (float (*)[D])so_;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t row = (int64_t)blockIdx.x * RPB + wave / NW;
-  if (row >= (int64_t)a.total_q * a.Hq) return;            // all of a workgroup, or it has a row for each wavefront and no barrier
   const int tok = (int)(row / a.Hq), hq = (int)(row - (int64_t)tok * a.Hq), h = hq / a.G;
   const int b = sequence_by_wave(a.cu_q, a.n_seqs, tok);
   const int4 p = own.plan[b];
@@ -1307,6 +1313,23 @@ __global__ void __launch_bounds__(NW > kWaves ? NW * 64 : kThreads) attend_join_
         Out{(T)(acc[0] * by), (T)(acc[1] * by), (T)(acc[2] * by), (T)(acc[3] * by)};
   }
   if (lane == 0 && a.lse != nullptr) a.lse[(int64_t)hq * a.total_q + tok] = z == 0.f ? -INFINITY : (m + __log2f(z)) * kLn2;
+}
+
+// The rows in turn; nothing where no row was cut.  With several wavefronts a row there is a workgroup for each row (a barrier in the way of
+// a second one).
+template <typename T, int D, int NW>
+__global__ void __launch_bounds__(NW > kWaves ? NW * 64 : kThreads) attend_join_kernel(AttendArgs a, Partials own, Partials shared) {
+  constexpr int WAVES = NW > kWaves ? NW : kWaves;
+  __shared__ __attribute__((aligned(16))) float so[WAVES * D];
+  __shared__ float sm[WAVES], sz[WAVES];
+  if (*own.cut == 0) return;
+  if constexpr (NW > 1) {
+    static_assert(NW == WAVES, "a workgroup has one row");
+    join_row<T, D, NW>(a, own, shared, (int64_t)blockIdx.x, so, sm, sz);
+  } else {
+    for (int64_t row = (int64_t)blockIdx.x * WAVES + (threadIdx.x >> 6); row < (int64_t)a.total_q * a.Hq; row += (int64_t)gridDim.x * WAVES)
+      join_row<T, D, 1>(a, own, shared, row, so, sm, sz);
+  }
 }
 
 // ------------------------------------------------------------------------------------------------------------------
@@ -1400,6 +1423,7 @@ hipError_t launch_d(const PagedWorkspace& ws, const AttendArgs& args, hipStream_
   po.mz = ws.part_mz + shared.cap;
   po.plan = ws.plan;
   po.group = ws.group;
+  po.cut = ps.cut = ws.cut;
   ps.arrived = nullptr;
   // Few pieces are joined by the workgroup that brings the last one.
   po.arrived = a.n_groups == 0 && own.rows == kSplit && a.max_kv_len <= kJoinKeys ? ws.arrived + shared.cap : nullptr;
@@ -1434,8 +1458,8 @@ hipError_t launch_d(const PagedWorkspace& ws, const AttendArgs& args, hipStream_
   else if (out_rows <= 2048)
     hipLaunchKernelGGL((attend_join_kernel<T, D, kWaves>), dim3((unsigned)out_rows), dim3(kThreads), 0, st, a, po, ps);
   else
-    hipLaunchKernelGGL((attend_join_kernel<T, D, 1>), dim3((unsigned)((out_rows + kWaves - 1) / kWaves)), dim3(kThreads), 0, st,
-                       a, po, ps);
+    hipLaunchKernelGGL((attend_join_kernel<T, D, 1>), dim3((unsigned)(out_rows < 4096 * kWaves ? (out_rows + kWaves - 1) / kWaves : 4096)),
+                       dim3(kThreads), 0, st, a, po, ps);
   return hipGetLastError();
 }
 

@@ -18,6 +18,7 @@ struct PagedWorkspace {
   int64_t part_rows;
   int4* plan;              // [2][kPagedMaxSeqs] how sequences and groups were cut
   int32_t* group;          // [kPagedMaxSeqs] the sequences' groups
+  int32_t* cut;            // [1] whether any row is in pieces
   int4* forks;             // [max_seqs] what the bookkeeping launch of a fork leaves for the copying one
   int32_t* fresh;          // [kMaxFresh] the free pages that a call takes, in order
   uint32_t* fault;         // [1]

@@ -57,7 +57,8 @@ asl_status asl_paged_reserve(asl_ctx* ctx, int32_t max_seqs, int32_t max_query_r
   const size_t fault = take(sizeof(uint32_t)), forks = take((size_t)max_seqs * sizeof(int4)),
                fresh = take((size_t)asl::kMaxFresh * sizeof(int32_t)),
                plan = take((size_t)2 * asl::kPagedMaxSeqs * sizeof(int4)),
-               group = take((size_t)asl::kPagedMaxSeqs * sizeof(int32_t));
+               group = take((size_t)asl::kPagedMaxSeqs * sizeof(int32_t)),
+               cut = take(sizeof(int32_t));
   // attention: room for every row twice (its own and its shared keys; not for the largest calls, which have no need to share),
   // and for the pieces that long spans are cut into
   w.part_rows = 2 * (int64_t)(max_query_rows < 131072 ? max_query_rows : 131072) + asl::kCutRows;
@@ -76,6 +77,7 @@ asl_status asl_paged_reserve(asl_ctx* ctx, int32_t max_seqs, int32_t max_query_r
   w.fresh = (int32_t*)(base + fresh);
   w.plan = (int4*)(base + plan);
   w.group = (int32_t*)(base + group);
+  w.cut = (int32_t*)(base + cut);
   w.part = (float*)(base + part);
   w.part_mz = (float2*)(base + part_mz);
   w.arrived = (uint32_t*)(base + arrived);

@@ -818,3 +818,27 @@ def test_the_example_from_prefill_to_decoding(gpu_device):
             ref = po.attention(f(q1[b:b + 1]), K, V, d ** -0.5, True)
             tol, _ = _bounds(d, K.shape[1], "bf16", ref)
             assert np.all(np.abs(f(out[b:b + 1]) - ref[0]) <= tol), (b, t)
+
+
+@pytest.mark.parametrize("kv", [600, 5000])
+def test_lists_that_do_not_ascend_leave_no_trace(ctx, gpu_device, kv):
+    """cu_q or group_start out of order: the fault word's bit 1, and the calls behind it (joined in the launch, or apart) as ever."""
+    torch = _torch()
+    c = Cache(gpu_device, [kv] * 8, 2, 64, 64, "bf16", 12)
+    q = _queries(8, 8, 64, "bf16", gpu_device, 13)
+    want, want_l = _attend(ctx, c, q, [1] * 8, 8)
+    out, lse = torch.empty_like(want), torch.empty_like(want_l)
+    for cu in ([0, 8, 0, 8, 0, 8, 0, 8, 8], [0, 5, 1, 7, 2, 8, 3, 8, 8], [-4, 1, 2, 3, 4, 5, 6, 7, 9], [8, 7, 6, 5, 4, 3, 2, 1, 0]):
+        a = asl.make_attn(8, 8, 8, kv)
+        ctx.asl_paged_attention(c.desc(8), a, q, c.k, c.v, c.table, c.kv_len, _ints(cu, gpu_device), out, lse=lse)
+        assert ctx.asl_device_fault() == 2
+        got, got_l = _attend(ctx, c, q, [1] * 8, 8)
+        assert torch.equal(got, want) and torch.equal(got_l, want_l)
+    for gs in ([0, 8, 0, 8], [3, 1, 9, 8], [-1, 2, 4, 8], [0, 2, 5, 100]):
+        a = asl.make_attn(8, 8, 1, 10 ** 8, n_groups=3)
+        ctx.asl_paged_attention(c.desc(8), a, q, c.k, c.v, c.table, c.kv_len, _ints(range(9), gpu_device), out, lse=lse,
+                                group_start=_ints(gs, gpu_device), prefix_len=_ints([kv] * 3, gpu_device))
+        ctx.asl_device_fault()
+        got, got_l = _attend(ctx, c, q, [1] * 8, 8)
+        assert torch.equal(got, want) and torch.equal(got_l, want_l)
+    assert ctx.asl_device_fault() == 0
