@@ -291,7 +291,9 @@ class Asl:
     def asl_pages_write(self, pages: AslPages, k, v, rows, cu, n: int, total: int, table, kv_len, k_pages, v_pages,
                         idx=None) -> None:
         """k, v: [Hk, n_src, d] of any strides (d contiguous); idx: [1 or Hk, total]."""
-        src = AslRows(k.shape[1], 0 if idx is None else idx.shape[0], k.stride(0), k.stride(1), v.stride(0), v.stride(1))
+        kh, kt, _ = k.stride()
+        vh, vt, _ = v.stride()
+        src = AslRows(k.shape[1], 0 if idx is None else idx.shape[0], kh, kt, vh, vt)
         self._check(self.lib.asl_pages_write(self.h, C.byref(pages), C.byref(src), _ptr(k), _ptr(v), _ptr(rows), _ptr(cu), n,
                                              total, _ptr(idx), _ptr(table), _ptr(kv_len), _ptr(k_pages), _ptr(v_pages),
                                              _stream()))

@@ -100,6 +100,7 @@ asl_status asl_pages_grow(asl_ctx* ctx, const asl_pages* p, const int32_t* rows,
   asl_status st = check_pages(ctx, p, table, kv_len, &m);
   if (st == ASL_OK) st = check_count(ctx, n);
   if (st != ASL_OK) return st;
+  if (n == 0) return ASL_OK;
   if (!rows || !add || !refs) return fail(ctx, ASL_EINVAL, "null tensor pointer");
   DeviceGuard guard(ctx->device);
   if (guard.err != hipSuccess) return hip_fail(ctx, guard.err, "set device");
@@ -115,10 +116,10 @@ asl_status asl_pages_fork(asl_ctx* ctx, const asl_pages* p, void* const* k_ptrs,
   asl_status st = check_pages(ctx, p, table, kv_len, &a.map);
   if (st == ASL_OK) st = check_count(ctx, n);
   if (st != ASL_OK) return st;
-  if (!parents || !children || !refs) return fail(ctx, ASL_EINVAL, "null tensor pointer");
   if (n_layers < 0) return fail(ctx, ASL_EINVAL, "n_layers must be >= 0");
   if (n_layers > 16384) return fail(ctx, ASL_EUNSUPPORTED, "more than 16384 layers per call");
-  if (n_layers > 0 && (!k_ptrs || !v_ptrs)) return fail(ctx, ASL_EINVAL, "null tensor pointer");
+  if (n == 0) return ASL_OK;
+  if (!parents || !children || !refs || (n_layers > 0 && (!k_ptrs || !v_ptrs))) return fail(ctx, ASL_EINVAL, "null tensor pointer");
   const int64_t row_bytes = (int64_t)p->head_dim * elem_bytes(p->dtype);
   if (row_bytes / 16 * p->page_size * p->n_kv_heads > (int64_t(1) << 26))
     return fail(ctx, ASL_EUNSUPPORTED, "pages of more than 2^30 bytes");
@@ -147,6 +148,7 @@ asl_status asl_pages_free(asl_ctx* ctx, const asl_pages* p, const int32_t* rows,
   asl_status st = check_pages(ctx, p, table, kv_len, &m);
   if (st == ASL_OK) st = check_count(ctx, n);
   if (st != ASL_OK) return st;
+  if (n == 0) return ASL_OK;
   if (!rows || !refs) return fail(ctx, ASL_EINVAL, "null tensor pointer");
   DeviceGuard guard(ctx->device);
   if (guard.err != hipSuccess) return hip_fail(ctx, guard.err, "set device");
@@ -161,8 +163,10 @@ static asl_status write_rows(asl_ctx* ctx, const asl_pages* p, asl::PagesWriteAr
                              const int32_t* kv_len, void* k_pages, void* v_pages, void* stream) {
   asl_status st = check_count(ctx, n);
   if (st != ASL_OK) return st;
-  if (!rows || !cu || !k_pages || !v_pages) return fail(ctx, ASL_EINVAL, "null tensor pointer");
   if (total < 0) return fail(ctx, ASL_EINVAL, "total must be >= 0");
+  if (n == 0 || total == 0) return ASL_OK;                 // (tensors without elements have no address)
+  if (!rows || !cu || !k_pages || !v_pages || !a.k || !a.v) return fail(ctx, ASL_EINVAL, "null tensor pointer");
+  if (a.src_rows && !idx) return fail(ctx, ASL_EINVAL, "null tensor pointer");
   if (idx && idx_rows != 1 && idx_rows != p->n_kv_heads)
     return fail(ctx, ASL_EINVAL, "idx_rows must be 1 or Hk (got %d)", idx_rows);
   if (!aligned16(k_pages) || !aligned16(v_pages)) return fail(ctx, ASL_EUNSUPPORTED, "pages must be 16-byte aligned");
@@ -188,7 +192,6 @@ asl_status asl_pages_write(asl_ctx* ctx, const asl_pages* p, const asl_rows* src
   asl::PagesWriteArgs a = {};
   asl_status st = check_pages(ctx, p, table, kv_len, &a.map);
   if (st != ASL_OK) return st;
-  if (!k || !v) return fail(ctx, ASL_EINVAL, "null tensor pointer");
   const char* why = "";
   st = asl::rows_status(*p, src, &why);
   if (st != ASL_OK) return fail(ctx, st, "%s", why);
@@ -210,7 +213,7 @@ asl_status asl_pages_compact(asl_ctx* ctx, const asl_pages* p, const int32_t* sr
   asl::PagesWriteArgs a = {};
   asl_status st = check_pages(ctx, p, table, kv_len, &a.map);
   if (st != ASL_OK) return st;
-  if (!src_rows || !idx) return fail(ctx, ASL_EINVAL, "null tensor pointer");
+  if (n > 0 && !src_rows) return fail(ctx, ASL_EINVAL, "null tensor pointer");
   a.src_rows = src_rows;
   a.k = static_cast<const char*>(k_pages);
   a.v = static_cast<const char*>(v_pages);
@@ -232,6 +235,7 @@ asl_status asl_paged_attention(asl_ctx* ctx, const asl_pages* p, const asl_attn*
   if (p->head_dim > ctx->paged.max_head_dim || (int64_t)at->total_q * p->n_q_heads > ctx->paged.max_query_rows)
     return fail(ctx, ASL_ENOMEM, "total_q*Hq=%lld rows of d=%d exceed what asl_paged_reserve was called for (%d, %d)",
                 (long long)at->total_q * p->n_q_heads, p->head_dim, ctx->paged.max_query_rows, ctx->paged.max_head_dim);
+  if (at->n_seqs == 0 || at->total_q == 0) return ASL_OK;  // (tensors without elements have no address)
   if (!q || !k_pages || !v_pages || !cu_q || !out) return fail(ctx, ASL_EINVAL, "null tensor pointer");
   if (at->n_groups > 0 && (!group_start || !prefix_len)) return fail(ctx, ASL_EINVAL, "groups need group_start and prefix_len");
   if (!aligned16(q) || !aligned16(out) || !aligned16(k_pages) || !aligned16(v_pages))

@@ -842,3 +842,58 @@ def test_lists_that_do_not_ascend_leave_no_trace(ctx, gpu_device, kv):
         got, got_l = _attend(ctx, c, q, [1] * 8, 8)
         assert torch.equal(got, want) and torch.equal(got_l, want_l)
     assert ctx.asl_device_fault() == 0
+
+
+def test_calls_without_work(ctx, gpu_device):
+    """No sequences, no tokens: nothing is read, nothing refused."""
+    torch = _torch()
+    c = Cache(gpu_device, [40, 20], 2, 64, 16, "bf16", 3)
+    none, i = torch.empty(0, dtype=torch.int32, device=gpu_device), lambda *x: _ints(x, gpu_device)
+    empty = torch.empty((2, 0, 64), dtype=torch.bfloat16, device=gpu_device)
+    before, books = c.k.clone(), c.kv_len.clone()
+    ctx.asl_pages_grow(c.desc(), none, none, 0, c.table, c.kv_len, c.refs)
+    ctx.asl_pages_fork(c.desc(), None, None, 0, none, none, 0, c.table, c.kv_len, c.refs)
+    ctx.asl_pages_free(c.desc(), none, 0, c.table, c.kv_len, c.refs)
+    ctx.asl_pages_write(c.desc(), empty, empty, i(0), i(0, 0), 1, 0, c.table, c.kv_len, c.k, c.v)
+    ctx.asl_pages_compact(c.desc(), i(0), i(1), i(0, 0), 1, 0, none.view(1, 0), c.table, c.kv_len, c.k, c.v)
+    out, lse = _attend(ctx, c, _queries(0, 4, 64, "bf16", gpu_device, 1), [0, 0], 4)
+    assert out.numel() == 0 and lse.numel() == 0
+    assert torch.equal(c.k.nan_to_num(), before.nan_to_num()) and torch.equal(c.kv_len, books)
+    assert ctx.asl_device_fault() == 0
+
+
+def test_offsets_past_32_bits(ctx, gpu_device):
+    """Pages beyond 4 GiB: grown, written, continued, compacted, attended to."""
+    torch = _torch()
+    Hq, Hk, d, ps, dev = 8, 2, 128, 64, gpu_device
+    n_pages = (9 << 30) // (Hk * ps * d * 2) // 2 + 7                         # 4.5 GiB each of K and V
+    kp, vp = (torch.empty((n_pages, Hk, ps, d), dtype=torch.bfloat16, device=dev) for _ in range(2))
+    table, kv = torch.zeros((4, 8), dtype=torch.int32, device=dev), torch.zeros(4, dtype=torch.int32, device=dev)
+    refs = torch.ones(n_pages, dtype=torch.int32, device=dev)
+    refs[-20:] = 0
+    refs[3] = 0                                               # one page at the beginning, the others at the end
+    p = asl.make_pages(Hq, Hk, d, ps, n_pages, 4, 8)
+    i = lambda *x: _ints(x, dev)
+    g = torch.Generator().manual_seed(2)
+    k, v = (torch.randn((Hk, 200, d), generator=g).to(torch.bfloat16).to(dev) for _ in range(2))
+    ctx.asl_pages_grow(p, i(0), i(200), 1, table, kv, refs)
+    assert table[0, :4].tolist() == [3, n_pages - 20, n_pages - 19, n_pages - 18]
+    ctx.asl_pages_write(p, k, v, i(0), i(0, 200), 1, 200, table, kv, kp, vp)
+    ptr = lambda x: torch.tensor([x.data_ptr()], dtype=torch.int64, device=dev)
+    kptr, vptr = ptr(kp), ptr(vp)
+    ctx.asl_pages_fork(p, kptr, vptr, 1, i(0), i(1), 1, table, kv, refs)
+    keep = [5, 70, 130, 190, 199]
+    ctx.asl_pages_grow(p, i(2), i(5), 1, table, kv, refs)
+    ctx.asl_pages_compact(p, i(1), i(2), i(0, 5), 1, 5, i(*keep).view(1, 5), table, kv, kp, vp)
+    f = lambda x: x.double().cpu().numpy()
+    for n_q in ([1, 1, 1], [40, 40, 3]):
+        q = _queries(sum(n_q), Hq, d, "bf16", dev, 3)
+        out, lse = torch.empty_like(q.contiguous()), torch.empty((Hq, sum(n_q)), dtype=torch.float32, device=dev)
+        cu = np.concatenate([[0], np.cumsum(n_q)])
+        for bound in (200, 1 << 20):                          # split items, tiles
+            ctx.asl_paged_attention(p, asl.make_attn(3, sum(n_q), max(n_q), bound), q, kp, vp, table, kv, _ints(cu, dev), out, lse=lse)
+            parts = [po.attention(f(q)[cu[b]:cu[b + 1]], f(k)[:, s], f(v)[:, s], d ** -0.5, True)
+                     for b, s in enumerate((slice(None), slice(None), keep))]
+            ref = tuple(np.concatenate([x[j] for x in parts], axis=1 if j == 1 else 0) for j in range(4))
+            _check(out, lse, ref, d, 200, "bf16", "past 32 bits")
+    assert ctx.asl_device_fault() == 0
