@@ -746,14 +746,16 @@ __device__ __forceinline__ void write_row(const AttendArgs& a, const Item& it, c
     return;
   }
   const int i = (int)((uint32_t)r / (uint32_t)a.G), tok = it.seg.c0 + i, hq = it.h * a.G + (r - i * a.G);
-  if (e0 < a.d) {
-    const float by = z == 0.f ? 0.f : 1.f / z;             // no key: the sums are zero
-    T* to = (T*)a.out + (int64_t)tok * a.ot + (int64_t)hq * a.oh + e0;
-    typedef T Out __attribute__((ext_vector_type(CNT)));
+  const float by = z == 0.f ? 0.f : 1.f / z;               // no key: the sums are zero
+  T* to = (T*)a.out + (int64_t)tok * a.ot + (int64_t)hq * a.oh + e0;
+  constexpr int W = store_elements(CNT, (int)sizeof(T));
+  typedef T Out __attribute__((ext_vector_type(W)));
+#pragma unroll
+  for (int x0 = 0; x0 < CNT; x0 += W) {
     Out w;
 #pragma unroll
-    for (int x = 0; x < CNT; ++x) w[x] = (T)(v[x] * by);
-    *(Out*)to = w;
+    for (int x = 0; x < W; ++x) w[x] = (T)(v[x0 + x] * by);
+    if (e0 + x0 < a.d) *(Out*)(to + x0) = w;
   }
   if (e0 == 0 && a.lse != nullptr) a.lse[(int64_t)hq * a.total_q + tok] = z == 0.f ? -INFINITY : (m + __log2f(z)) * kLn2;
 }

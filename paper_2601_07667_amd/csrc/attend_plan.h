@@ -58,4 +58,8 @@ ASL_HD int shared_tokens(int stated, int first_len, int members) {
 // 1024 (84 MB) 34, 27, 2090 (171 MB) 37, 45).
 constexpr unsigned long long kMinSaved = 128ull << 20;
 
+// Elements that one store to a row of `out` takes, of `held` neighbouring ones that a thread has: 16 bytes at most, since d and the strides
+// of `out` are whole multiples of those and need not be of more (d = 100 in fp32: the thread that has elements 96 .. 103 stores four).
+ASL_HD constexpr int store_elements(int held, int bytes) { return held * bytes > 16 ? 16 / bytes : held; }
+
 }  // namespace asl

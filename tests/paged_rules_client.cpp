@@ -1,0 +1,31 @@
+// Reads commands from its input and prints what the library's rules for the paged calls come to (built and run by tests/test_paged_rules.py).
+#include <cstdio>
+#include <cstring>
+#include <vector>
+
+#include "attend_plan.h"
+
+static long long num() {
+  long long x = 0;
+  if (std::scanf("%lld", &x) != 1) x = 0;
+  return x;
+}
+
+int main() {
+  char what[16];
+  while (std::scanf("%15s", what) == 1) {
+    if (!std::strcmp(what, "stores")) {
+      // bytes of an element, elements that a thread holds, padded and true head size: whether the threads' stores to a row take each
+      // of its elements once and nothing behind it
+      const int bytes = (int)num(), held = (int)num(), D = (int)num(), d = (int)num(), w = asl::store_elements(held, bytes);
+      std::vector<int> hit(D + 64);
+      for (int e0 = 0; e0 < D; e0 += held)
+        for (int x0 = 0; x0 < held; x0 += w)
+          for (int x = 0; x < w && e0 + x0 < d; ++x) ++hit[e0 + x0 + x];
+      bool ok = held % w == 0;
+      for (int e = 0; e < D + 64; ++e) ok = ok && hit[e] == (e < d ? 1 : 0);
+      std::printf("%d %d\n", ok ? 1 : 0, w);
+    }
+  }
+  return 0;
+}
