@@ -309,7 +309,10 @@ typedef struct {
 
 /* Allocates the paged calls' part of the workspace, for at most max_seqs sequences per call (<= 4096) and attention of
  * total_q * Hq <= max_query_rows, d <= max_head_dim (<= 256).  Call it once before them, outside stream capture; again to
- * change the limits.  A call past them, or without it, returns ASL_ENOMEM. */
+ * change the limits.  Lower ones take nothing; for higher ones it allocates anew, and calls that are queued and graphs that are
+ * captured keep the memory that they were made with: it is freed with the context (at most 8 allocations in all).  If the
+ * allocation fails, limits and workspace stay as they were.  A fault that was raised stays raised.
+ * A call past the limits, or without it, returns ASL_ENOMEM. */
 asl_status asl_paged_reserve(asl_ctx* ctx, int32_t max_seqs, int32_t max_query_rows, int32_t max_head_dim);
 
 /* Makes row rows[i] add[i] tokens longer (>= 0), for i < n: kv_len grows, and where the tokens need pages the row gets the

@@ -218,8 +218,12 @@ asl_status asl_destroy(asl_ctx* ctx) {
   (void)hipStreamDestroy(ctx->side);
   hipError_t e = hipFree(ctx->base);
   if (ctx->paged.base) {
-    const hipError_t ep = hipFree(ctx->paged.base);
+    hipError_t ep = hipFree(ctx->paged.base);
     if (e == hipSuccess) e = ep;
+    for (int i = 0; i < ctx->n_paged_kept; ++i) {
+      ep = hipFree(ctx->paged_kept[i]);
+      if (e == hipSuccess) e = ep;
+    }
   }
   delete ctx;
   return e == hipSuccess ? ASL_OK : ASL_EHIP;

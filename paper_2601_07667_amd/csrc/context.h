@@ -17,6 +17,8 @@ struct asl_ctx {
   hipEvent_t ev_fork, ev_join;
   bool side_pending;         // a deferred asl_layer_step left work on `side` that nobody has waited for yet
   asl::PagedWorkspace paged; // asl_paged_reserve's; all null before it
+  void* paged_kept[asl::kPagedKept];   // workspaces that it has outgrown: queued calls and captured graphs may use them
+  int n_paged_kept;
   char err[256];
 };
 

@@ -11,7 +11,8 @@ namespace asl {
 // What asl_paged_reserve allocates.
 struct PagedWorkspace {
   void* base;
-  int32_t max_seqs, max_query_rows, max_head_dim;
+  int32_t room_rows, room_dim;                         // what it was made for (room_for)
+  int32_t max_seqs, max_query_rows, max_head_dim;      // the limits last asked for
   float* part;             // [part_rows][max_head_dim, a power of two >= 64] attention: unnormalised results of cut rows ...
   float2* part_mz;         // [part_rows] ... with their reference and sum
   uint32_t* arrived;       // [part_rows] zeros between calls
@@ -19,9 +20,9 @@ struct PagedWorkspace {
   int4* plan;              // [2][kPagedMaxSeqs] how sequences and groups were cut
   int32_t* group;          // [kPagedMaxSeqs] the sequences' groups
   int32_t* cut;            // [1] whether any row is in pieces
-  int4* forks;             // [max_seqs] what the bookkeeping launch of a fork leaves for the copying one
+  int4* forks;             // [kPagedMaxSeqs] what the bookkeeping launch of a fork leaves for the copying one
   int32_t* fresh;          // [kMaxFresh] the free pages that a call takes, in order
-  uint32_t* fault;         // [1]
+  uint32_t* fault;         // [1] the context's first workspace has it, for all
 };
 
 struct PagesWriteArgs {

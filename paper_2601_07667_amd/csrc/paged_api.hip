@@ -30,6 +30,12 @@ void set_row_pieces(int64_t row_bytes, int32_t* cpr, int32_t* shift) {
   *shift = (*cpr & (*cpr - 1)) == 0 ? asl::log2_of(*cpr) : -1;
 }
 
+// Rows of pieces of attention's results: every row twice (its own and its shared keys; not for the largest calls, which have no need to
+// share), and the pieces that long spans are cut into.
+int64_t part_rows(int32_t query_rows) {
+  return 2 * (int64_t)(query_rows < asl::kPagedRowsHeld ? query_rows : asl::kPagedRowsHeld) + asl::kCutRows;
+}
+
 }  // namespace
 
 extern "C" {
@@ -40,57 +46,58 @@ asl_status asl_paged_reserve(asl_ctx* ctx, int32_t max_seqs, int32_t max_query_r
   if (max_seqs < 1 || max_query_rows < 1 || max_head_dim < 1) return fail(ctx, ASL_EINVAL, "limits must be >= 1");
   if (max_seqs > asl::kPagedMaxSeqs) return fail(ctx, ASL_EUNSUPPORTED, "more than %d sequences per call", asl::kPagedMaxSeqs);
   if (max_head_dim > asl::kPagedMaxDim) return fail(ctx, ASL_EUNSUPPORTED, "head_dim > %d not supported", asl::kPagedMaxDim);
-  DeviceGuard guard(ctx->device);
-  if (guard.err != hipSuccess) return hip_fail(ctx, guard.err, "set device");
-  if (ctx->paged.base) {
-    hipError_t e = hipFree(ctx->paged.base);               // waits for the work that may still use it
-    ctx->paged = asl::PagedWorkspace();
-    if (e != hipSuccess) return hip_fail(ctx, e, "free");
+  asl::PagedWorkspace& ws = ctx->paged;
+  const asl::PagedRoom room = asl::room_for({ws.room_rows, ws.room_dim}, max_query_rows, max_head_dim);
+  if (!ws.base || room.rows != ws.room_rows || room.dim != ws.room_dim) {
+    if (ws.base && ctx->n_paged_kept == asl::kPagedKept) return fail(ctx, ASL_ENOMEM, "limits were raised too often");
+    DeviceGuard guard(ctx->device);
+    if (guard.err != hipSuccess) return hip_fail(ctx, guard.err, "set device");
+    asl::PagedWorkspace w = {};
+    size_t off = 0;
+    auto take = [&](size_t bytes) {
+      const size_t at = off;
+      off += align_up(bytes);
+      return at;
+    };
+    const size_t rows = (size_t)part_rows(room.rows);
+    const size_t fault = take(sizeof(uint32_t)), forks = take((size_t)asl::kPagedMaxSeqs * sizeof(int4)),
+                 fresh = take((size_t)asl::kMaxFresh * sizeof(int32_t)),
+                 plan = take((size_t)2 * asl::kPagedMaxSeqs * sizeof(int4)),
+                 group = take((size_t)asl::kPagedMaxSeqs * sizeof(int32_t)),
+                 cut = take(sizeof(int32_t));
+    const size_t part = take(rows * room.dim * sizeof(float)), part_mz = take(rows * sizeof(float2)),
+                 arrived = take(rows * sizeof(uint32_t));
+    char* base = nullptr;
+    hipError_t e = hipMalloc(&base, off);
+    if (e != hipSuccess) {
+      (void)hipGetLastError();
+      return fail(ctx, e == hipErrorOutOfMemory ? ASL_ENOMEM : ASL_EHIP, "workspace of %zu bytes: %s", off, hipGetErrorString(e));
+    }
+    e = hipMemset(base, 0, off);
+    if (e == hipSuccess) e = hipStreamSynchronize(nullptr);  // calls may follow on any stream
+    if (e != hipSuccess) {
+      (void)hipFree(base);
+      return hip_fail(ctx, e, "workspace");
+    }
+    w.base = base;
+    w.room_rows = room.rows;
+    w.room_dim = room.dim;
+    w.fault = ws.base ? ws.fault : (uint32_t*)(base + fault);
+    w.forks = (int4*)(base + forks);
+    w.fresh = (int32_t*)(base + fresh);
+    w.plan = (int4*)(base + plan);
+    w.group = (int32_t*)(base + group);
+    w.cut = (int32_t*)(base + cut);
+    w.part = (float*)(base + part);
+    w.part_mz = (float2*)(base + part_mz);
+    w.arrived = (uint32_t*)(base + arrived);
+    if (ws.base) ctx->paged_kept[ctx->n_paged_kept++] = ws.base;
+    ws = w;
   }
-  asl::PagedWorkspace w = {};
-  size_t off = 0;
-  auto take = [&](size_t bytes) {
-    const size_t at = off;
-    off += align_up(bytes);
-    return at;
-  };
-  const size_t fault = take(sizeof(uint32_t)), forks = take((size_t)max_seqs * sizeof(int4)),
-               fresh = take((size_t)asl::kMaxFresh * sizeof(int32_t)),
-               plan = take((size_t)2 * asl::kPagedMaxSeqs * sizeof(int4)),
-               group = take((size_t)asl::kPagedMaxSeqs * sizeof(int32_t)),
-               cut = take(sizeof(int32_t));
-  // attention: room for every row twice (its own and its shared keys; not for the largest calls, which have no need to share),
-  // and for the pieces that long spans are cut into
-  w.part_rows = 2 * (int64_t)(max_query_rows < 131072 ? max_query_rows : 131072) + asl::kCutRows;
-  const int D = max_head_dim <= 64 ? 64 : max_head_dim <= 128 ? 128 : 256;
-  const size_t part = take((size_t)w.part_rows * D * sizeof(float)), part_mz = take((size_t)w.part_rows * sizeof(float2)),
-               arrived = take((size_t)w.part_rows * sizeof(uint32_t));
-  char* base = nullptr;
-  hipError_t e = hipMalloc(&base, off);
-  if (e != hipSuccess) {
-    (void)hipGetLastError();
-    return fail(ctx, e == hipErrorOutOfMemory ? ASL_ENOMEM : ASL_EHIP, "workspace of %zu bytes: %s", off, hipGetErrorString(e));
-  }
-  w.base = base;
-  w.fault = (uint32_t*)(base + fault);
-  w.forks = (int4*)(base + forks);
-  w.fresh = (int32_t*)(base + fresh);
-  w.plan = (int4*)(base + plan);
-  w.group = (int32_t*)(base + group);
-  w.cut = (int32_t*)(base + cut);
-  w.part = (float*)(base + part);
-  w.part_mz = (float2*)(base + part_mz);
-  w.arrived = (uint32_t*)(base + arrived);
-  w.max_seqs = max_seqs;
-  w.max_query_rows = max_query_rows;
-  w.max_head_dim = max_head_dim;
-  e = hipMemset(base, 0, off);
-  if (e == hipSuccess) e = hipStreamSynchronize(nullptr);  // calls may follow on any stream
-  if (e != hipSuccess) {
-    (void)hipFree(base);
-    return hip_fail(ctx, e, "workspace");
-  }
-  ctx->paged = w;
+  ws.part_rows = part_rows(max_query_rows);
+  ws.max_seqs = max_seqs;
+  ws.max_query_rows = max_query_rows;
+  ws.max_head_dim = max_head_dim;
   return ASL_OK;
 }
 

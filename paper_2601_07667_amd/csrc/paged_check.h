@@ -1,4 +1,4 @@
-// The paged calls' checks of the structs that they are given.  Host code, without a GPU.
+// The paged calls' checks of the structs that they are given, and the size of their workspace.  Host code, without a GPU.
 #pragma once
 #include <stdint.h>
 
@@ -14,6 +14,22 @@ inline int log2_of(int x) {
 }
 
 inline int bytes_of(int dtype) { return dtype == ASL_BF16 ? 2 : 4; }
+
+// What a workspace of the paged calls has room for.
+struct PagedRoom {
+  int32_t rows;            // query rows (as far as the pieces of their results grow with them)
+  int32_t dim;             // padded head size
+};
+
+// The room that limits need beside what there is: never less in either measure, rows a power of two.  So a context's limits may go up and
+// down in any order, and of 6 sizes by 3 it takes at most 7 steps from the first workspace to the largest.
+inline PagedRoom room_for(const PagedRoom& have, int32_t max_query_rows, int32_t max_head_dim) {
+  PagedRoom r = {4096, max_head_dim <= 64 ? 64 : max_head_dim <= 128 ? 128 : 256};
+  while (r.rows < max_query_rows && r.rows < kPagedRowsHeld) r.rows *= 2;
+  if (r.rows < have.rows) r.rows = have.rows;
+  if (r.dim < have.dim) r.dim = have.dim;
+  return r;
+}
 
 // Strides and rows that 16-byte pieces take.
 inline bool whole_pieces(int64_t elements, int dtype) { return elements * bytes_of(dtype) % 16 == 0; }

@@ -18,6 +18,8 @@ constexpr int kPagedMaxSeqs = 4096;        // sequences of one call
 constexpr int kMaxFresh = 65536;           // pages that one call takes
 constexpr int kCutRows = 131072;           // rows of partial results beside one for each row's own and shared keys
 constexpr int kPagedMaxDim = 256;          // head_dim of asl_paged_attention
+constexpr int kPagedRowsHeld = 131072;     // query rows beyond which the workspace does not grow
+constexpr int kPagedKept = 7;              // workspaces that a context outgrows at most (see room_for)
 
 struct PageMap {
   const int32_t* table;                    // [n_rows][row_stride]

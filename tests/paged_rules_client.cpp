@@ -4,6 +4,7 @@
 #include <vector>
 
 #include "attend_plan.h"
+#include "paged_check.h"
 
 static long long num() {
   long long x = 0;
@@ -25,6 +26,16 @@ int main() {
       bool ok = held % w == 0;
       for (int e = 0; e < D + 64; ++e) ok = ok && hit[e] == (e < d ? 1 : 0);
       std::printf("%d %d\n", ok ? 1 : 0, w);
+    } else if (!std::strcmp(what, "room")) {
+      // n limits (query rows, head size) in turn: the room after each
+      asl::PagedRoom r = {0, 0};
+      for (int n = (int)num(); n > 0; --n) {
+        const int rows = (int)num(), dim = (int)num();
+        r = asl::room_for(r, rows, dim);
+        std::printf("%d %d\n", r.rows, r.dim);
+      }
+    } else if (!std::strcmp(what, "kept")) {
+      std::printf("%d\n", asl::kPagedKept);
     }
   }
   return 0;

@@ -1,4 +1,5 @@
-"""The paged calls on the GPU where their paths part: head sizes that leave a part of a store."""
+"""The paged calls on the GPU where their paths part: head sizes that leave a part of a store,
+limits that change."""
 import numpy as np
 import pytest
 
@@ -30,3 +31,83 @@ def test_rows_of_head_sizes_that_leave_a_part_of_a_store(ctx, gpu_device, lens, 
         _check(rows[..., :d], lse, ref, d, max(lens), dtype, "d %d, pad %d" % (d, pad))
         assert bool((rows[..., d:] == 77).all()) and bool((room[total * Hq * (d + pad):] == 77).all())
     assert ctx.asl_device_fault() == 0
+
+
+def test_a_fault_outlives_new_limits(gpu_device):
+    import torch
+    x = asl.Asl(2, 1, 1)
+    i = lambda *v: _ints(v, gpu_device)
+    table, kv, refs = torch.zeros((2, 4), dtype=torch.int32, device=gpu_device), i(0, 0), i(*[0] * 8)
+    p = asl.make_pages(1, 1, 64, 16, 8, 2, 4)
+    for limits in ((4, 64, 64), (2, 8, 16), (4, 5000, 64), (4, 5000, 256), (4096, 1 << 20, 256), (1, 1, 1)):
+        x.asl_paged_reserve(*limits)
+        assert x.asl_device_fault() == 0
+        x.asl_pages_grow(p, i(9), i(1), 1, table, kv, refs)               # no such row
+        x.asl_paged_reserve(4, 20000 if limits[0] == 4 else 1, 256)
+        assert x.asl_device_fault() == 2, limits
+    x.close()
+
+
+def test_graphs_captured_before_new_limits_keep_their_workspace(gpu_device):
+    """A graph that joins pieces in the launch, one that joins them after it, and one that grows, writes and forks: captured, the limits
+    raised and lowered, replayed between calls under the new ones."""
+    import torch
+    dev = gpu_device
+    x = asl.Asl(2, 1, 1)
+    x.asl_paged_reserve(8, 64, 64)
+    lens = [1900, 300, 20, 700]
+    c = Cache(dev, lens, 2, 64, 16, "bf16", 31)
+    q, n_q = _queries(4, 4, 64, "bf16", dev, 32), [1] * 4
+    cu = _ints(range(5), dev)
+    outs = [torch.empty_like(q) for _ in range(2)]
+    lses = [torch.empty((4, 4), dtype=torch.float32, device=dev) for _ in range(2)]
+    batches = [asl.make_attn(4, 4, 1, most) for most in (2000, 20000)]
+    i = lambda *v: _ints(v, dev)
+    pages = asl.make_pages(2, 2, 64, 16, 40, 6, 8)
+    table, kv, refs = torch.zeros((6, 8), dtype=torch.int32, device=dev), torch.zeros(6, dtype=torch.int32, device=dev), i(*[0] * 40)
+    kp, vp = (torch.zeros((40, 2, 16, 64), dtype=torch.bfloat16, device=dev) for _ in range(2))
+    kptr, vptr = (torch.tensor([t.data_ptr()], dtype=torch.int64, device=dev) for t in (kp, vp))
+    new = _queries(2 * 21, 1, 64, "bf16", dev, 33).reshape(2, 21, 64)
+    lists = dict(row=i(0), add=i(21), cu=i(0, 21), parents=i(0, 0, 0), children=i(1, 2, 3), all=i(0, 1, 2, 3))
+
+    def attend():
+        for a, out, lse in zip(batches, outs, lses):
+            x.asl_paged_attention(c.desc(4), a, q, c.k, c.v, c.table, c.kv_len, cu, out, lse=lse)
+
+    def books():
+        x.asl_pages_grow(pages, lists["row"], lists["add"], 1, table, kv, refs)
+        x.asl_pages_write(pages, new, new, lists["row"], lists["cu"], 1, 21, table, kv, kp, vp)
+        x.asl_pages_fork(pages, kptr, vptr, 1, lists["parents"], lists["children"], 3, table, kv, refs)
+
+    attend()
+    books()
+    torch.cuda.synchronize()
+    want = [t.clone() for t in outs + lses]
+    _check(outs[0], lses[0], _oracle(c, q, n_q), 64, max(lens), "bf16", "before")
+    want_books = [t.clone() for t in (table, kv, refs, kp, vp)]
+    x.asl_pages_free(pages, lists["all"], 4, table, kv, refs)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        attend()
+        books()
+    limits = [(8, 64, 64), (8, 100, 64), (8, 60000, 64), (2, 8, 16), (4096, 1 << 18, 256), (8, 16, 64)]
+    for limit in limits:
+        x.asl_paged_reserve(*limit)
+        fill = torch.full((1 << 24,), -1, dtype=torch.int32, device=dev)      # what a freed workspace could be handed out as
+        for t in outs + lses:
+            t.fill_(float("nan"))
+        for t in (kv, refs, kp, vp):
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs + lses, want)), limit
+        assert all(torch.equal(a, b) for a, b in zip((kv, refs, kp, vp), want_books[1:])), limit
+        assert bool((fill == -1).all())
+        if limit[0] >= 8 and limit[1] >= 16 and limit[2] >= 64:               # the same calls now
+            for t in outs + lses:
+                t.fill_(float("nan"))
+            attend()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(outs + lses, want)), limit
+    assert x.asl_device_fault() == 0
+    x.close()
