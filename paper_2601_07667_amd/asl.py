@@ -150,6 +150,13 @@ def _ptr(t) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
 
+def _refuse_gaps(**tensors) -> None:
+    """The calls take the outer strides of these tensors; the elements of a row have to be neighbours."""
+    for name, t in tensors.items():
+        if t.stride(2) != 1:
+            raise AslError(ASL_EUNSUPPORTED, f"the last dimension of {name} must be contiguous (its stride is {t.stride(2)})")
+
+
 def _stream() -> int:
     """Handle of the calling thread's current stream on its current device, without the Stream object that
     torch.cuda.current_stream() makes (2.9 us of a call whose one launch takes 2.5; so 0.1 us)."""
@@ -174,7 +181,7 @@ def make_pages(Hq: int, Hk: int, d: int, page_size: int, n_pages: int, n_rows: i
 
 
 def make_attn(n_seqs: int, total_q: int, max_q_len: int, max_kv_len: int, n_groups: int = 0, causal: bool = True) -> AslAttn:
-    """The strides of q and out are set by each call from its tensors."""
+    """Each call takes the strides of q and out from its tensors; the description stays as it is."""
     return AslAttn(n_seqs, total_q, max_q_len, max_kv_len, n_groups, ASL_ATTN_CAUSAL if causal else 0, 0, 0, 0, 0)
 
 
@@ -291,8 +298,12 @@ class Asl:
     def asl_pages_write(self, pages: AslPages, k, v, rows, cu, n: int, total: int, table, kv_len, k_pages, v_pages,
                         idx=None) -> None:
         """k, v: [Hk, n_src, d] of any strides (d contiguous); idx: [1 or Hk, total]."""
-        kh, kt, _ = k.stride()
-        vh, vt, _ = v.stride()
+        kh, kt, k1 = k.stride()
+        vh, vt, v1 = v.stride()
+        if k1 != 1 or v1 != 1:
+            _refuse_gaps(k=k, v=v)
+        if v.shape != k.shape:
+            raise AslError(ASL_EINVAL, f"k and v differ in shape: {tuple(k.shape)}, {tuple(v.shape)}")
         src = AslRows(k.shape[1], 0 if idx is None else idx.shape[0], kh, kt, vh, vt)
         self._check(self.lib.asl_pages_write(self.h, C.byref(pages), C.byref(src), _ptr(k), _ptr(v), _ptr(rows), _ptr(cu), n,
                                              total, _ptr(idx), _ptr(table), _ptr(kv_len), _ptr(k_pages), _ptr(v_pages),
@@ -308,9 +319,12 @@ class Asl:
     def asl_paged_attention(self, pages: AslPages, attn: AslAttn, q, k_pages, v_pages, table, kv_len, cu_q, out, lse=None,
                             rows=None, group_start=None, prefix_len=None) -> None:
         """q, out: [total_q, Hq, d] of any strides (d contiguous); lse: [Hq, total_q]."""
-        attn.q_stride_tok, attn.q_stride_head, _ = q.stride()
-        attn.out_stride_tok, attn.out_stride_head, _ = out.stride()
-        self._check(self.lib.asl_paged_attention(self.h, C.byref(pages), C.byref(attn), _ptr(q), _ptr(k_pages), _ptr(v_pages),
+        a = AslAttn.from_buffer_copy(attn)                   # the description may be another thread's too
+        a.q_stride_tok, a.q_stride_head, q1 = q.stride()
+        a.out_stride_tok, a.out_stride_head, out1 = out.stride()
+        if q1 != 1 or out1 != 1:
+            _refuse_gaps(q=q, out=out)
+        self._check(self.lib.asl_paged_attention(self.h, C.byref(pages), C.byref(a), _ptr(q), _ptr(k_pages), _ptr(v_pages),
                                                  _ptr(rows), _ptr(table), _ptr(kv_len), _ptr(cu_q), _ptr(group_start),
                                                  _ptr(prefix_len), _ptr(out), _ptr(lse), _stream()))
 

@@ -1,4 +1,5 @@
 """The rules of the paged calls without a GPU."""
+import ctypes
 import os
 import random
 import shutil
@@ -6,6 +7,7 @@ import subprocess
 
 import pytest
 
+from paper_2601_07667_amd import asl as libasl
 from test_bound import ROOT
 
 
@@ -49,3 +51,73 @@ def test_a_workspace_is_outgrown_seven_times_at_most(client):
     slowly = [(4096 << i, 64) for i in range(6)] + [(1, 128), (1, 256)]
     rooms = client(["room %d %s" % (len(slowly), " ".join("%d %d" % x for x in slowly))])
     assert most <= 7 and len(set(rooms)) - 1 == 7 == int(client(["kept"])[0])
+
+
+# ------------------------------------------------------------------------------------------------- the binding
+class _Recorder:
+    """Stands in for the library: keeps what the paged calls are given."""
+
+    def __init__(self):
+        self.attn, self.rows = [], []
+
+    def asl_paged_attention(self, h, pages, attn, *pointers):
+        self.attn.append(libasl.AslAttn.from_buffer_copy(attn._obj))
+        return libasl.ASL_OK
+
+    def asl_pages_write(self, h, pages, src, *rest):
+        self.rows.append(libasl.AslRows.from_buffer_copy(src._obj))
+        return libasl.ASL_OK
+
+    def asl_destroy(self, h):
+        return libasl.ASL_OK
+
+
+@pytest.fixture
+def recorded(monkeypatch):
+    monkeypatch.setattr(libasl, "_stream", lambda: 0)
+    x = libasl.Asl.__new__(libasl.Asl)
+    x.lib, x.h, x.device = _Recorder(), ctypes.c_void_p(1), 0
+    return x
+
+
+def _attend_on_cpu(x, attn, q, out):
+    import torch
+    i = torch.zeros(4, dtype=torch.int32)
+    x.asl_paged_attention(libasl.make_pages(4, 2, 8, 16, 1, 1, 1), attn, q, q, q, i, i, i, out)
+
+
+def test_a_call_leaves_the_description_of_its_batch_alone(recorded):
+    import torch
+    attn = libasl.make_attn(2, 3, 2, 100, causal=False)
+    before = bytes(attn)
+    q, wide = torch.zeros(3, 4, 8), torch.zeros(3, 4, 24)[..., :8]
+    _attend_on_cpu(recorded, attn, q, wide)
+    _attend_on_cpu(recorded, attn, q.transpose(0, 1).contiguous().transpose(0, 1), q)
+    assert bytes(attn) == before
+    a, b = recorded.lib.attn
+    assert (a.n_seqs, a.total_q, a.max_q_len, a.max_kv_len, a.flags) == (2, 3, 2, 100, 0)
+    assert (a.q_stride_tok, a.q_stride_head, a.out_stride_tok, a.out_stride_head) == (32, 8, 96, 24)
+    assert (b.q_stride_tok, b.q_stride_head, b.out_stride_tok, b.out_stride_head) == (8, 24, 32, 8)
+
+
+def test_rows_that_are_not_contiguous_are_refused(recorded):
+    import torch
+    attn, good = libasl.make_attn(2, 3, 2, 100), torch.zeros(3, 4, 8)
+    bad = torch.zeros(3, 8, 4).transpose(1, 2)
+    for q, out, word in ((bad, good, "q"), (good, bad, "out"), (good[..., :4].expand(3, 4, 4)[..., ::2], good, "q")):
+        with pytest.raises(libasl.AslError, match="last dimension of " + word) as e:
+            _attend_on_cpu(recorded, attn, q, out)
+        assert e.value.status == libasl.ASL_EUNSUPPORTED
+    pages, i = libasl.make_pages(2, 2, 8, 16, 1, 1, 1), torch.zeros(4, dtype=torch.int32)
+    k = torch.zeros(2, 3, 8)
+    write = lambda k, v: recorded.asl_pages_write(pages, k, v, i, i, 1, 3, i, i, k, k)
+    for a, b, status in ((torch.zeros(2, 8, 3).transpose(1, 2), k, libasl.ASL_EUNSUPPORTED),
+                         (k, torch.zeros(2, 8, 3).transpose(1, 2), libasl.ASL_EUNSUPPORTED),
+                         (k, k[:, :2], libasl.ASL_EINVAL), (k, k[:1], libasl.ASL_EINVAL)):    # v ends before k does
+        with pytest.raises(libasl.AslError) as e:
+            write(a, b)
+        assert e.value.status == status
+    assert not recorded.lib.attn and not recorded.lib.rows
+    write(k.transpose(0, 1).contiguous().transpose(0, 1), k)
+    src = recorded.lib.rows[0]
+    assert (src.n_src, src.k_stride_head, src.k_stride_tok, src.v_stride_head, src.v_stride_tok) == (3, 8, 16, 24, 8)
