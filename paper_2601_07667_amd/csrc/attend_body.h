@@ -118,7 +118,7 @@ struct Groups {
       shared = group_shared(a, g);
       saved += (unsigned long long)max(0, end - start - 1) * (uint32_t)shared;
     }
-    on = wave_sum(saved) * (unsigned long long)a.key_bytes >= kMinSaved;
+    on = groups_pay(wave_sum(saved), a.key_bytes);
   }
   // The group of sequence b, or -1; *tokens: what it shares.  (Every lane of the wavefront calls it.)
   __device__ __forceinline__ int find(const AttendArgs& a, int b, int* tokens) const {
@@ -1359,9 +1359,6 @@ __global__ void __launch_bounds__(NW > kWaves ? NW * 64 : kThreads) attend_join_
 }
 
 // ------------------------------------------------------------------------------------------------------------------
-// How a kind of segments is worked on: by split items of 16 rows, or tiles of 64 or 128 (0: there are none).
-constexpr int kNone = 0, kSplit = 16, kTile1 = 64, kTile2 = 128;
-
 template <typename T, int D, int KIND, bool PAD, bool SHARED, bool STREAM>
 __device__ __forceinline__ void run_item(const AttendArgs& a, const AttendCut& cut, const Partials& pt, int item, char* lds) {
   if constexpr (KIND == kSplit) split_item<T, D, 1, PAD, SHARED, STREAM>(a, cut, pt, item, lds);
@@ -1406,40 +1403,13 @@ hipError_t launch_kinds(const AttendArgs& a, const AttendCut& own, const AttendC
   return hipGetLastError();
 }
 
-// The longest sequences whose pieces (of 128 keys or more) are joined within the launch.
-constexpr int kJoinKeys = 2048;
-
-// The kind for `segments` segments of up to `rows` rows and `keys` keys.  A split item has all four wavefronts' loads on their way and
-// needs no barrier, a tile reads its keys once for 64 or 128 rows: calls of little work are bound by latency and are split
-// (32 query heads, 8 KV heads, d = 128; us, split and tiles: 32 rows 512 keys 11, 23; 128 rows 512 keys 11, 27; 64 rows 4096 keys 18,
-// 25), others are not (8 sequences, 4096 keys: 32 rows 34, 36, 64 rows 50, 38; 32768 keys: 32 rows 225, 208, 64 rows 357, 214).
-// Tiles of 64 rows up to 64 (8 sequences, 32768 keys, 64 rows 214 us, with tiles of 128 228).
-constexpr double kSplitWork = 524288.;     // tiles of 16 rows x keys x KV heads
-// Pieces of tiles: about 512 of own keys, two a compute unit (one chunk of 512 tokens over 4096 keys 63 us, with 384 74), 384 of
-// shared ones, beside which there are others (shared prompt of 32768 keys 88 us, with 512 93.5); at least 8 key tiles each
-// (shared drafts 36 us, with 4 47).
-AttendCut cut_for(bool tiles, int64_t rows, int64_t keys, int64_t segments, int Hk, bool shared) {
-  const double work = (double)((rows + 15) / 16) * (double)keys * (double)segments * Hk;
-  if (tiles && rows > 16 && work >= kSplitWork) return AttendCut{rows > 64 ? kTile2 : kTile1, shared ? 384 : 512, 8, 0};
-  return AttendCut{kSplit, 512, 2, 0};
-}
-
 template <typename T, int D>
 hipError_t launch_d(const PagedWorkspace& ws, const AttendArgs& args, hipStream_t st) {
   AttendArgs a = args;
   constexpr bool kTiles = sizeof(T) == 2 && D <= 128;
-  const int64_t rows = (int64_t)a.total_q * a.G;           // of a KV head
-  const int64_t most = (int64_t)a.max_q_len * a.G < rows ? (int64_t)a.max_q_len * a.G : rows;
-  AttendCut own = cut_for(kTiles, most, a.max_kv_len, a.n_seqs, a.Hk, false);
-  AttendCut shared = cut_for(kTiles, a.n_groups > 0 ? rows / a.n_groups : 0, a.max_kv_len, a.n_groups, a.Hk, true);
-  const int64_t room = ws.part_rows;
-  shared.cap = max_partials(shared, rows, a.Hk);
-  // a sequence whose own rows fill a tile gains nothing, and groups cannot save more than all sequences' keys but one each (kMinSaved);
-  // every row of a group is joined from two parts, for which there has to be room
-  const double most_saved = (double)(a.n_seqs - a.n_groups) * (double)a.max_kv_len * (double)a.key_bytes;
-  if (a.n_groups > 0 && (own.rows == kTile2 || most_saved < (double)kMinSaved || shared.cap + rows * a.Hk > room)) a.n_groups = 0;
-  if (a.n_groups == 0) shared.cap = 0;
-  own.cap = room - shared.cap;
+  const AttendRule rule = rule_for(kTiles, a.total_q, a.G, a.Hk, a.n_seqs, a.n_groups, a.max_q_len, a.max_kv_len, a.key_bytes, ws.part_rows);
+  const AttendCut own = rule.own, shared = rule.shared;
+  if (!rule.groups) a.n_groups = 0;
   Partials po, ps;
   ps.o = ws.part;
   ps.mz = ws.part_mz;
@@ -1451,15 +1421,15 @@ hipError_t launch_d(const PagedWorkspace& ws, const AttendArgs& args, hipStream_
   po.group = ws.group;
   po.cut = ps.cut = ws.cut;
   ps.arrived = nullptr;
-  // Few pieces are joined by the workgroup that brings the last one.
-  po.arrived = a.n_groups == 0 && own.rows == kSplit && a.max_kv_len <= kJoinKeys ? ws.arrived + shared.cap : nullptr;
+  po.arrived = rule.joined ? ws.arrived + shared.cap : nullptr;
   hipError_t e = hipErrorInvalidValue;
   const int ks = a.n_groups > 0 ? shared.rows : kNone;
+  const bool once = rule.most <= kSplit;                   // a sequence's keys are read by one tile of rows
   if constexpr (kTiles) {
     if (ks == kNone) {
       e = own.rows == kTile2   ? launch_kinds<T, D, kTile2, kNone, true>(a, own, shared, po, ps, st)
           : own.rows == kTile1 ? launch_kinds<T, D, kTile1, kNone, true>(a, own, shared, po, ps, st)
-          : most <= kSplit     ? launch_kinds<T, D, kSplit, kNone, true>(a, own, shared, po, ps, st)
+          : once               ? launch_kinds<T, D, kSplit, kNone, true>(a, own, shared, po, ps, st)
                                : launch_kinds<T, D, kSplit, kNone, false>(a, own, shared, po, ps, st);
     } else if (own.rows == kTile1) {
       e = ks == kTile2   ? launch_kinds<T, D, kTile1, kTile2, true>(a, own, shared, po, ps, st)
@@ -1471,8 +1441,8 @@ hipError_t launch_d(const PagedWorkspace& ws, const AttendArgs& args, hipStream_
                          : launch_kinds<T, D, kSplit, kSplit, false>(a, own, shared, po, ps, st);
     }
   } else if (ks == kNone) {
-    e = most <= kSplit ? launch_kinds<T, D, kSplit, kNone, true>(a, own, shared, po, ps, st)
-                       : launch_kinds<T, D, kSplit, kNone, false>(a, own, shared, po, ps, st);
+    e = once ? launch_kinds<T, D, kSplit, kNone, true>(a, own, shared, po, ps, st)
+             : launch_kinds<T, D, kSplit, kNone, false>(a, own, shared, po, ps, st);
   } else {
     e = launch_kinds<T, D, kSplit, kSplit, false>(a, own, shared, po, ps, st);
   }

@@ -26,6 +26,16 @@ int main() {
       bool ok = held % w == 0;
       for (int e = 0; e < D + 64; ++e) ok = ok && hit[e] == (e < d ? 1 : 0);
       std::printf("%d %d\n", ok ? 1 : 0, w);
+    } else if (!std::strcmp(what, "rule")) {
+      // whether there are tiles, query tokens, G, Hk, sequences, groups, most queries and keys, bytes of a key, room; then the groups'
+      // shared keys: kinds of own and shared segments, whether the host leaves groups on, whether the device does, joined in the launch
+      const bool tiles = num() != 0;
+      const long long total = num();
+      const int G = (int)num(), Hk = (int)num(), seqs = (int)num(), groups = (int)num(), mq = (int)num(), mk = (int)num(), bytes = (int)num();
+      const long long room = num(), keys = num();
+      const asl::AttendRule r = asl::rule_for(tiles, total, G, Hk, seqs, groups, mq, mk, bytes, room);
+      std::printf("%d %d %d %d %d\n", r.own.rows, r.shared.rows, r.groups ? 1 : 0, asl::groups_pay((unsigned long long)keys, bytes) ? 1 : 0,
+                  r.joined ? 1 : 0);
     } else if (!std::strcmp(what, "room")) {
       // n limits (query rows, head size) in turn: the room after each
       asl::PagedRoom r = {0, 0};

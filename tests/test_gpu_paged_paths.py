@@ -1,12 +1,22 @@
 """The paged calls on the GPU where their paths part: head sizes that leave a part of a store,
-limits that change."""
+limits that change, work items of every kind."""
 import numpy as np
 import pytest
 
+import paged_paths
 from paper_2601_07667_amd import asl
-from test_gpu_paged import Cache, _check, _dt, _ints, _oracle, _queries, ctx  # noqa: F401
+from test_gpu_paged import Cache, _attend, _check, _dt, _ints, _oracle, _queries, ctx, wide  # noqa: F401
 
 pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def wide_heads(gpu_device):
+    c = asl.Asl(2, 1, 1)
+    c.asl_paged_reserve(4096, 1 << 17, 256)
+    yield c
+    assert c.asl_device_fault() == 0
+    c.close()
 
 
 @pytest.mark.parametrize("dtype,d", [("f32", 68), ("f32", 100), ("f32", 132), ("f32", 252), ("f32", 4), ("f32", 60),
@@ -111,3 +121,51 @@ def test_graphs_captured_before_new_limits_keep_their_workspace(gpu_device):
             assert all(torch.equal(a, b) for a, b in zip(outs + lses, want)), limit
     assert x.asl_device_fault() == 0
     x.close()
+
+
+# ----------------------------------------------------------------------------------- work items of every kind
+def _cache(dev, c, seed):
+    """The case's rows.  A group's members read its prefix from their first one's pages: their own table entries for the whole tiles of it
+    lead to a page of NaN, so that a call that does not read them apart shows."""
+    lens, groups, ps = c["lens"], c["groups"] or [], c["ps"]
+    x = Cache(dev, lens, c["Hk"], c["d"], ps, c["dtype"], seed)
+    at, poison = 0, next((p for p in range(x.n_pages) if x.refs_host[p] == 0))
+    table = x.host_table.copy()
+    for m, p in groups:
+        tokens = min(p, lens[at]) // 64 * 64 if m > 1 else 0
+        for r in range(at + 1, at + m):
+            n = min(p, lens[r])
+            for pages in x.pages_t:                          # the same tokens
+                for t in range(0, -(-n // ps)):
+                    part = min(ps, n - t * ps)
+                    pages[x.host_table[r, t], :, :part] = pages[x.host_table[at, t], :, :part]
+            if tokens >= 128:
+                table[r, :tokens // ps] = poison
+        at += m
+    x.table = _ints(table, dev)
+    assert bool(x.k[poison].isnan().all())
+    return x
+
+
+def _run(ctx, dev, c, x, q):
+    groups = c["groups"]
+    return _attend(ctx, x, q, c["n_q"], c["Hq"], c["causal"], groups, max_kv=c["max_kv"])
+
+
+@pytest.mark.parametrize("c", paged_paths.shared_cases(), ids=lambda c: c["name"])
+def test_prefixes_that_are_read_apart(wide, wide_heads, gpu_device, c):
+    x = _cache(gpu_device, c, 41)
+    q = _queries(sum(c["n_q"]), c["Hq"], c["d"], c["dtype"], gpu_device, 42)
+    ctx = wide if c["d"] <= 128 else wide_heads
+    out, lse = _run(ctx, gpu_device, c, x, q)
+    _check(out, lse, _oracle(x, q, c["n_q"], causal=c["causal"]), c["d"], max(c["lens"]), c["dtype"], c["name"])
+    assert ctx.asl_device_fault() == 0
+
+
+@pytest.mark.parametrize("c", paged_paths.tile_cases(), ids=lambda c: c["name"])
+def test_tiles(wide, gpu_device, c):
+    x = _cache(gpu_device, c, 43)
+    q = _queries(sum(c["n_q"]), c["Hq"], c["d"], c["dtype"], gpu_device, 44)
+    out, lse = _run(wide, gpu_device, c, x, q)
+    _check(out, lse, _oracle(x, q, c["n_q"], causal=c["causal"]), c["d"], max(c["lens"]), c["dtype"], c["name"])
+    assert wide.asl_device_fault() == 0

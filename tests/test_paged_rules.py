@@ -7,6 +7,7 @@ import subprocess
 
 import pytest
 
+import paged_paths
 from paper_2601_07667_amd import asl as libasl
 from test_bound import ROOT
 
@@ -51,6 +52,29 @@ def test_a_workspace_is_outgrown_seven_times_at_most(client):
     slowly = [(4096 << i, 64) for i in range(6)] + [(1, 128), (1, 256)]
     rooms = client(["room %d %s" % (len(slowly), " ".join("%d %d" % x for x in slowly))])
     assert most <= 7 and len(set(rooms)) - 1 == 7 == int(client(["kept"])[0])
+
+
+def _rule(client, c):
+    e, groups = (2 if c["dtype"] == "bf16" else 4), c["groups"] or []
+    saved, at = 0, 0
+    for m, p in groups:                                      # whole tiles of what is stated and there, two of them at least
+        tokens = min(p, c["lens"][at]) // 64 * 64
+        saved += (m - 1) * tokens if m > 1 and tokens >= 128 else 0
+        at += m
+    got = client(["rule %d %d %d %d %d %d %d %d %d %d %d" % (
+        c["dtype"] == "bf16" and c["d"] <= 128, sum(c["n_q"]), c["Hq"] // c["Hk"], c["Hk"], len(c["lens"]), len(groups), max(c["n_q"]),
+        c["max_kv"], 2 * c["d"] * e * c["Hk"], 2 * (1 << 17) + 131072, saved)])[0]
+    own, shared, host, device, joined = map(int, got.split())
+    return (own, shared if host and device else 0), joined
+
+
+def test_the_cases_take_the_kernels_that_they_are_for(client):
+    cases = paged_paths.shared_cases() + paged_paths.tile_cases()
+    for c in cases:
+        kinds, joined = _rule(client, c)
+        assert kinds == c["kinds"] and not joined, c["name"]
+    taken = {c["kinds"] for c in cases}
+    assert taken >= {(16, 16), (16, 64), (16, 128), (64, 16), (64, 64), (64, 128), (64, 0), (128, 0)}
 
 
 # ------------------------------------------------------------------------------------------------- the binding
