@@ -72,3 +72,22 @@ def tile_cases():
     out.append(case("one sequence that sees little", (128, 0), [1500, 20, 1], [100, 300, 200], 4, 2, 128, max_kv=WIDE))
     out.append(case("cross", (128, 0), [4000, 1, 129], [90, 90, 40], 8, 2, 128, causal=False))
     return out
+
+
+LEAP_PREFIX = 3328
+
+
+def leap_cases():
+    """Every pair of kinds, 4 query heads on each of 8 KV heads; for d = 64 those of tiles."""
+    P, out = LEAP_PREFIX, []
+    for d in (64, 128, 80):
+        for kinds, groups, n_q in (((64, 0), None, [16] * 3), ((128, 0), None, [33] * 3), ((16, 16), [(24, P)], [1] * 24),
+                                   ((16, 64), [(12, P)] * 2, [1] * 24), ((16, 128), [(24, P)], [1] * 24),
+                                   ((64, 16), [(3, P)] * 12, [6] + [1] * 35), ((64, 64), [(12, P)] * 2, [1] * 20 + [6] + [1] * 3),
+                                   ((64, 128), [(24, P)], [1] * 9 + [16] + [1] * 14)):
+            if d == 64 and 16 in kinds:
+                continue
+            lens = [P + 40 + 3 * (i % 50) for i in range(len(n_q))]
+            out.append(case("leaps, d = %d, kinds %d and %d" % ((d,) + kinds), kinds, lens, n_q, 32, 8, d, 64, groups=groups,
+                            max_kv=None if kinds == (16, 16) else WIDE))
+    return out

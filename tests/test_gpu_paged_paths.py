@@ -5,7 +5,7 @@ import pytest
 
 import paged_paths
 from paper_2601_07667_amd import asl
-from test_gpu_paged import Cache, _attend, _check, _dt, _ints, _oracle, _queries, ctx, wide  # noqa: F401
+from test_gpu_paged import Cache, _attend, _bounds, _check, _dt, _ints, _oracle, _queries, ctx, wide  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -168,4 +168,94 @@ def test_tiles(wide, gpu_device, c):
     q = _queries(sum(c["n_q"]), c["Hq"], c["d"], c["dtype"], gpu_device, 44)
     out, lse = _run(wide, gpu_device, c, x, q)
     _check(out, lse, _oracle(x, q, c["n_q"], causal=c["causal"]), c["d"], max(c["lens"]), c["dtype"], c["name"])
+    assert wide.asl_device_fault() == 0
+
+
+def _same_where_seen(out, lse, ref, d, n_keys, dtype, what):
+    """Like _check, with infinities and NaN where the oracle has them."""
+    o, l = out.double().cpu().numpy(), lse.double().cpu().numpy()
+    with np.errstate(invalid="ignore"):
+        tol, tol_lse = _bounds(d, n_keys, dtype, ref)
+        finite = np.isfinite(ref[0])
+        assert np.array_equal(o[~finite], ref[0][~finite], equal_nan=True), (what, "not finite")
+        assert np.all(np.abs(o - ref[0])[finite] <= tol[finite]), (what, "out")
+        seen = np.isfinite(ref[1])
+        assert np.array_equal(l[~seen], ref[1][~seen], equal_nan=True), (what, "lse of rows without keys")
+        assert np.all(np.abs(l - ref[1])[seen] <= tol_lse[seen]), (what, "lse")
+
+
+ODD = [c for c in paged_paths.tile_cases() if c["causal"] and max(c["n_q"]) >= 17 and c["d"] >= 64] + [
+    c for c in paged_paths.shared_cases() if c["name"] in ("members of any length", "drafts", "tiles for both", "tiles beside split prefixes")]
+
+
+@pytest.mark.filterwarnings("ignore:invalid value encountered")
+@pytest.mark.parametrize("c", ODD, ids=lambda c: "%s, %d %d" % ((c["name"],) + c["kinds"]))
+def test_values_that_are_no_numbers_reach_those_that_see_them(wide, gpu_device, c):
+    """Infinities of either sign and NaN among the values, where some queries of a sequence see them and others do not, and in sight of all:
+    each reaches its element of the queries that see it.  NaN, infinite and lowest keys and values behind what any query sees reach nobody."""
+    import torch
+    x = _cache(gpu_device, c, 45)
+    q = _queries(sum(c["n_q"]), c["Hq"], c["d"], c["dtype"], gpu_device, 46, spread=1.0)
+    inf, nan, ps = float("inf"), float("nan"), c["ps"]
+    lowest = torch.finfo(torch.bfloat16).min
+    firsts, at = {}, 0                                       # whose pages hold a member's prefix
+    for m, p in c["groups"] or []:
+        tokens = min(p, c["lens"][at]) // 64 * 64 if m > 1 else 0
+        firsts.update({r: (at, min(tokens, c["lens"][r]) if tokens >= 128 else 0) for r in range(at, at + m)})
+        at += m
+
+    def put(r, t, e, value, of=x.v):
+        """Token t of row r, in its own pages and, of a prefix, in those of every member that has it."""
+        a, shared = firsts.get(r, (r, 0))
+        rows = [s for s in firsts if firsts[s][0] == a and t < c["lens"][s]] if t < shared else [r]
+        for s in rows:
+            of[x.host_table[s, t // ps], 0, t % ps, e] = value
+
+    for r, (L, n) in enumerate(zip(c["lens"], c["n_q"])):
+        if L < 3 or n < 3:
+            continue
+        d, last = c["d"], min(n, L)
+        put(r, L - 1, 1, inf)                                # the last query alone sees it
+        put(r, L - last // 2 - 1, 5 % d, -inf)
+        put(r, L - last // 2 - 1, d - 1, nan)
+        put(r, L - 2, 6, inf)
+        put(r, L - 1, 6, -inf)                               # the last query: NaN
+        put(r, 0, 7, inf)                                    # all
+        put(r, L // 2, d // 2, -inf)
+    want = _oracle(x, q, c["n_q"], causal=True)
+    for r, L in enumerate(c["lens"]):                        # slots behind a row's end
+        if L % ps:
+            for of, values in ((x.k, (nan, inf, -inf, lowest)), (x.v, (inf, lowest, nan, -inf))):
+                for i, value in enumerate(values):
+                    of[x.host_table[r, L // ps], :, L % ps + i:L % ps + i + 1] = value
+    out, lse = _run(wide, gpu_device, c, x, q)
+    _same_where_seen(out, lse, want, c["d"], max(c["lens"]), c["dtype"], c["name"])
+    assert not np.isfinite(want[0]).all() and wide.asl_device_fault() == 0
+
+
+@pytest.mark.parametrize("c", paged_paths.leap_cases(), ids=lambda c: c["name"])
+def test_logits_that_rise_from_tile_to_tile(wide, gpu_device, c):
+    """For the first KV head the largest logit of some rows grows by tens and hundreds of nats from tile to tile, in sight of all and among
+    the last tokens; for the second it falls; for the last the first 80 tokens and one of the last have logits of -Inf in fp32."""
+    import torch
+    x = _cache(gpu_device, c, 47)
+    lens, n_q, d, Hk, ps, P = c["lens"], c["n_q"], c["d"], c["Hk"], c["ps"], paged_paths.LEAP_PREFIX
+    G = c["Hq"] // Hk
+    lowest = [*range(80), P + 1]
+    for r in range(len(lens)):
+        for t, size in ((70, 2.0), (130, 4.0), (200, 8.0), (420, 9.0), (P - 1, 12.0), (P + 3, 16.0), (P + 20, 24.0)):
+            x.k[x.host_table[r, t // ps], 0, t % ps] = size
+            x.k[x.host_table[r, t // ps], 1, t % ps] = -size
+        for t in lowest:
+            x.k[x.host_table[r, t // ps], Hk - 1, t % ps] = 0
+    q = _queries(sum(n_q), c["Hq"], d, "bf16", gpu_device, 48, spread=0.5)
+    q[:, :2 * G:3] = q[:, :2 * G:3].abs() * 2 + 1
+    q[:, -G:] = q[:, -G:].abs() + 0.5
+    reach = _oracle(x, q, n_q)[3]                            # without the keys that count for nothing
+    for r in range(len(lens)):
+        for t in lowest:
+            x.k[x.host_table[r, t // ps], Hk - 1, t % ps] = torch.finfo(torch.bfloat16).min
+    want = _oracle(x, q, n_q)
+    out, lse = _run(wide, gpu_device, c, x, q)
+    _check(out, lse, (want[0], want[1], want[2], reach), d, max(lens), "bf16", c["name"])
     assert wide.asl_device_fault() == 0
