@@ -359,8 +359,8 @@ asl_status asl_pages_compact(asl_ctx* ctx, const asl_pages* pages, const int32_t
  * n_groups > 0: sequences group_start[g] .. group_start[g+1]-1 have their first prefix_len[g] tokens in common (their rows
  * begin with the same pages, or with copies); those are read once for all of the group's queries.  group_start [n_groups+1]
  * int32 ascending from 0 to n_seqs.  The result is that of n_groups = 0 up to rounding.
- * Products take bf16 (fp32) operands and are summed in fp32 (values beyond 2^100 may overflow there); softmax and sums are fp32
- * and of a fixed order; in bf16 a probability is rounded to 8 bits before its product with v.  Masked keys and slots behind
+ * Products take bf16 (fp32) operands and are summed in fp32, ahead of the division and with probabilities of up to 2^24: over n keys,
+ * values of 2^103 / n and more may overflow there.  Softmax and sums are fp32 and of a fixed order; in bf16 a probability is rounded to 8 bits before its product with v.  Masked keys and slots behind
  * a sequence's end may hold anything.  d: multiples of 16 bytes up to 256 elements. */
 asl_status asl_paged_attention(asl_ctx* ctx, const asl_pages* pages, const asl_attn* attn, const void* q, const void* k_pages,
                                const void* v_pages, const int32_t* rows, const int32_t* table, const int32_t* kv_len,

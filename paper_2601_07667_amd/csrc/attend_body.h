@@ -42,8 +42,8 @@ constexpr float kLn2 = 0.6931471805599453f;
 // blocks need no maximum over lanes and no rescaling.
 constexpr float kSlack = 8.f;
 // The same where a row's reference cannot move in place: probabilities up to 2^24 lose nothing in fp32 and bf16 (a result is a
-// quotient of two such sums; it is values beyond 2^100 whose sums overflow), and only rows whose first tile was that much lower
-// than a later one need the step that moves it.
+// quotient of two such sums; over n keys sums of values below 2^103 / n stay below 2^128), and only rows whose first tile was that
+// much lower than a later one need the step that moves it.
 constexpr float kWideSlack = 24.f;
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }

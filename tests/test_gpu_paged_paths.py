@@ -259,3 +259,19 @@ def test_logits_that_rise_from_tile_to_tile(wide, gpu_device, c):
     out, lse = _run(wide, gpu_device, c, x, q)
     _check(out, lse, (want[0], want[1], want[2], reach), d, max(lens), "bf16", c["name"])
     assert wide.asl_device_fault() == 0
+
+
+@pytest.mark.parametrize("kinds,n_q,max_kv,dtype", [((16, 0), 1, None, "f32"), ((16, 0), 4, None, "bf16"), ((64, 0), 16, paged_paths.WIDE, "bf16"),
+                                                   ((128, 0), 33, paged_paths.WIDE, "bf16")])
+def test_values_up_to_the_stated_size_do_not_overflow(wide, gpu_device, kinds, n_q, max_kv, dtype):
+    """n keys, values just below 2^103 / n, and logits that rise by 23.4 bits behind the first tile, where a reference stays."""
+    n = 4096
+    c = paged_paths.case("large values", kinds, [n], [n_q], 4, 1, 64, max_kv=max_kv, dtype=dtype)
+    x = _cache(gpu_device, c, 51)
+    q = _queries(n_q, 4, 64, dtype, gpu_device, 52) * 0 + 1
+    for t in range(n):
+        x.k[x.host_table[0, t // 16], 0, t % 16] = 0.0 if t < 64 else 2.03125
+        x.v[x.host_table[0, t // 16], 0, t % 16] = 0.99 * 2.0 ** 91 * (1 if t % 3 else -1)
+    out, lse = _run(wide, gpu_device, c, x, q)
+    _check(out, lse, _oracle(x, q, [n_q]), 64, n, dtype, "large values")
+    assert wide.asl_device_fault() == 0
