@@ -70,6 +70,7 @@ def tile_cases():
         out.append(case("cut, pages of %d" % ps, (128, 0), [5000, 700, 65], [70, 19, 65], 8, 2, 128, ps))
         out.append(case("cut, 64 rows, pages of %d" % ps, (64, 0), [4100, 1700, 64], [16, 15, 9], 8, 2, 64, ps, max_kv=WIDE))
     out.append(case("one sequence that sees little", (128, 0), [1500, 20, 1], [100, 300, 200], 4, 2, 128, max_kv=WIDE))
+    out.append(case("a chunk beside decoding", (128, 0), [3000] + _own(40, 20, 1, 900), [300] + [1] * 40, 8, 2, 128, 64))
     out.append(case("cross", (128, 0), [4000, 1, 129], [90, 90, 40], 8, 2, 128, causal=False))
     return out
 
@@ -91,3 +92,14 @@ def leap_cases():
             out.append(case("leaps, d = %d, kinds %d and %d" % ((d,) + kinds), kinds, lens, n_q, 32, 8, d, 64, groups=groups,
                             max_kv=None if kinds == (16, 16) else WIDE))
     return out
+
+
+def large_cases():
+    """Calls of more rows than the workspace's pieces grow with (131072): many queries, and so many sequences behind a prefix that there is
+    room for their rows' own and shared parts, but for no further piece of the long one among them."""
+    n = 4095
+    return [
+        case("192000 rows", (128, 0), [70, 64, 1, 90, 0, 33, 300, 65], [600] * 8, 40, 8, 64, causal=False, max_kv=WIDE),
+        case("171990 rows behind a prefix", (16, 128), [130 + (10000 if i == 77 else 1 + i % 20) for i in range(n)], [1] * n, 42, 6, 64,
+             groups=[(n, 130)], max_kv=WIDE),
+    ]

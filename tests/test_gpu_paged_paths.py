@@ -275,3 +275,15 @@ def test_values_up_to_the_stated_size_do_not_overflow(wide, gpu_device, kinds, n
     out, lse = _run(wide, gpu_device, c, x, q)
     _check(out, lse, _oracle(x, q, [n_q]), 64, n, dtype, "large values")
     assert wide.asl_device_fault() == 0
+
+
+@pytest.mark.parametrize("c", paged_paths.large_cases(), ids=lambda c: c["name"])
+def test_more_rows_than_the_workspace_grows_with(gpu_device, c):
+    ctx = asl.Asl(2, 1, 1)
+    ctx.asl_paged_reserve(4096, 1 << 18, 64)
+    x = _cache(gpu_device, c, 53)
+    q = _queries(sum(c["n_q"]), c["Hq"], c["d"], c["dtype"], gpu_device, 54)
+    out, lse = _run(ctx, gpu_device, c, x, q)
+    _check(out, lse, _oracle(x, q, c["n_q"], causal=c["causal"]), c["d"], max(c["lens"]), c["dtype"], c["name"])
+    assert ctx.asl_device_fault() == 0
+    ctx.close()

@@ -69,7 +69,7 @@ def _rule(client, c):
 
 
 def test_the_cases_take_the_kernels_that_they_are_for(client):
-    cases = paged_paths.shared_cases() + paged_paths.tile_cases() + paged_paths.leap_cases()
+    cases = paged_paths.shared_cases() + paged_paths.tile_cases() + paged_paths.leap_cases() + paged_paths.large_cases()
     for c in cases:
         kinds, joined = _rule(client, c)
         assert kinds == c["kinds"] and not joined, c["name"]
