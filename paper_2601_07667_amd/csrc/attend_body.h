@@ -541,42 +541,39 @@ struct Rows {
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
       for (int t = 0; t < B::SUB; ++t) x[mt][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-    // fp32: a score is summed in four chains of d / 16 products, since a chain's roundings grow with its length and a score's error is
-    // its probability's.  Relative error of out against 64 bits at 300 .. 20000 keys, one chain / two / four: 4.8e-7 .. 8.9e-7 /
-    // 3.3e-7 .. 6.1e-7 / 2.6e-7 .. 5.1e-7 for d = 64, 1.0e-6 .. 1.6e-6 / 6.2e-7 .. 1.1e-6 / 4.2e-7 .. 6.4e-7 for d = 256, in the same time
-    // (150 / 154 / 153 us for 3 x 100 rows of 16 heads of d = 128 on 3000 keys).  (Summing out by blocks of 16 keys as well takes 5.6e-7 to
-    // 4.6e-7 there, but 221 us.)
-    f32x4 part[MT][B::SUB][3];
-    if constexpr (!B::kBf16) {
+    if constexpr (B::kBf16) {
 #pragma unroll
-      for (int mt = 0; mt < MT; ++mt)
+      for (int p = 0; p < B::KP; ++p)
 #pragma unroll
         for (int t = 0; t < B::SUB; ++t)
 #pragma unroll
-          for (int u = 0; u < 3; ++u) part[mt][t][u] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
-#pragma unroll
-    for (int p = 0; p < B::KP; ++p)
-#pragma unroll
-      for (int t = 0; t < B::SUB; ++t)
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-          if constexpr (B::kBf16) {
+          for (int mt = 0; mt < MT; ++mt)
             x[mt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, b.k[t][p]),
                                                                __builtin_bit_cast(bf16x8, q[mt][p]), x[mt][t], 0, 0, 0);
-          } else {
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-              f32x4& to = u == 0 ? x[mt][t] : part[mt][t][u - 1];
-              to = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(b.k[t][p][u]), __uint_as_float(q[mt][p][u]), to, 0, 0, 0);
-            }
-          }
-        }
-    if constexpr (!B::kBf16) {
+    } else {
+      // A score is summed in four chains of d / 16 instructions, since a chain's roundings grow with its length and a score's error is its
+      // probability's.  Relative error of out against 64 bits at 300 .. 20000 keys, one chain / four: 4.8e-7 .. 8.9e-7 / 2.6e-7 .. 5.1e-7
+      // for d = 64, 1.0e-6 .. 1.6e-6 / 3.7e-7 .. 6.4e-7 for d = 256.  One chain after the other, over neighbouring elements: with all
+      // four open the kernels of d = 128 spill (3 x 100 rows of 16 heads on 3000 keys 149 us, so 141, one chain 143; 16 sequences of 3000
+      // keys 45.6, 43.5, 44.1).  (Summing out by blocks of 16 keys as well takes 5.6e-7 to 4.6e-7 there, but half as long again.)
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-        for (int t = 0; t < B::SUB; ++t) x[mt][t] = (x[mt][t] + part[mt][t][0]) + (part[mt][t][1] + part[mt][t][2]);
+        for (int t = 0; t < B::SUB; ++t) {
+          f32x4 pair = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            f32x4 y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int p = c * B::KP / 4; p < (c + 1) * B::KP / 4; ++p)
+#pragma unroll
+              for (int u = 0; u < 4; ++u)
+                y = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(b.k[t][p][u]), __uint_as_float(q[mt][p][u]), y, 0, 0, 0);
+            pair = c % 2 == 0 ? y : pair + y;
+            if (c == 1) x[mt][t] = pair;
+          }
+          x[mt][t] += pair;
+        }
     }
     float p[MT][B::SUB][4];
 #pragma unroll
