@@ -1,4 +1,4 @@
-// How the work of an attention call is cut: index arithmetic for device and host.
+// How the work of an attention call is cut, and which kernels take it: arithmetic for device and host.
 //
 // The queries of a sequence that share a KV head are its rows (token-major: row = token * G + head of the group), the keys that only
 // it sees its span, in tiles of kKeyTile.  A group with a shared prefix has a second such segment: the rows of all its sequences over
