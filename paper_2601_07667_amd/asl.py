@@ -157,6 +157,16 @@ def _refuse_gaps(**tensors) -> None:
             raise AslError(ASL_EUNSUPPORTED, f"the last dimension of {name} must be contiguous (its stride is {t.stride(2)})")
 
 
+def _index_rows(idx, total: int) -> int:
+    """The rows of idx [1 or Hk, total], which the calls read as they follow one another without a gap."""
+    rows, n = idx.shape
+    outer, inner = idx.stride()
+    if n < total or (inner != 1 and total > 1) or (outer != total and rows > 1):
+        raise AslError(ASL_EINVAL, f"idx must be [1 or Hk, {total}] without gaps (its shape is {tuple(idx.shape)}, "
+                                   f"its strides {tuple(idx.stride())})")
+    return rows
+
+
 def _stream() -> int:
     """Handle of the calling thread's current stream on its current device, without the Stream object that
     torch.cuda.current_stream() makes (2.9 us of a call whose one launch takes 2.5; so 0.1 us)."""
@@ -304,7 +314,7 @@ class Asl:
             _refuse_gaps(k=k, v=v)
         if v.shape != k.shape:
             raise AslError(ASL_EINVAL, f"k and v differ in shape: {tuple(k.shape)}, {tuple(v.shape)}")
-        src = AslRows(k.shape[1], 0 if idx is None else idx.shape[0], kh, kt, vh, vt)
+        src = AslRows(k.shape[1], 0 if idx is None else _index_rows(idx, total), kh, kt, vh, vt)
         self._check(self.lib.asl_pages_write(self.h, C.byref(pages), C.byref(src), _ptr(k), _ptr(v), _ptr(rows), _ptr(cu), n,
                                              total, _ptr(idx), _ptr(table), _ptr(kv_len), _ptr(k_pages), _ptr(v_pages),
                                              _stream()))
@@ -313,7 +323,7 @@ class Asl:
                           v_pages) -> None:
         """idx: [1 or Hk, total]."""
         self._check(self.lib.asl_pages_compact(self.h, C.byref(pages), _ptr(src_rows), _ptr(dst_rows), _ptr(cu), n, total,
-                                               _ptr(idx), idx.shape[0], _ptr(table), _ptr(kv_len), _ptr(k_pages),
+                                               _ptr(idx), _index_rows(idx, total), _ptr(table), _ptr(kv_len), _ptr(k_pages),
                                                _ptr(v_pages), _stream()))
 
     def asl_paged_attention(self, pages: AslPages, attn: AslAttn, q, k_pages, v_pages, table, kv_len, cu_q, out, lse=None,
@@ -324,6 +334,8 @@ class Asl:
         a.out_stride_tok, a.out_stride_head, out1 = out.stride()
         if q1 != 1 or out1 != 1:
             _refuse_gaps(q=q, out=out)
+        if lse is not None and not lse.is_contiguous():
+            raise AslError(ASL_EUNSUPPORTED, f"lse must be without gaps (its strides are {tuple(lse.stride())})")
         self._check(self.lib.asl_paged_attention(self.h, C.byref(pages), C.byref(a), _ptr(q), _ptr(k_pages), _ptr(v_pages),
                                                  _ptr(rows), _ptr(table), _ptr(kv_len), _ptr(cu_q), _ptr(group_start),
                                                  _ptr(prefix_len), _ptr(out), _ptr(lse), _stream()))

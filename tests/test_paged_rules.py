@@ -82,7 +82,7 @@ class _Recorder:
     """Stands in for the library: keeps what the paged calls are given."""
 
     def __init__(self):
-        self.attn, self.rows = [], []
+        self.attn, self.rows, self.idx_rows = [], [], []
 
     def asl_paged_attention(self, h, pages, attn, *pointers):
         self.attn.append(libasl.AslAttn.from_buffer_copy(attn._obj))
@@ -90,6 +90,10 @@ class _Recorder:
 
     def asl_pages_write(self, h, pages, src, *rest):
         self.rows.append(libasl.AslRows.from_buffer_copy(src._obj))
+        return libasl.ASL_OK
+
+    def asl_pages_compact(self, h, pages, src, dst, cu, n, total, idx, idx_rows, *rest):
+        self.idx_rows.append(idx_rows)
         return libasl.ASL_OK
 
     def asl_destroy(self, h):
@@ -145,3 +149,30 @@ def test_rows_that_are_not_contiguous_are_refused(recorded):
     write(k.transpose(0, 1).contiguous().transpose(0, 1), k)
     src = recorded.lib.rows[0]
     assert (src.n_src, src.k_stride_head, src.k_stride_tok, src.v_stride_head, src.v_stride_tok) == (3, 8, 16, 24, 8)
+
+
+def test_indices_and_normalisers_with_gaps_are_refused(recorded):
+    """What a selection leaves is [Hk + 1, k + W]: a slice of its columns is no list that the calls can read."""
+    import torch
+    pages, i = libasl.make_pages(2, 2, 8, 16, 1, 1, 1), torch.zeros(4, dtype=torch.int32)
+    k, picked = torch.zeros(2, 9, 8), torch.zeros(3, 6, dtype=torch.int32)
+    calls = (lambda idx, n: recorded.asl_pages_write(pages, k, k, i, i, 1, n, i, i, k, k, idx=idx),
+             lambda idx, n: recorded.asl_pages_compact(pages, i, i, i, 1, n, idx, i, i, k, k))
+    for call in calls:
+        for idx, n in ((picked[:2, :4], 4), (picked[:2], 4), (picked[:2], 7), (picked[:1], 7), (picked[:2, ::2], 3), (picked[:1, ::2], 3),
+                       (picked.t()[:2], 3), (picked[:2, :1], 1)):
+            with pytest.raises(libasl.AslError, match="idx") as e:
+                call(idx, n)
+            assert e.value.status == libasl.ASL_EINVAL
+        for idx, n in ((picked[:2], 6), (picked[2:], 6), (picked[:1], 4), (picked[:1, :4], 4), (picked[:1, ::2], 1), (picked[:2, :1].contiguous(), 1),
+                       (picked[:1, :0], 0)):
+            call(idx, n)
+    assert [r.idx_rows for r in recorded.lib.rows] == recorded.lib.idx_rows == [2, 1, 1, 1, 1, 2, 1]
+    attn, q, lse = libasl.make_attn(1, 3, 3, 100), torch.zeros(3, 4, 8), torch.zeros(4, 5)
+    attend = lambda lse: recorded.asl_paged_attention(libasl.make_pages(4, 2, 8, 16, 1, 1, 1), attn, q, q, q, i, i, i, q, lse=lse)
+    for bad in (lse[:, :3], lse[:, 4:], lse.t()):
+        with pytest.raises(libasl.AslError, match="lse") as e:
+            attend(bad)
+        assert e.value.status == libasl.ASL_EUNSUPPORTED
+    attend(lse), attend(None)
+    assert len(recorded.lib.attn) == 2
