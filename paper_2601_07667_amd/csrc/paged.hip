@@ -421,10 +421,9 @@ hipError_t launch_pages_write(const PagesWriteArgs& args, int Hk, hipStream_t st
 hipError_t launch_pages_fork(const PagesForkArgs& a, int32_t* fresh, hipStream_t st) {
   if (a.n == 0) return hipSuccess;
   hipLaunchKernelGGL(pages_fork_kernel, dim3(1), dim3(kBookThreads), 0, st, a, fresh);
-  const int64_t pieces = (int64_t)(a.map.ps - 1) * a.cpr * a.Hk;
+  const int64_t pieces = (int64_t)(a.map.ps - 1) * a.cpr * a.Hk;   // at most 2^26 (asl_pages_fork)
   const dim3 grid((unsigned)((a.n + kForkGroup - 1) / kForkGroup), (unsigned)(1 + 2 * a.n_layers),
                   (unsigned)((pieces + kForkPieces - 1) / kForkPieces));
-  if (grid.z > 65535u) return hipErrorInvalidValue;
   hipLaunchKernelGGL(pages_fork_copy_kernel, grid, dim3(kWriteThreads), 0, st, a);
   return hipGetLastError();
 }

@@ -49,7 +49,6 @@ asl_status asl_paged_reserve(asl_ctx* ctx, int32_t max_seqs, int32_t max_query_r
   asl::PagedWorkspace& ws = ctx->paged;
   const asl::PagedRoom room = asl::room_for({ws.room_rows, ws.room_dim}, max_query_rows, max_head_dim);
   if (!ws.base || room.rows != ws.room_rows || room.dim != ws.room_dim) {
-    if (ws.base && ctx->n_paged_kept == asl::kPagedKept) return fail(ctx, ASL_ENOMEM, "limits were raised too often");
     DeviceGuard guard(ctx->device);
     if (guard.err != hipSuccess) return hip_fail(ctx, guard.err, "set device");
     asl::PagedWorkspace w = {};
@@ -91,7 +90,7 @@ asl_status asl_paged_reserve(asl_ctx* ctx, int32_t max_seqs, int32_t max_query_r
     w.part = (float*)(base + part);
     w.part_mz = (float2*)(base + part_mz);
     w.arrived = (uint32_t*)(base + arrived);
-    if (ws.base) ctx->paged_kept[ctx->n_paged_kept++] = ws.base;
+    if (ws.base) ctx->paged_kept[ctx->n_paged_kept++] = ws.base;   // kPagedKept times at most (room_for)
     ws = w;
   }
   ws.part_rows = part_rows(max_query_rows);
