@@ -213,7 +213,7 @@ def _inputs(c, seed):
             return s
     # a cache in use: no row's pages are neighbours
     width = max(ln.pages) + 1                                    # entries of a table row
-    shared = c["prefix"] // ps if op == "tree" and c["members"] > 1 else 0
+    shared = c["prefix"] // ps if op == "tree" and c["members"] > 1 else 0    # pages that a group's rows have in common
     held = ln.old_pages if op == "plan" else [p - shared for p in ln.pages]
     used = sum(held) + (shared * c["groups"] if shared else 0)
     if op == "plan":
@@ -255,7 +255,7 @@ def _inputs(c, seed):
     elif op == "tree":
         s["k_pages"], s["v_pages"] = normal(n_pages, c["Hk"], ps, c["d"]), normal(n_pages, c["Hk"], ps, c["d"])
         s["parent"] = ints(sum((_draft(m, host) for m in ln.n), []))
-        s |= dict(group_start=ints(_cumulative([c["members"]] * c["groups"])), prefix_len=ints([c["prefix"]] * c["groups"]))
+        s |= dict(group_start=ints(_cumulative([c["members"]] * c["groups"])), prefix_len=ints([shared * ps] * c["groups"]))
         s["q"] = normal(s["total"], c["Hq"], c["d"]) * 2         # logits with a spread of 2: some tokens stand out
         s["out"] = torch.empty_like(s["q"])
         s["lse"] = torch.empty((c["Hq"], s["total"]), dtype=torch.float32, device=dev)
