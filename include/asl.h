@@ -367,6 +367,117 @@ asl_status asl_paged_attention(asl_ctx* ctx, const asl_pages* pages, const asl_a
                                const int32_t* cu_q, const int32_t* group_start, const int32_t* prefix_len, void* out,
                                float* lse, void* stream);
 
+/* ---- Drafting over the paged cache ------------------------------------------------------------
+ * A decoding step that proposes several tokens of each sequence as a tree, attends over all of them at once and keeps one path:
+ *   asl_pages_plan     pages for the drafts, and of each node its slot and its position
+ *   asl_rotate_write   (each layer) rotary positions of q and k; k and v into the slots
+ *   asl_tree_attention (each layer) every node sees its sequence's context, its ancestors and itself
+ *   asl_pages_accept   the accepted path moves to the front of the draft, in all layers; the rest is given back
+ * The host reads none of the lists, so a step can be captured and replayed.  A draft is a sequence's last tokens, its nodes; node i's parent
+ * is an earlier node of the draft (parent < i) or -1, the context.  Positions are not places in the cache: pruning takes tokens out of a row,
+ * and those behind keep their positions.  These calls are of the paged family (workspace, fault word, limits of asl_paged_reserve);
+ * asl_rotate and asl_rotation_freqs are not and share nothing with any call. */
+
+/* Rotary positions: pair i of a head's first rot_dim elements, (a, b), becomes
+ *   (magnitude (a cos t - b sin t), magnitude (a sin t + b cos t)),  t = pos * freqs[i];
+ * the others stay as they are.  Angles are taken in 64 bits, for positions of any size. */
+#define ASL_PAIRS_HALVES 0      /* pair i: elements i and rot_dim / 2 + i      */
+#define ASL_PAIRS_NEIGHBOURS 1  /* pair i: elements 2 i and 2 i + 1            */
+/* The other way round, -t: the map's transpose, i.e. its gradient (and with magnitude 1 its inverse). */
+#define ASL_ROTATE_BACK 1
+typedef struct {
+  int32_t n_q_heads;      /* Hq, 0: no q                                       */
+  int32_t n_kv_heads;     /* Hk, 0: no k (asl_rotate)                          */
+  int32_t head_dim;       /* d, even, <= 2048                                  */
+  int32_t dtype;          /* asl_dtype of q, k, v and what comes of them       */
+  int32_t rot_dim;        /* elements of a head that are rotated, the first ones: even, 2 .. d */
+  int32_t pairs;          /* ASL_PAIRS_HALVES or ASL_PAIRS_NEIGHBOURS          */
+  int32_t flags;          /* ASL_ROTATE_BACK or 0                              */
+  float magnitude;        /* factor of cos and sin; <= 0 means 1               */
+  int64_t q_stride_tok;   /* element strides; d contiguous                     */
+  int64_t q_stride_head;
+  int64_t k_stride_tok;
+  int64_t k_stride_head;
+  int64_t v_stride_tok;   /* (asl_rotate_write)                                */
+  int64_t v_stride_head;
+  int64_t q_out_stride_tok;
+  int64_t q_out_stride_head;
+  int64_t k_out_stride_tok;   /* (asl_rotate)                                  */
+  int64_t k_out_stride_head;
+} asl_rotation;
+
+/* Frequencies f_i = base^(-2 i / rot_dim), scaled for contexts that are `factor` times longer than a model was made for:
+ *   ASL_FREQS_PLAIN   f_i
+ *   ASL_FREQS_LINEAR  f_i / factor
+ *   ASL_FREQS_BASE    of base * factor^(rot_dim / (rot_dim - 2)): the last pair's is divided by factor, the first one's is not
+ *   ASL_FREQS_PARTS   f_i (g + (1 - g) / factor), g = (n - low) / (high - low) between 0 and 1, n = context f_i / (2 pi) the pair's turns
+ *                     over the original context: pairs of many turns stay as they are, those of few are divided. */
+#define ASL_FREQS_PLAIN 0
+#define ASL_FREQS_LINEAR 1
+#define ASL_FREQS_BASE 2
+#define ASL_FREQS_PARTS 3
+typedef struct {
+  int32_t rot_dim;        /* even, >= 2                                        */
+  int32_t kind;           /* ASL_FREQS_*                                       */
+  double base;            /* > 0, e.g. 10000                                   */
+  double factor;          /* > 0                                               */
+  double context;         /* ASL_FREQS_PARTS: tokens of the original context   */
+  double low, high;       /* ASL_FREQS_PARTS: turns, low < high                */
+} asl_freqs;
+
+/* Writes freqs [rot_dim / 2], radians per position, to HOST memory (no context, no GPU).  ASL_EINVAL for numbers out of range. */
+asl_status asl_rotation_freqs(const asl_freqs* freqs, double* out);
+
+/* Rotates q and k of n tokens (Hq or Hk 0: that one may be NULL).
+ *   q, q_out [n, Hq, d], k, k_out [n, Hk, d] by the strides in rotation; an output may be its input (same strides), and must not overlap it
+ *          otherwise.  Rows, strides and addresses of 16 bytes are moved in 16-byte pieces, others in narrower ones.
+ *   pos    [n] int32, negative ones too;  freqs [rot_dim / 2] f64, both device memory.
+ * fp32 arithmetic, each output rounded once. */
+asl_status asl_rotate(asl_ctx* ctx, const asl_rotation* rotation, const void* q, const void* k, const int32_t* pos, const double* freqs,
+                      int32_t n, void* q_out, void* k_out, void* stream);
+
+/* The same for new tokens of the cache: rotated k, and v as it is, go to the tokens' slots, of all KV heads.
+ *   v      [n, Hk, d] by the strides in rotation.
+ *   slot   [n] int64: page * page_size + place in the page; -1: the token is not written.  No slot twice. */
+asl_status asl_rotate_write(asl_ctx* ctx, const asl_pages* pages, const asl_rotation* rotation, const void* q, const void* k,
+                            const void* v, const int32_t* pos, const int64_t* slot, const double* freqs, int32_t n, void* q_out,
+                            void* k_pages, void* v_pages, void* stream);
+
+/* A batch from its requests' lengths alone: rows rows[i] become add[i] tokens longer, as by asl_pages_grow, and of every new token comes its
+ * place.  Request i's tokens are cu[i] .. cu[i+1]-1.
+ *   parent [total] int32 or NULL: the tokens are drafts, and a node's position is by its depth.  NULL: one token behind the other.
+ *   pruned [n_rows] int32 or NULL: tokens that pruning has taken out of each row, i.e. position minus place of its last tokens.
+ *   cu     [n+1] int32 out.  total: room for tokens; the first request that does not fit in it whole, and all behind it, get none (and
+ *          raise the fault word).
+ *   slot   [total] int64 out: as asl_rotate_write takes them; -1 where the row did not get its pages, and behind the last request.
+ *   pos    [total] int32 out: the row's old length + the token's place among the new ones (or its depth) + pruned; -1 where the row is out
+ *          of range, and behind the last request. */
+asl_status asl_pages_plan(asl_ctx* ctx, const asl_pages* pages, const int32_t* rows, const int32_t* add, int32_t n, int32_t total,
+                          const int32_t* parent, const int32_t* pruned, int32_t* table, int32_t* kv_len, int32_t* refs, int32_t* cu,
+                          int64_t* slot, int32_t* pos, void* stream);
+
+/* asl_paged_attention of drafts: the queries are nodes, sequence b's cu_q[b] .. cu_q[b+1]-1 its last tokens, and each sees the tokens
+ * before the draft, its ancestors and itself.  Arguments and results as there, with
+ *   parent [total_q] int32: of each node its parent's number in the draft, less than its own, or -1.  Other numbers stand for -1, and raise
+ *          the fault word.
+ * attn->flags is ASL_ATTN_CAUSAL.  At most 512 nodes a sequence (max_q_len, and what cu_q says: a longer draft is left out, its rows of out
+ * and lse stay as they were).  Of a shared prefix the tokens before the drafts are read for the whole group. */
+asl_status asl_tree_attention(asl_ctx* ctx, const asl_pages* pages, const asl_attn* attn, const void* q, const void* k_pages,
+                              const void* v_pages, const int32_t* rows, const int32_t* table, const int32_t* kv_len,
+                              const int32_t* cu_q, const int32_t* parent, const int32_t* group_start, const int32_t* prefix_len,
+                              void* out, float* lse, void* stream);
+
+/* Of row rows[i], whose last cu[i+1] - cu[i] tokens are a draft, the nodes path[i][0 .. n_path[i]-1] stay, as the tokens behind the context;
+ * the others go, and pages that no token is left in are given back.
+ *   path   [n, path_stride] int32, path_stride <= 512: a row's nodes from the root on, ascending (as parents stand before their children).
+ *          The first number that does not ascend, or is none of the draft's, ends the path, and raises the fault word.
+ *   n_path [n] int32, 0: the whole draft goes.
+ *   k_ptrs, v_ptrs  DEVICE arrays of n_layers device pointers to each layer's k_pages (v_pages).
+ * The pages of a draft are its row's alone.  No row twice. */
+asl_status asl_pages_accept(asl_ctx* ctx, const asl_pages* pages, void* const* k_ptrs, void* const* v_ptrs, int32_t n_layers,
+                            const int32_t* rows, const int32_t* cu, const int32_t* path, int32_t path_stride, const int32_t* n_path,
+                            int32_t n, const int32_t* table, int32_t* kv_len, int32_t* refs, void* stream);
+
 /* Health check (not a step of the paper's method).  Workgroups of a launch that wait for other workgroups of it do so with
  * a bounded number of polls, and raise a fault word in the workspace if their wait runs out (every wave still exits):
  *  - the first workgroup of a statistic, for the others' partial sums: it then reports no result (evaluated = 0) and leaves the

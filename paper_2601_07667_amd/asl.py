@@ -18,13 +18,17 @@ ASL_BF16, ASL_F32 = 0, 1
 ASL_FLAG_GENERIC_SCORE = 1
 ASL_FLAG_DEFER_JOIN = 2
 ASL_ATTN_CAUSAL = 1
+ASL_PAIRS_HALVES, ASL_PAIRS_NEIGHBOURS = 0, 1
+ASL_ROTATE_BACK = 1
+ASL_FREQS_PLAIN, ASL_FREQS_LINEAR, ASL_FREQS_BASE, ASL_FREQS_PARTS = 0, 1, 2, 3
 _STATUS = {0: "ASL_OK", -1: "ASL_EINVAL", -2: "ASL_ENOMEM", -3: "ASL_EHIP", -4: "ASL_EUNSUPPORTED"}
 
 EXPORTS = ["asl_create", "asl_destroy", "asl_last_error", "asl_workspace_bytes", "asl_score_layer",
            "asl_window_lse", "asl_gather_kv_layers", "asl_rank_static", "asl_static_last_error", "asl_pool", "asl_rank", "asl_rankvar", "asl_rank_stat", "asl_select_topk", "asl_gather_kv",
            "asl_gather_rows", "asl_layer_step", "asl_join", "asl_device_fault", "asl_profile_enable", "asl_profile_collect",
            "asl_paged_reserve", "asl_pages_grow", "asl_pages_fork", "asl_pages_free", "asl_pages_write", "asl_pages_compact",
-           "asl_paged_attention"]
+           "asl_paged_attention", "asl_rotation_freqs", "asl_rotate", "asl_rotate_write", "asl_pages_plan", "asl_tree_attention",
+           "asl_pages_accept"]
 
 
 class AslParams(C.Structure):
@@ -63,6 +67,19 @@ class AslAttn(C.Structure):
     _fields_ = [("n_seqs", C.c_int32), ("total_q", C.c_int32), ("max_q_len", C.c_int32), ("max_kv_len", C.c_int32),
                 ("n_groups", C.c_int32), ("flags", C.c_int32), ("q_stride_tok", C.c_int64), ("q_stride_head", C.c_int64),
                 ("out_stride_tok", C.c_int64), ("out_stride_head", C.c_int64)]
+
+
+class AslRotation(C.Structure):
+    _fields_ = [("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int32),
+                ("rot_dim", C.c_int32), ("pairs", C.c_int32), ("flags", C.c_int32), ("magnitude", C.c_float),
+                ("q_stride_tok", C.c_int64), ("q_stride_head", C.c_int64), ("k_stride_tok", C.c_int64), ("k_stride_head", C.c_int64),
+                ("v_stride_tok", C.c_int64), ("v_stride_head", C.c_int64), ("q_out_stride_tok", C.c_int64),
+                ("q_out_stride_head", C.c_int64), ("k_out_stride_tok", C.c_int64), ("k_out_stride_head", C.c_int64)]
+
+
+class AslFreqs(C.Structure):
+    _fields_ = [("rot_dim", C.c_int32), ("kind", C.c_int32), ("base", C.c_double), ("factor", C.c_double), ("context", C.c_double),
+                ("low", C.c_double), ("high", C.c_double)]
 
 
 class AslError(RuntimeError):
@@ -139,7 +156,13 @@ def load() -> C.CDLL:
             "asl_pages_free": [vp, C.POINTER(AslPages), vp, i32, vp, vp, vp, vp],
             "asl_pages_write": [vp, C.POINTER(AslPages), C.POINTER(AslRows), vp, vp, vp, vp, i32, i32, vp, vp, vp, vp, vp, vp],
             "asl_pages_compact": [vp, C.POINTER(AslPages), vp, vp, vp, i32, i32, vp, i32, vp, vp, vp, vp, vp],
-            "asl_paged_attention": [vp, C.POINTER(AslPages), C.POINTER(AslAttn)] + [vp] * 12}.items():
+            "asl_paged_attention": [vp, C.POINTER(AslPages), C.POINTER(AslAttn)] + [vp] * 12,
+            "asl_rotation_freqs": [C.POINTER(AslFreqs), vp],
+            "asl_rotate": [vp, C.POINTER(AslRotation), vp, vp, vp, vp, i32, vp, vp, vp],
+            "asl_rotate_write": [vp, C.POINTER(AslPages), C.POINTER(AslRotation)] + [vp] * 6 + [i32] + [vp] * 4,
+            "asl_pages_plan": [vp, C.POINTER(AslPages), vp, vp, i32, i32] + [vp] * 9,
+            "asl_tree_attention": [vp, C.POINTER(AslPages), C.POINTER(AslAttn)] + [vp] * 13,
+            "asl_pages_accept": [vp, C.POINTER(AslPages), vp, vp, i32, vp, vp, vp, i32, vp, i32] + [vp] * 4}.items():
         getattr(lib, name).argtypes = args
         getattr(lib, name).restype = C.c_int
     _lib = lib
@@ -155,6 +178,52 @@ def _refuse_gaps(**tensors) -> None:
     for name, t in tensors.items():
         if t.stride(2) != 1:
             raise AslError(ASL_EUNSUPPORTED, f"the last dimension of {name} must be contiguous (its stride is {t.stride(2)})")
+
+
+def _batch_of(attn, q, out, lse):
+    """The description of a batch with the strides of this call's tensors."""
+    a = AslAttn.from_buffer_copy(attn)                       # the description may be another thread's too
+    a.q_stride_tok, a.q_stride_head, q1 = q.stride()
+    a.out_stride_tok, a.out_stride_head, out1 = out.stride()
+    if q1 != 1 or out1 != 1:
+        _refuse_gaps(q=q, out=out)
+    if lse is not None and not lse.is_contiguous():
+        raise AslError(ASL_EUNSUPPORTED, f"lse must be without gaps (its strides are {tuple(lse.stride())})")
+    return a
+
+
+def _rotation_of(rotation, **tensors):
+    """The description of a rotation with the strides of this call's tensors."""
+    r = AslRotation.from_buffer_copy(rotation)
+    for name, t in tensors.items():
+        if t is None:
+            continue
+        tok, head, one = t.stride()
+        if one != 1:
+            _refuse_gaps(**{name: t})
+        setattr(r, name + "_stride_tok", tok)
+        setattr(r, name + "_stride_head", head)
+    return r
+
+
+def _tokens_of(r, pos, freqs, *tensors) -> int:
+    """The number of tokens of a rotation, whose tensors have to agree on it."""
+    n = pos.shape[0]
+    for name, t, heads in tensors:
+        if heads > 0 and (t is None or tuple(t.shape) != (n, heads, r.head_dim)):
+            raise AslError(ASL_EINVAL, f"{name} must be [{n}, {heads}, {r.head_dim}] (it is {None if t is None else tuple(t.shape)})")
+    _list_of("pos", pos, n, "int32")
+    _list_of("freqs", freqs, r.rot_dim // 2, "float64")
+    return n
+
+
+def _list_of(name, t, n: int, dtype: str) -> None:
+    """A list that a call reads or writes n entries of, one behind the other."""
+    if t is None and n == 0:
+        return
+    if t is None or t.numel() < n or not t.is_contiguous() or str(t.dtype) != "torch." + dtype:
+        raise AslError(ASL_EINVAL, f"{name} must be {n} x {dtype} without gaps (it is "
+                                   f"{None if t is None else (tuple(t.shape), tuple(t.stride()), str(t.dtype))})")
 
 
 def _index_rows(idx, total: int) -> int:
@@ -193,6 +262,24 @@ def make_pages(Hq: int, Hk: int, d: int, page_size: int, n_pages: int, n_rows: i
 def make_attn(n_seqs: int, total_q: int, max_q_len: int, max_kv_len: int, n_groups: int = 0, causal: bool = True) -> AslAttn:
     """Each call takes the strides of q and out from its tensors; the description stays as it is."""
     return AslAttn(n_seqs, total_q, max_q_len, max_kv_len, n_groups, ASL_ATTN_CAUSAL if causal else 0, 0, 0, 0, 0)
+
+
+def make_rotation(Hq: int, Hk: int, d: int, rot_dim: Optional[int] = None, pairs: int = ASL_PAIRS_HALVES, dtype: int = ASL_BF16,
+                  magnitude: float = 0.0, back: bool = False) -> AslRotation:
+    """Each call takes the strides from its tensors; the description stays as it is.  back: the transposed map, i.e. the gradient."""
+    return AslRotation(Hq, Hk, d, dtype, d if rot_dim is None else rot_dim, pairs, ASL_ROTATE_BACK if back else 0, magnitude, *[0] * 10)
+
+
+def rotation_freqs(rot_dim: int, base: float = 10000.0, kind: int = ASL_FREQS_PLAIN, factor: float = 1.0, context: float = 0.0,
+                   low: float = 1.0, high: float = 32.0):
+    """[rot_dim / 2] float64 on the host: radians that a position adds to the angle of each pair."""
+    import torch
+    out = torch.empty(max(rot_dim, 0) // 2, dtype=torch.float64)
+    f = AslFreqs(rot_dim, kind, base, factor, context, low, high)
+    st = load().asl_rotation_freqs(C.byref(f), out.data_ptr())
+    if st != ASL_OK:
+        raise AslError(st, f"rot_dim={rot_dim}, base={base}, kind={kind}, factor={factor}, context={context}, low={low}, high={high}")
+    return out
 
 
 class Asl:
@@ -329,16 +416,55 @@ class Asl:
     def asl_paged_attention(self, pages: AslPages, attn: AslAttn, q, k_pages, v_pages, table, kv_len, cu_q, out, lse=None,
                             rows=None, group_start=None, prefix_len=None) -> None:
         """q, out: [total_q, Hq, d] of any strides (d contiguous); lse: [Hq, total_q]."""
-        a = AslAttn.from_buffer_copy(attn)                   # the description may be another thread's too
-        a.q_stride_tok, a.q_stride_head, q1 = q.stride()
-        a.out_stride_tok, a.out_stride_head, out1 = out.stride()
-        if q1 != 1 or out1 != 1:
-            _refuse_gaps(q=q, out=out)
-        if lse is not None and not lse.is_contiguous():
-            raise AslError(ASL_EUNSUPPORTED, f"lse must be without gaps (its strides are {tuple(lse.stride())})")
+        a = _batch_of(attn, q, out, lse)
         self._check(self.lib.asl_paged_attention(self.h, C.byref(pages), C.byref(a), _ptr(q), _ptr(k_pages), _ptr(v_pages),
                                                  _ptr(rows), _ptr(table), _ptr(kv_len), _ptr(cu_q), _ptr(group_start),
                                                  _ptr(prefix_len), _ptr(out), _ptr(lse), _stream()))
+
+    # -- drafting over the paged cache -------------------------------------------------------------
+    def asl_rotate(self, rotation: AslRotation, q, k, pos, freqs, q_out, k_out) -> None:
+        """q, q_out: [n, Hq, d], k, k_out: [n, Hk, d] of any strides (d contiguous); None where the rotation has no such heads."""
+        r = _rotation_of(rotation, q=q, k=k, q_out=q_out, k_out=k_out)
+        n = _tokens_of(r, pos, freqs, ("q", q, r.n_q_heads), ("k", k, r.n_kv_heads), ("q_out", q_out, r.n_q_heads),
+                       ("k_out", k_out, r.n_kv_heads))
+        self._check(self.lib.asl_rotate(self.h, C.byref(r), _ptr(q), _ptr(k), _ptr(pos), _ptr(freqs), n, _ptr(q_out), _ptr(k_out),
+                                        _stream()))
+
+    def asl_rotate_write(self, pages: AslPages, rotation: AslRotation, q, k, v, pos, slot, freqs, q_out, k_pages, v_pages) -> None:
+        """q, q_out: [n, Hq, d], k, v: [n, Hk, d] of any strides (d contiguous); slot: [n] int64."""
+        r = _rotation_of(rotation, q=q, k=k, v=v, q_out=q_out)
+        n = _tokens_of(r, pos, freqs, ("q", q, r.n_q_heads), ("k", k, r.n_kv_heads), ("v", v, r.n_kv_heads), ("q_out", q_out, r.n_q_heads))
+        _list_of("slot", slot, n, "int64")
+        self._check(self.lib.asl_rotate_write(self.h, C.byref(pages), C.byref(r), _ptr(q), _ptr(k), _ptr(v), _ptr(pos), _ptr(slot),
+                                              _ptr(freqs), n, _ptr(q_out), _ptr(k_pages), _ptr(v_pages), _stream()))
+
+    def asl_pages_plan(self, pages: AslPages, rows, add, n: int, total: int, table, kv_len, refs, cu, slot, pos, parent=None,
+                       pruned=None) -> None:
+        """cu: [n + 1] int32, slot: [total] int64, pos: [total] int32, all written; parent: [total], pruned: [rows of the table]."""
+        _list_of("slot", slot, total, "int64")
+        _list_of("pos", pos, total, "int32")
+        _list_of("cu", cu, n + 1, "int32")
+        self._check(self.lib.asl_pages_plan(self.h, C.byref(pages), _ptr(rows), _ptr(add), n, total, _ptr(parent), _ptr(pruned),
+                                            _ptr(table), _ptr(kv_len), _ptr(refs), _ptr(cu), _ptr(slot), _ptr(pos), _stream()))
+
+    def asl_tree_attention(self, pages: AslPages, attn: AslAttn, q, k_pages, v_pages, table, kv_len, cu_q, parent, out, lse=None,
+                           rows=None, group_start=None, prefix_len=None) -> None:
+        """q, out: [total_q, Hq, d] of any strides (d contiguous); parent: [total_q] int32; lse: [Hq, total_q]."""
+        a = _batch_of(attn, q, out, lse)
+        _list_of("parent", parent, a.total_q, "int32")
+        self._check(self.lib.asl_tree_attention(self.h, C.byref(pages), C.byref(a), _ptr(q), _ptr(k_pages), _ptr(v_pages),
+                                                _ptr(rows), _ptr(table), _ptr(kv_len), _ptr(cu_q), _ptr(parent), _ptr(group_start),
+                                                _ptr(prefix_len), _ptr(out), _ptr(lse), _stream()))
+
+    def asl_pages_accept(self, pages: AslPages, k_ptrs, v_ptrs, n_layers: int, rows, cu, path, n_path, n: int, table, kv_len,
+                         refs) -> None:
+        """k_ptrs, v_ptrs: int64 device tensors holding one device pointer per layer; path: [n, longest path] without gaps."""
+        if path.dim() != 2 or path.shape[0] < n or not path.is_contiguous():
+            raise AslError(ASL_EINVAL, f"path must be [{n}, longest path] without gaps (its shape is {tuple(path.shape)}, its strides "
+                                       f"{tuple(path.stride())})")
+        self._check(self.lib.asl_pages_accept(self.h, C.byref(pages), _ptr(k_ptrs), _ptr(v_ptrs), n_layers, _ptr(rows), _ptr(cu),
+                                              _ptr(path), path.shape[1], _ptr(n_path), n, _ptr(table), _ptr(kv_len), _ptr(refs),
+                                              _stream()))
 
     def asl_gather_kv(self, params: AslParams, k, v, idx, idx_rows: int, n_idx: int, k_out, v_out) -> None:
         self._check(self.lib.asl_gather_kv(self.h, C.byref(params), _ptr(k), _ptr(v), _ptr(idx), idx_rows,

@@ -11,7 +11,8 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libasl.so")
 SOURCES = ["api.hip", "score.hip", "pool.hip", "rank.hip", "rankvar.hip", "select.hip", "gather.hip", "tail.hip",
-           "paged_api.hip", "paged.hip", "attend.hip", "attend_64.hip", "attend_128.hip"]
+           "paged_api.hip", "paged.hip", "attend.hip", "attend_64.hip", "attend_128.hip", "attend_tree.hip", "attend_tree_64.hip",
+           "attend_tree_128.hip", "rotate.hip", "draft.hip"]
 # packed-fp32 instructions are switched off for all device code
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -24,7 +25,8 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hi
 # MFMA results are kept in ordinary VGPRs: the softmax arithmetic reads every accumulator, and
 # copies out of accumulation registers would cost one vector instruction per element.
 PER_FILE_FLAGS = {"score.hip": ["-fno-honor-nans", "-mllvm", "-amdgpu-mfma-vgpr-form"],
-                  **{f: ["-mllvm", "-amdgpu-mfma-vgpr-form"] for f in ("attend.hip", "attend_64.hip", "attend_128.hip")}}
+                  **{f: ["-mllvm", "-amdgpu-mfma-vgpr-form"] for f in ("attend.hip", "attend_64.hip", "attend_128.hip", "attend_tree.hip",
+                                                                       "attend_tree_64.hip", "attend_tree_128.hip")}}
 
 
 def _hipcc() -> str:

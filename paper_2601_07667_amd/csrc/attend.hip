@@ -9,11 +9,11 @@ hipError_t launch_attend(const PagedWorkspace& ws, const AttendArgs& a, int dtyp
   if (dtype == ASL_BF16) {
     if (a.d <= 64) return launch_attend_bf16_64(ws, a, st);
     if (a.d <= 128) return launch_attend_bf16_128(ws, a, st);
-    return launch_d<__bf16, 256>(ws, a, st);
+    return launch_d<__bf16, 256, false>(ws, a, st);
   }
-  if (a.d <= 64) return launch_d<float, 64>(ws, a, st);
-  if (a.d <= 128) return launch_d<float, 128>(ws, a, st);
-  return launch_d<float, 256>(ws, a, st);
+  if (a.d <= 64) return launch_d<float, 64, false>(ws, a, st);
+  if (a.d <= 128) return launch_d<float, 128, false>(ws, a, st);
+  return launch_d<float, 256, false>(ws, a, st);
 }
 
 }  // namespace asl

@@ -3,6 +3,6 @@
 
 namespace asl {
 
-hipError_t launch_attend_bf16_128(const PagedWorkspace& ws, const AttendArgs& a, hipStream_t st) { return launch_d<__bf16, 128>(ws, a, st); }
+hipError_t launch_attend_bf16_128(const PagedWorkspace& ws, const AttendArgs& a, hipStream_t st) { return launch_d<__bf16, 128, false>(ws, a, st); }
 
 }  // namespace asl

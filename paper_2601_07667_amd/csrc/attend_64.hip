@@ -3,6 +3,6 @@
 
 namespace asl {
 
-hipError_t launch_attend_bf16_64(const PagedWorkspace& ws, const AttendArgs& a, hipStream_t st) { return launch_d<__bf16, 64>(ws, a, st); }
+hipError_t launch_attend_bf16_64(const PagedWorkspace& ws, const AttendArgs& a, hipStream_t st) { return launch_d<__bf16, 64, false>(ws, a, st); }
 
 }  // namespace asl

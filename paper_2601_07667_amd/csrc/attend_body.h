@@ -142,9 +142,15 @@ struct Groups {
   }
 };
 
+// Tokens of a sequence that all nodes of its draft see: those before the draft.
+__device__ __forceinline__ int context_of(int len, int nodes) { return max(0, len - nodes); }
+
+// Those of them that its group's shared segment takes: whole key tiles.
+__device__ __forceinline__ int tree_shared(int tokens, int len, int nodes) { return min(tokens, context_of(len, nodes) & ~(kKeyTile - 1)); }
+
 // Segment i: sequence i's own (SHARED false), or group i's shared one.  *bad: a number out of range.
 // (Every lane of the wavefront calls it; those with i out of range get an empty one.)
-template <bool SHARED>
+template <bool SHARED, bool TREE>
 __device__ __forceinline__ Segment segment_of(const AttendArgs& a, const Groups& groups, int i, bool* bad) {
   Segment s = {};
   s.group = -1;
@@ -171,11 +177,12 @@ __device__ __forceinline__ Segment segment_of(const AttendArgs& a, const Groups&
   s.row = seq_row(a, i);
   if (!row_length(a.map, s.row, &s.len)) *bad = true;
   if (c0 < 0 || c1 < c0 || c1 > a.total_q) { *bad = true; return s; }
+  if (TREE && c1 - c0 > kTreeNodes) { *bad = true; return s; }
   s.c0 = c0;
   s.rows = (c1 - c0) * a.G;
   if (a.n_groups > 0) {
     if (s.group < 0) *bad = true;
-    s.shared = tokens;
+    s.shared = TREE ? tree_shared(tokens, s.len, c1 - c0) : tokens;
   }
   s.t0 = s.shared / kKeyTile;
   s.span = max(0, (s.len + kKeyTile - 1) / kKeyTile - s.t0);
@@ -202,7 +209,7 @@ __device__ __forceinline__ int4 plan_entry(const Segment& s, int splits, bool pa
   return make_int4(s.c0, s.rows, partial ? splits : 0, (int)slot);
 }
 
-template <bool SHARED>
+template <bool SHARED, bool TREE>
 __device__ __forceinline__ bool find_item(const AttendArgs& a, const AttendCut& cut, int item, const Partials& pt, Item* out) {
   const int lane = threadIdx.x & 63;
   const int n = SHARED ? a.n_groups : a.n_seqs, per = (n + 63) / 64;
@@ -214,7 +221,7 @@ __device__ __forceinline__ bool find_item(const AttendArgs& a, const AttendCut& 
   const Groups groups(a);
   unsigned long long work = 0, all_rows = 0;
   for (int u = 0; u < per; ++u) {
-    own = segment_of<SHARED>(a, groups, lane * per + u, &bad);
+    own = segment_of<SHARED, TREE>(a, groups, lane * per + u, &bad);
     all_rows += (unsigned long long)own.rows;
     work += (unsigned long long)row_tiles(own) * (uint32_t)max(own.span, 1);   // (no rows: 0)
   }
@@ -234,7 +241,7 @@ __device__ __forceinline__ bool find_item(const AttendArgs& a, const AttendCut& 
   for (int round = 0;; ++round) {
     items = slots = 0;
     for (int u = 0; u < per; ++u) {
-      if (per > 1) own = segment_of<SHARED>(a, groups, lane * per + u, &bad);
+      if (per > 1) own = segment_of<SHARED, TREE>(a, groups, lane * per + u, &bad);
       const int k = splits_of(own.span, per_item);
       items += row_tiles(own) * (uint32_t)k;
       slots += is_partial(own, k) ? (uint32_t)own.rows * (uint32_t)a.Hk * (uint32_t)k : 0u;
@@ -249,7 +256,7 @@ __device__ __forceinline__ bool find_item(const AttendArgs& a, const AttendCut& 
     uint32_t at = slots_upto - slots;
     for (int u = 0; u < per; ++u) {
       const int i = lane * per + u;
-      if (per > 1) own = segment_of<SHARED>(a, groups, i, &bad);
+      if (per > 1) own = segment_of<SHARED, TREE>(a, groups, i, &bad);
       if (i >= n) continue;
       const int k = splits_of(own.span, per_item);
       const bool partial = is_partial(own, k);
@@ -267,7 +274,7 @@ __device__ __forceinline__ bool find_item(const AttendArgs& a, const AttendCut& 
   if (per > 1) {                                           // the same among the lane's segments (per <= 64)
     const int i = l * per + lane;
     items = slots = 0;
-    own = segment_of<SHARED>(a, groups, lane < per ? i : n, &bad);
+    own = segment_of<SHARED, TREE>(a, groups, lane < per ? i : n, &bad);
     if (lane < per && i < n) {
       const int k = splits_of(own.span, per_item);
       items = row_tiles(own) * (uint32_t)k;
@@ -303,19 +310,20 @@ __device__ __forceinline__ bool find_item(const AttendArgs& a, const AttendCut& 
 
 // The fewest keys that a row of a shared segment's sequences sees, or the segment's if that is less: found by lanes over the sequences,
 // since a row's own takes a search for its sequence.
+template <bool TREE>
 __device__ __forceinline__ int least_limit(const AttendArgs& a, const Segment& s) {
   uint32_t least = (uint32_t)s.len;
   for (int b = s.b0 + (int)(threadIdx.x & 63); b < s.b1; b += 64) {
     const int n = a.cu_q[b + 1] - a.cu_q[b];
     int len;
     row_length(a.map, seq_row(a, b), &len);
-    if (n > 0) least = min(least, (uint32_t)(a.causal ? max(0, len - n + 1) : len));
+    if (n > 0) least = min(least, (uint32_t)(TREE ? tree_shared(s.len, len, n) : a.causal ? max(0, len - n + 1) : len));
   }
   return (int)wave_min(least);
 }
 
-// Keys that row r of a segment sees.  all: as many as every row of a shared segment sees.
-template <bool SHARED>
+// Keys that row r of a segment sees, of a draft's own segment those up to the last one.  all: as many as every row of a shared segment sees.
+template <bool SHARED, bool TREE>
 __device__ __forceinline__ int row_limit(const AttendArgs& a, const Segment& s, int r, int all) {
   const int i = (int)((uint32_t)r / (uint32_t)a.G);
   if (!SHARED) return a.causal ? max(0, s.len - s.rows / a.G + i + 1) : s.len;
@@ -323,6 +331,7 @@ __device__ __forceinline__ int row_limit(const AttendArgs& a, const Segment& s, 
   const int tok = s.c0 + i, b = sequence_of(a.cu_q, a.n_seqs, tok);
   int len;
   row_length(a.map, seq_row(a, b), &len);
+  if (TREE) return tree_shared(s.len, len, a.cu_q[b + 1] - a.cu_q[b]);
   return min(s.len, a.causal ? max(0, len - (a.cu_q[b + 1] - tok) + 1) : len);
 }
 
@@ -511,9 +520,27 @@ __device__ __forceinline__ void add_values(f32x4* (&o)[MT], const Weights<T> (&p
   }
 }
 
+// Which keys the rows of a tile see of their sequence's draft (DRAFT): all before it, and of its nodes those whose bits are set.
+template <int MT, bool DRAFT>
+struct Sight {};
+template <int MT>
+struct Sight<MT, true> {
+  const uint32_t* bits[MT];                                // in LDS, kTreeWords words and two zeros
+  int base;                                                // key of node 0 (below 0: the first nodes have no place)
+  // Bit j: whether row mt, which sees no key from lim on, sees key key0 + j.
+  __device__ __forceinline__ uint32_t window(int mt, int lim, int key0) const {
+    const int o = key0 - base;
+    if (lim == 0) return 0u;
+    if (o <= -32) return ~0u;
+    if (o < 0) return (bits[mt][0] << -o) | ((1u << -o) - 1u);
+    const int w = min(o >> 5, kTreeWords);
+    return (uint32_t)((((uint64_t)bits[mt][w + 1] << 32) | bits[mt][w]) >> (o & 31));
+  }
+};
+
 // A wavefront's running results for MT tiles of 16 rows.
-template <typename T, int D, int MT>
-struct Rows {
+template <typename T, int D, int MT, bool DRAFT = false>
+struct Rows : Sight<MT, DRAFT> {
   typedef Block<T, D> B;
   Piece q[MT][B::KP];
   f32x4 o[MT][B::NT];
@@ -579,12 +606,14 @@ struct Rows {
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
       float top = -INFINITY;
+      uint32_t sight = 0;
+      if constexpr (MASKED && DRAFT) sight = this->window(mt, lim[mt], key0) >> (4 * g);
 #pragma unroll
       for (int t = 0; t < B::SUB; ++t)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           float y = x[mt][t][i] * scale;
-          if (MASKED) y = b.ok[t] && key0 + 16 * t + 4 * g + i < lim[mt] ? y : -INFINITY;
+          if (MASKED) y = b.ok[t] && (DRAFT ? ((sight >> (16 * t + i)) & 1u) != 0 : key0 + 16 * t + 4 * g + i < lim[mt]) ? y : -INFINITY;
           p[mt][t][i] = y;
           top = fmaxf(top, y);
         }
@@ -670,10 +699,13 @@ struct Rows {
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) {
         float one[B::SUB][4];
+        uint32_t sight = 0;
+        if constexpr (DRAFT) sight = this->window(mt, lim[mt], key0) >> (4 * g);
 #pragma unroll
         for (int t = 0; t < B::SUB; ++t)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) one[t][i] = ok[t] && key0 + 16 * t + 4 * g + i < lim[mt] ? 1.f : 0.f;
+          for (int i = 0; i < 4; ++i)
+            one[t][i] = ok[t] && (DRAFT ? ((sight >> (16 * t + i)) & 1u) != 0 : key0 + 16 * t + 4 * g + i < lim[mt]) ? 1.f : 0.f;
         see[mt].set(one);
       }
 #pragma unroll
@@ -776,7 +808,7 @@ __device__ __forceinline__ Source source_of(const AttendArgs& a, const Item& it)
 template <bool SHARED>
 __device__ __forceinline__ void tiles_of(const AttendArgs& a, const Item& it, int tile_rows, int* t0, int* t1) {
   int any = it.seg.len;
-  if (!SHARED) any = row_limit<false>(a, it.seg, min(it.seg.rows, (it.tile + 1) * tile_rows) - 1, 0);
+  if (!SHARED) any = row_limit<false, false>(a, it.seg, min(it.seg.rows, (it.tile + 1) * tile_rows) - 1, 0);
   split_range(min(it.seg.span, max(0, (any + kKeyTile - 1) / kKeyTile - it.seg.t0)), it.splits, it.split, t0, t1);
   *t0 += it.seg.t0;
   *t1 += it.seg.t0;
@@ -842,6 +874,49 @@ __device__ __forceinline__ void join_last(const AttendArgs& a, const AttendCut& 
   }
 }
 
+// A draft's nodes that each node of a tile sees, itself and its ancestors, as bits (TREE; else nothing).  A node's parent stands before it, so a
+// walk over the parents ends after as many steps as the node is deep; the list is taken to LDS first, since the steps wait for one another
+// (about 130 cycles each from there).
+template <int M, bool TREE>
+struct TreeLds {};
+template <int M>
+struct TreeLds<M, true> {
+  uint32_t bits[M][kTreeWords + 3];                        // (an odd number of words: rows start in different banks)
+  int16_t parent[kTreeNodes];
+};
+
+// Fills l for rows tile_row0 .. tile_row0 + M - 1 of segment s (M rows have at most M nodes).  Every thread of the workgroup calls it.
+template <int M>
+__device__ __forceinline__ void read_tree(const AttendArgs& a, const Segment& s, int tile_row0, TreeLds<M, true>& l) {
+  const int n = s.rows / a.G, i0 = (int)((uint32_t)tile_row0 / (uint32_t)a.G);
+  bool bad = false;
+  for (int i = threadIdx.x; i < n; i += kThreads) {
+    const int p = a.parent[s.c0 + i];
+    const bool in = p >= -1 && p < i;
+    bad = bad || !in;
+    l.parent[i] = (int16_t)(in ? p : -1);
+  }
+  for (int i = threadIdx.x; i < M * (kTreeWords + 3); i += kThreads) (&l.bits[0][0])[i] = 0;
+  __syncthreads();
+  if ((int)threadIdx.x < M && i0 + (int)threadIdx.x < n) {
+    uint32_t* to = l.bits[threadIdx.x];
+    int i = i0 + (int)threadIdx.x, w = i >> 5;
+    uint32_t x = 0;
+    while (i >= 0) {
+      if (i >> 5 != w) {
+        to[w] = x;
+        w = i >> 5;
+        x = 0;
+      }
+      x |= 1u << (i & 31);
+      i = l.parent[i];
+    }
+    to[w] = x;
+  }
+  __syncthreads();
+  if (bad) paged_fault(a.map);
+}
+
 // What the wavefronts of a split item leave for each other.
 template <int D>
 struct SplitLds {
@@ -849,12 +924,13 @@ struct SplitLds {
   float m[kWaves][16], z[kWaves][16];
 };
 
-template <typename T, int D, int MT, bool PAD, bool SHARED, bool STREAM>
+template <typename T, int D, int MT, bool PAD, bool SHARED, bool STREAM, bool TREE>
 __device__ __forceinline__ void split_item(const AttendArgs& a, const AttendCut& cut, const Partials& pt, int item, char* lds) {
   typedef Block<T, D> B;
+  constexpr bool DRAFT = TREE && !SHARED;
   SplitLds<D>& l = *(SplitLds<D>*)lds;
   Item it;
-  if (!find_item<SHARED>(a, cut, item, pt, &it)) return;
+  if (!find_item<SHARED, TREE>(a, cut, item, pt, &it)) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r16 = lane & 15, g = lane >> 4;
   const Source src = source_of(a, it);
   int t0, t1;
@@ -863,16 +939,17 @@ __device__ __forceinline__ void split_item(const AttendArgs& a, const AttendCut&
   int key = t0 * kKeyTile + wave * B::KEYS;
   PageWindow<B::SUB, STEP> window;                         // (ahead of the queries and limits, which wait for loads of their own)
   if (t0 < t1) window.start(src, key);
-  Rows<T, D, MT> rows;
+  Rows<T, D, MT, DRAFT> rows;
   rows.clear();
-  const int all = SHARED ? least_limit(a, it.seg) : 0;
+  const int all = SHARED ? least_limit<TREE>(a, it.seg) : 0;
+  const int context = DRAFT ? context_of(it.seg.len, it.seg.rows / a.G) : 0;
   uint32_t least = 0x7fffffffu, most = 0;
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
     const int r = it.tile * cut.rows + 16 * mt + r16;
     const bool in = r < it.seg.rows;
-    rows.lim[mt] = in ? row_limit<SHARED>(a, it.seg, r, all) : 0;
-    least = min(least, in ? (uint32_t)rows.lim[mt] : 0x7fffffffu);
+    rows.lim[mt] = in ? row_limit<SHARED, TREE>(a, it.seg, r, all) : 0;
+    least = min(least, in ? (uint32_t)(DRAFT ? context : rows.lim[mt]) : 0x7fffffffu);
     most = max(most, (uint32_t)rows.lim[mt]);
     const int i = (int)((uint32_t)r / (uint32_t)a.G);
     const T* q = (const T*)a.q + (int64_t)(it.seg.c0 + i) * a.qt + (int64_t)(it.h * a.G + (r - i * a.G)) * a.qh;
@@ -884,6 +961,15 @@ __device__ __forceinline__ void split_item(const AttendArgs& a, const AttendCut&
   }
   least = wave_min(least);
   most = wave_max(most);
+  if constexpr (DRAFT) {
+    TreeLds<16 * MT, true>& tree = *(TreeLds<16 * MT, true>*)(lds + sizeof(SplitLds<D>));
+    rows.base = it.seg.len - it.seg.rows / a.G;
+    const int i0 = (int)((uint32_t)(it.tile * cut.rows) / (uint32_t)a.G);
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+      rows.bits[mt] = tree.bits[min((int)((uint32_t)(it.tile * cut.rows + 16 * mt + r16) / (uint32_t)a.G) - i0, 16 * MT - 1)];
+    if (t1 * kKeyTile > context) read_tree<16 * MT>(a, it.seg, it.tile * cut.rows, tree);   // (else no key of the draft is looked at)
+  }
   const int end = min(t1 * kKeyTile, (int)most);
   const float scale = a.scale * kLog2e;
   bool bad = false;
@@ -1011,8 +1097,8 @@ __device__ __forceinline__ uint32_t fetch_tile(TileBuffer<D>& to, const Source& 
 // A wavefront's step over a tile in LDS.  MASKED: some row may not see some key, or its reference may have to move.  Else every row
 // sees every key and no reference moves; returns false, nothing done, if one has to.  (A branch that rescales the accumulators
 // makes the compiler keep them twice, which does not fit the registers: the prefill chunk took 1629 us with it and 1142 without.)
-template <int D, int MT, bool PAD, bool MASKED>
-__device__ __forceinline__ bool tile_step(Rows<__bf16, D, MT>& R, const TileBuffer<D>& b, int key0, uint32_t ok, int least, int most,
+template <int D, int MT, bool PAD, bool MASKED, bool DRAFT>
+__device__ __forceinline__ bool tile_step(Rows<__bf16, D, MT, DRAFT>& R, const TileBuffer<D>& b, int key0, uint32_t ok, int least, int most,
                                           int d, float scale) {
   typedef Block<__bf16, D> B;
   const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
@@ -1064,11 +1150,19 @@ __device__ __forceinline__ bool tile_step(Rows<__bf16, D, MT>& R, const TileBuff
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
     float top = -INFINITY;
+    uint32_t sight[2] = {0, 0};
+    if constexpr (MASKED && DRAFT) {
+      sight[0] = R.window(mt, R.lim[mt], key0) >> (4 * g);
+      sight[1] = R.window(mt, R.lim[mt], key0 + 32) >> (4 * g);
+    }
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        if (MASKED) x[mt][t][i] = ((ok >> t) & 1u) != 0 && key0 + 16 * t + 4 * g + i < R.lim[mt] ? x[mt][t][i] : -INFINITY;
+        if (MASKED) {
+          const bool sees = DRAFT ? ((sight[t >> 1] >> (16 * (t & 1) + i)) & 1u) != 0 : key0 + 16 * t + 4 * g + i < R.lim[mt];
+          x[mt][t][i] = ((ok >> t) & 1u) != 0 && sees ? x[mt][t][i] : -INFINITY;
+        }
         top = fmaxf(top, x[mt][t][i]);
       }
     tops[mt] = top * scale;
@@ -1144,12 +1238,13 @@ __device__ __forceinline__ bool tile_step(Rows<__bf16, D, MT>& R, const TileBuff
   return true;
 }
 
-template <int D, int MT, bool PAD, bool SHARED>
+template <int D, int MT, bool PAD, bool SHARED, bool TREE>
 __device__ __forceinline__ void tile_item(const AttendArgs& a, const AttendCut& cut, const Partials& pt, int item, char* lds) {
   typedef Block<__bf16, D> B;
+  constexpr bool DRAFT = TREE && !SHARED;
   TileBuffer<D>* buf = (TileBuffer<D>*)lds;
   Item it;
-  if (!find_item<SHARED>(a, cut, item, pt, &it)) return;
+  if (!find_item<SHARED, TREE>(a, cut, item, pt, &it)) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r16 = lane & 15, g = lane >> 4;
   const int row0 = it.tile * cut.rows + wave * 16 * MT;
   const Source src = source_of(a, it);
@@ -1157,17 +1252,18 @@ __device__ __forceinline__ void tile_item(const AttendArgs& a, const AttendCut& 
   tiles_of<SHARED>(a, it, cut.rows, &t0, &t1);
   PageWindow<4, kKeyTile> window;                          // (ahead of the queries and limits, which wait for loads of their own)
   if (t0 < t1) window.start(src, t0 * kKeyTile);
-  Rows<__bf16, D, MT> rows;
+  Rows<__bf16, D, MT, DRAFT> rows;
   rows.clear();
-  const int all = SHARED ? least_limit(a, it.seg) : 0;
+  const int all = SHARED ? least_limit<TREE>(a, it.seg) : 0;
+  const int context = DRAFT ? context_of(it.seg.len, it.seg.rows / a.G) : 0;
   uint32_t least = 0x7fffffffu, most = 0;
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
     const int r = row0 + 16 * mt + r16;
     const bool in = r < it.seg.rows;
-    rows.lim[mt] = in ? row_limit<SHARED>(a, it.seg, r, all) : 0;
+    rows.lim[mt] = in ? row_limit<SHARED, TREE>(a, it.seg, r, all) : 0;
     if (!in) rows.m[mt] = 0.f;                             // rows that are not there have logits 0: no reference to move for them
-    least = min(least, in ? (uint32_t)rows.lim[mt] : 0x7fffffffu);
+    least = min(least, in ? (uint32_t)(DRAFT ? context : rows.lim[mt]) : 0x7fffffffu);
     most = max(most, (uint32_t)rows.lim[mt]);
     const int i = (int)((uint32_t)r / (uint32_t)a.G);
     const __bf16* q = (const __bf16*)a.q + (int64_t)(it.seg.c0 + i) * a.qt + (int64_t)(it.h * a.G + (r - i * a.G)) * a.qh;
@@ -1179,8 +1275,17 @@ __device__ __forceinline__ void tile_item(const AttendArgs& a, const AttendCut& 
   }
   least = wave_min(least);
   most = wave_max(most);
+  if constexpr (DRAFT) {
+    TreeLds<64 * MT, true>& tree = *(TreeLds<64 * MT, true>*)(lds + 2 * sizeof(TileBuffer<D>));
+    rows.base = it.seg.len - it.seg.rows / a.G;
+    const int i0 = (int)((uint32_t)(it.tile * cut.rows) / (uint32_t)a.G);
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+      rows.bits[mt] = tree.bits[min((int)((uint32_t)(row0 + 16 * mt + r16) / (uint32_t)a.G) - i0, 64 * MT - 1)];
+    if (t1 * kKeyTile > context) read_tree<64 * MT>(a, it.seg, it.tile * cut.rows, tree);   // (else no key of the draft is looked at)
+  }
   // keys that all rows of the workgroup see (an own segment's limits rise with the row)
-  const int all_see = SHARED ? all : row_limit<SHARED>(a, it.seg, it.tile * cut.rows, 0);
+  const int all_see = SHARED ? all : DRAFT ? context : row_limit<SHARED, TREE>(a, it.seg, it.tile * cut.rows, 0);
   const float scale = a.scale * kLog2e;
   bool bad = false;
   if (t0 < t1) {
@@ -1207,7 +1312,7 @@ __device__ __forceinline__ void tile_item(const AttendArgs& a, const AttendCut& 
       const int key0 = t * kKeyTile;
       bad = bad || here != 15u;
       if (key0 < (int)most)
-        tile_step<D, MT, PAD, true>(rows, buf[(t - t0) & 1], key0, here, (int)least, (int)most, a.d, scale);
+        tile_step<D, MT, PAD, true, DRAFT>(rows, buf[(t - t0) & 1], key0, here, (int)least, (int)most, a.d, scale);
       fetched = false;
       ++t;
       window.move(src, t - t0);
@@ -1215,7 +1320,7 @@ __device__ __forceinline__ void tile_item(const AttendArgs& a, const AttendCut& 
       // one a tile.)
       while (t < t1 && ok == 15u && (t + 1) * kKeyTile <= all_see) {
         here = next();
-        fetched = !tile_step<D, MT, PAD, false>(rows, buf[(t - t0) & 1], t * kKeyTile, 15u, (int)least, (int)most, a.d, scale);
+        fetched = !tile_step<D, MT, PAD, false, DRAFT>(rows, buf[(t - t0) & 1], t * kKeyTile, 15u, (int)least, (int)most, a.d, scale);
         if (fetched) break;
         ++t;
         window.move(src, t - t0);
@@ -1356,36 +1461,36 @@ __global__ void __launch_bounds__(NW > kWaves ? NW * 64 : kThreads) attend_join_
 }
 
 // ------------------------------------------------------------------------------------------------------------------
-template <typename T, int D, int KIND, bool PAD, bool SHARED, bool STREAM>
+template <typename T, int D, int KIND, bool PAD, bool SHARED, bool STREAM, bool TREE>
 __device__ __forceinline__ void run_item(const AttendArgs& a, const AttendCut& cut, const Partials& pt, int item, char* lds) {
-  if constexpr (KIND == kSplit) split_item<T, D, 1, PAD, SHARED, STREAM>(a, cut, pt, item, lds);
-  if constexpr (KIND == kTile1) tile_item<D, 1, PAD, SHARED>(a, cut, pt, item, lds);
-  if constexpr (KIND == kTile2) tile_item<D, 2, PAD, SHARED>(a, cut, pt, item, lds);
+  if constexpr (KIND == kSplit) split_item<T, D, 1, PAD, SHARED, STREAM, TREE>(a, cut, pt, item, lds);
+  if constexpr (KIND == kTile1) tile_item<D, 1, PAD, SHARED, TREE>(a, cut, pt, item, lds);
+  if constexpr (KIND == kTile2) tile_item<D, 2, PAD, SHARED, TREE>(a, cut, pt, item, lds);
 }
-template <int D, int KIND>
+template <int D, int KIND, bool DRAFT>
 constexpr size_t lds_of() {
-  return KIND == kNone ? 0 : KIND == kSplit ? sizeof(SplitLds<D>) : 2 * sizeof(TileBuffer<D>);
+  return KIND == kNone ? 0 : (KIND == kSplit ? sizeof(SplitLds<D>) : 2 * sizeof(TileBuffer<D>)) + (DRAFT ? sizeof(TreeLds<KIND, DRAFT>) : 0);
 }
 
 // One launch has the items of both kinds, the shared ones first: those are the longer ones, and the own ones fill the units as they
 // come free.  (In turn, eight of each, some units end up with more of the long ones: shared prompt 121 us, 93 so.)
-template <typename T, int D, int OWN, int SHARED, bool PAD, bool STREAM>
+template <typename T, int D, int OWN, int SHARED, bool PAD, bool STREAM, bool TREE>
 __global__ void __launch_bounds__(kThreads, D > 128 ? 1 : 2)
 attend_kernel(AttendArgs a, AttendCut own, AttendCut shared, Partials po, Partials ps, int n_shared) {
-  constexpr size_t LDS = lds_of<D, OWN>() > lds_of<D, SHARED>() ? lds_of<D, OWN>() : lds_of<D, SHARED>();
+  constexpr size_t LDS = lds_of<D, OWN, TREE>() > lds_of<D, SHARED, false>() ? lds_of<D, OWN, TREE>() : lds_of<D, SHARED, false>();
   __shared__ __attribute__((aligned(16))) char lds[LDS];
   int i = (int)blockIdx.x;
   if constexpr (SHARED != kNone) {
     if (i < n_shared) {
-      run_item<T, D, SHARED, PAD, true, STREAM>(a, shared, ps, i, lds);
+      run_item<T, D, SHARED, PAD, true, STREAM, TREE>(a, shared, ps, i, lds);
       return;
     }
     i -= n_shared;                                         // a multiple of 8: an item's die is its head's
   }
-  run_item<T, D, OWN, PAD, false, STREAM>(a, own, po, i, lds);
+  run_item<T, D, OWN, PAD, false, STREAM, TREE>(a, own, po, i, lds);
 }
 
-template <typename T, int D, int OWN, int SHARED, bool STREAM>
+template <typename T, int D, int OWN, int SHARED, bool STREAM, bool TREE>
 hipError_t launch_kinds(const AttendArgs& a, const AttendCut& own, const AttendCut& shared, const Partials& po, const Partials& ps,
                         hipStream_t st) {
   const int64_t rows = (int64_t)a.total_q * a.G;
@@ -1394,13 +1499,13 @@ hipError_t launch_kinds(const AttendArgs& a, const AttendCut& own, const AttendC
   if (n_own + n_shared >= (int64_t(1) << 31)) return hipErrorInvalidValue;
   const dim3 grid((unsigned)(n_own + n_shared)), block(kThreads);
   if (a.d == D)
-    hipLaunchKernelGGL((attend_kernel<T, D, OWN, SHARED, false, STREAM>), grid, block, 0, st, a, own, shared, po, ps, (int)n_shared);
+    hipLaunchKernelGGL((attend_kernel<T, D, OWN, SHARED, false, STREAM, TREE>), grid, block, 0, st, a, own, shared, po, ps, (int)n_shared);
   else
-    hipLaunchKernelGGL((attend_kernel<T, D, OWN, SHARED, true, STREAM>), grid, block, 0, st, a, own, shared, po, ps, (int)n_shared);
+    hipLaunchKernelGGL((attend_kernel<T, D, OWN, SHARED, true, STREAM, TREE>), grid, block, 0, st, a, own, shared, po, ps, (int)n_shared);
   return hipGetLastError();
 }
 
-template <typename T, int D>
+template <typename T, int D, bool TREE>
 hipError_t launch_d(const PagedWorkspace& ws, const AttendArgs& args, hipStream_t st) {
   AttendArgs a = args;
   constexpr bool kTiles = sizeof(T) == 2 && D <= 128;
@@ -1424,24 +1529,24 @@ hipError_t launch_d(const PagedWorkspace& ws, const AttendArgs& args, hipStream_
   const bool once = rule.most <= kSplit;                   // a sequence's keys are read by one tile of rows
   if constexpr (kTiles) {
     if (ks == kNone) {
-      e = own.rows == kTile2   ? launch_kinds<T, D, kTile2, kNone, true>(a, own, shared, po, ps, st)
-          : own.rows == kTile1 ? launch_kinds<T, D, kTile1, kNone, true>(a, own, shared, po, ps, st)
-          : once               ? launch_kinds<T, D, kSplit, kNone, true>(a, own, shared, po, ps, st)
-                               : launch_kinds<T, D, kSplit, kNone, false>(a, own, shared, po, ps, st);
+      e = own.rows == kTile2   ? launch_kinds<T, D, kTile2, kNone, true, TREE>(a, own, shared, po, ps, st)
+          : own.rows == kTile1 ? launch_kinds<T, D, kTile1, kNone, true, TREE>(a, own, shared, po, ps, st)
+          : once               ? launch_kinds<T, D, kSplit, kNone, true, TREE>(a, own, shared, po, ps, st)
+                               : launch_kinds<T, D, kSplit, kNone, false, TREE>(a, own, shared, po, ps, st);
     } else if (own.rows == kTile1) {
-      e = ks == kTile2   ? launch_kinds<T, D, kTile1, kTile2, true>(a, own, shared, po, ps, st)
-          : ks == kTile1 ? launch_kinds<T, D, kTile1, kTile1, true>(a, own, shared, po, ps, st)
-                         : launch_kinds<T, D, kTile1, kSplit, true>(a, own, shared, po, ps, st);
+      e = ks == kTile2   ? launch_kinds<T, D, kTile1, kTile2, true, TREE>(a, own, shared, po, ps, st)
+          : ks == kTile1 ? launch_kinds<T, D, kTile1, kTile1, true, TREE>(a, own, shared, po, ps, st)
+                         : launch_kinds<T, D, kTile1, kSplit, true, TREE>(a, own, shared, po, ps, st);
     } else {
-      e = ks == kTile2   ? launch_kinds<T, D, kSplit, kTile2, true>(a, own, shared, po, ps, st)
-          : ks == kTile1 ? launch_kinds<T, D, kSplit, kTile1, true>(a, own, shared, po, ps, st)
-                         : launch_kinds<T, D, kSplit, kSplit, false>(a, own, shared, po, ps, st);
+      e = ks == kTile2   ? launch_kinds<T, D, kSplit, kTile2, true, TREE>(a, own, shared, po, ps, st)
+          : ks == kTile1 ? launch_kinds<T, D, kSplit, kTile1, true, TREE>(a, own, shared, po, ps, st)
+                         : launch_kinds<T, D, kSplit, kSplit, false, TREE>(a, own, shared, po, ps, st);
     }
   } else if (ks == kNone) {
-    e = once ? launch_kinds<T, D, kSplit, kNone, true>(a, own, shared, po, ps, st)
-             : launch_kinds<T, D, kSplit, kNone, false>(a, own, shared, po, ps, st);
+    e = once ? launch_kinds<T, D, kSplit, kNone, true, TREE>(a, own, shared, po, ps, st)
+             : launch_kinds<T, D, kSplit, kNone, false, TREE>(a, own, shared, po, ps, st);
   } else {
-    e = launch_kinds<T, D, kSplit, kSplit, false>(a, own, shared, po, ps, st);
+    e = launch_kinds<T, D, kSplit, kSplit, false, TREE>(a, own, shared, po, ps, st);
   }
   if (e != hipSuccess || po.arrived != nullptr) return e;
   const int64_t out_rows = (int64_t)a.total_q * a.Hq;

@@ -59,6 +59,59 @@ hipError_t launch_pages_grow(const PageMap& map, int32_t* table, int32_t* kv_len
                              const int32_t* add, int n, int32_t* fresh, hipStream_t st);
 hipError_t launch_pages_free(const PageMap& map, int32_t* kv_len, int32_t* refs, const int32_t* rows, int n, hipStream_t st);
 
+struct RotateArgs {
+  PageMap map;             // asl_rotate_write's
+  const char* q;
+  const char* k;
+  const char* v;
+  char* q_out;
+  char* k_out;             // or the pages
+  char* v_out;             // the pages
+  const int32_t* pos;      // [n]
+  const int64_t* slot;     // [n]
+  const double* freqs;     // [rot / 2]
+  int64_t qt, qh, kt, kh, vt, vh, qot, qoh, kot, koh;      // strides in bytes
+  int32_t n, Hq, Hk, d, rot;
+  float cos_by, sin_by;
+  bool in_place;           // what is not rotated stands where it belongs
+  int32_t turned, units, parts, heads;                     // set by launch_rotate
+};
+// width: bytes of a piece, 16, 4 (neighbours: a pair) or an element.
+hipError_t launch_rotate(const RotateArgs& a, int dtype, bool halves, bool write, int width, hipStream_t st);
+
+struct PlanArgs {
+  PageMap map;
+  int32_t* table;
+  int32_t* kv_len;
+  int32_t* refs;
+  const int32_t* rows;     // [n]
+  const int32_t* add;      // [n] new tokens
+  const int32_t* parent;   // [total] or null
+  const int32_t* pruned;   // [n_rows] or null
+  int32_t* cu;             // [n + 1] out
+  int64_t* slot;           // [total] out
+  int32_t* pos;            // [total] out
+  int4* placed;            // [n] row, old length, whether it has grown: for a second launch
+  int32_t* fresh;
+  int32_t n, total;
+};
+hipError_t launch_pages_plan(const PlanArgs& a, hipStream_t st);
+
+struct AcceptArgs {
+  PageMap map;
+  int32_t* kv_len;
+  int32_t* refs;
+  const int32_t* rows;     // [n]
+  const int32_t* cu;       // [n + 1] where the drafts' nodes begin
+  const int32_t* path;     // [n][path_stride]
+  const int32_t* n_path;   // [n]
+  void* const* k_ptrs;     // device arrays [n_layers]
+  void* const* v_ptrs;
+  uint32_t* arrived;       // [n] zeros between calls
+  int32_t n, path_stride, n_layers, Hk, cpr, cpr_shift;
+};
+hipError_t launch_pages_accept(const AcceptArgs& a, hipStream_t st);
+
 struct AttendArgs {
   PageMap map;
   const void* q;
@@ -70,6 +123,7 @@ struct AttendArgs {
   const int32_t* cu_q;     // [n_seqs + 1]
   const int32_t* group_start;  // [n_groups + 1] or null
   const int32_t* prefix_len;   // [n_groups]
+  const int32_t* parent;   // [total_q] asl_tree_attention: a node's parent in its draft, or -1
   int64_t qt, qh, ot, oh;  // strides of q and out in elements
   int32_t Hq, Hk, G, d;
   int32_t n_seqs, total_q, max_q_len, max_kv_len, n_groups, causal;
@@ -77,6 +131,9 @@ struct AttendArgs {
   float scale;
 };
 hipError_t launch_attend(const PagedWorkspace& ws, const AttendArgs& a, int dtype, hipStream_t st);
+hipError_t launch_attend_tree(const PagedWorkspace& ws, const AttendArgs& a, int dtype, hipStream_t st);
+hipError_t launch_attend_tree_bf16_64(const PagedWorkspace& ws, const AttendArgs& a, hipStream_t st);
+hipError_t launch_attend_tree_bf16_128(const PagedWorkspace& ws, const AttendArgs& a, hipStream_t st);
 hipError_t launch_attend_bf16_64(const PagedWorkspace& ws, const AttendArgs& a, hipStream_t st);
 hipError_t launch_attend_bf16_128(const PagedWorkspace& ws, const AttendArgs& a, hipStream_t st);
 

@@ -2,6 +2,8 @@
 #pragma once
 #include <stdint.h>
 
+#include <cmath>
+
 #include "asl.h"
 #include "paged_index.h"
 
@@ -69,6 +71,66 @@ inline asl_status rows_status(const asl_pages& p, const asl_rows* r, const char*
   if (!whole_pieces(r->k_stride_tok, p.dtype) || !whole_pieces(r->k_stride_head, p.dtype) ||
       !whole_pieces(r->v_stride_tok, p.dtype) || !whole_pieces(r->v_stride_head, p.dtype))
     return no(ASL_EUNSUPPORTED, "strides of k and v must be multiples of 16 bytes");
+  return ASL_OK;
+}
+
+constexpr int kRotateMaxDim = 2048;        // head_dim of the rotations
+
+inline asl_status rotation_status(const asl_rotation* r, const char** why) {
+  auto no = [&](asl_status st, const char* text) { *why = text; return st; };
+  if (!r) return no(ASL_EINVAL, "rotation is null");
+  if (r->n_q_heads < 0 || r->n_kv_heads < 0) return no(ASL_EINVAL, "numbers of heads must be >= 0");
+  if (r->head_dim < 2 || r->rot_dim < 2 || r->rot_dim > r->head_dim || r->rot_dim % 2 != 0)
+    return no(ASL_EINVAL, "need rot_dim even, 2 <= rot_dim <= head_dim");
+  if (r->pairs != ASL_PAIRS_HALVES && r->pairs != ASL_PAIRS_NEIGHBOURS) return no(ASL_EINVAL, "unknown order of pairs");
+  if (r->flags & ~ASL_ROTATE_BACK) return no(ASL_EINVAL, "unknown bits in flags");
+  if (r->dtype != ASL_BF16 && r->dtype != ASL_F32) return no(ASL_EUNSUPPORTED, "dtype not supported");
+  if (r->head_dim % 2 != 0) return no(ASL_EUNSUPPORTED, "head_dim must be even");
+  if (r->head_dim > kRotateMaxDim) return no(ASL_EUNSUPPORTED, "head_dim > 2048 not supported");
+  if (r->n_q_heads > 65535 || r->n_kv_heads > 65535) return no(ASL_EUNSUPPORTED, "more than 65535 heads");
+  const int64_t strides[] = {r->q_stride_tok, r->q_stride_head, r->k_stride_tok, r->k_stride_head, r->v_stride_tok, r->v_stride_head,
+                             r->q_out_stride_tok, r->q_out_stride_head, r->k_out_stride_tok, r->k_out_stride_head};
+  for (int64_t x : strides)
+    if (x < 0) return no(ASL_EINVAL, "strides must be >= 0");
+  return ASL_OK;
+}
+
+// Bytes of the pieces in which a rotation takes rows whose addresses and strides are whole multiples of `align` bytes (a power of two): 16
+// where every part of a head is whole in them, else a pair of neighbours, or with halves 4 or an element.
+inline int rotate_width(const asl_rotation& r, int64_t align) {
+  const int eb = bytes_of(r.dtype), E = 16 / eb;
+  const int part = r.pairs == ASL_PAIRS_HALVES ? r.rot_dim / 2 : r.rot_dim;
+  if (align % 16 == 0 && part % E == 0 && (r.head_dim - r.rot_dim) % E == 0) return 16;
+  if (r.pairs == ASL_PAIRS_NEIGHBOURS) return 2 * eb;
+  return eb == 4 || (part % 2 == 0 && align % 4 == 0) ? 4 : 2;
+}
+
+// The radians that a position adds to the angle of each pair, for a length of context that a model was not made for.
+inline asl_status rotation_freqs(const asl_freqs* f, double* out) {
+  if (!f || !out || f->rot_dim < 2 || f->rot_dim % 2 != 0 || !(f->base > 0.)) return ASL_EINVAL;
+  if (f->kind < ASL_FREQS_PLAIN || f->kind > ASL_FREQS_PARTS) return ASL_EINVAL;
+  if (f->kind != ASL_FREQS_PLAIN && !(f->factor > 0.)) return ASL_EINVAL;
+  if (f->kind == ASL_FREQS_PARTS && (!(f->context > 0.) || !(f->high > f->low))) return ASL_EINVAL;
+  const int r = f->rot_dim;
+  const double base = f->kind != ASL_FREQS_BASE ? f->base : f->base * std::pow(f->factor, r / (r > 2 ? r - 2. : 1.));
+  for (int i = 0; i < r / 2; ++i) {
+    double x = std::pow(base, -2. * i / r);
+    if (f->kind == ASL_FREQS_LINEAR) x /= f->factor;
+    if (f->kind == ASL_FREQS_PARTS) {
+      double keep = (f->context * x / 6.283185307179586 - f->low) / (f->high - f->low);
+      keep = keep < 0. ? 0. : keep > 1. ? 1. : keep;
+      x *= keep + (1. - keep) / f->factor;
+    }
+    out[i] = x;
+  }
+  return ASL_OK;
+}
+
+// asl_attn of asl_tree_attention, beside attn_status.
+inline asl_status tree_status(const asl_attn& a, const char** why) {
+  auto no = [&](asl_status st, const char* text) { *why = text; return st; };
+  if (a.flags != ASL_ATTN_CAUSAL) return no(ASL_EINVAL, "nodes are their sequence's last tokens: flags must be ASL_ATTN_CAUSAL");
+  if (a.max_q_len > kTreeNodes) return no(ASL_EUNSUPPORTED, "a draft of more than 512 nodes");
   return ASL_OK;
 }
 
