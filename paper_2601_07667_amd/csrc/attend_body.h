@@ -1097,8 +1097,8 @@ __device__ __forceinline__ uint32_t fetch_tile(TileBuffer<D>& to, const Source& 
 // A wavefront's step over a tile in LDS.  MASKED: some row may not see some key, or its reference may have to move.  Else every row
 // sees every key and no reference moves; returns false, nothing done, if one has to.  (A branch that rescales the accumulators
 // makes the compiler keep them twice, which does not fit the registers: the prefill chunk took 1629 us with it and 1142 without.)
-template <int D, int MT, bool PAD, bool MASKED, bool DRAFT>
-__device__ __forceinline__ bool tile_step(Rows<__bf16, D, MT, DRAFT>& R, const TileBuffer<D>& b, int key0, uint32_t ok, int least, int most,
+template <int D, int MT, bool PAD, bool MASKED>
+__device__ __forceinline__ bool tile_step(Rows<__bf16, D, MT>& R, const TileBuffer<D>& b, int key0, uint32_t ok, int least, int most,
                                           int d, float scale) {
   typedef Block<__bf16, D> B;
   const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
@@ -1150,19 +1150,11 @@ __device__ __forceinline__ bool tile_step(Rows<__bf16, D, MT, DRAFT>& R, const T
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
     float top = -INFINITY;
-    uint32_t sight[2] = {0, 0};
-    if constexpr (MASKED && DRAFT) {
-      sight[0] = R.window(mt, R.lim[mt], key0) >> (4 * g);
-      sight[1] = R.window(mt, R.lim[mt], key0 + 32) >> (4 * g);
-    }
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        if (MASKED) {
-          const bool sees = DRAFT ? ((sight[t >> 1] >> (16 * (t & 1) + i)) & 1u) != 0 : key0 + 16 * t + 4 * g + i < R.lim[mt];
-          x[mt][t][i] = ((ok >> t) & 1u) != 0 && sees ? x[mt][t][i] : -INFINITY;
-        }
+        if (MASKED) x[mt][t][i] = ((ok >> t) & 1u) != 0 && key0 + 16 * t + 4 * g + i < R.lim[mt] ? x[mt][t][i] : -INFINITY;
         top = fmaxf(top, x[mt][t][i]);
       }
     tops[mt] = top * scale;
@@ -1238,13 +1230,12 @@ __device__ __forceinline__ bool tile_step(Rows<__bf16, D, MT, DRAFT>& R, const T
   return true;
 }
 
-template <int D, int MT, bool PAD, bool SHARED, bool TREE>
+template <int D, int MT, bool PAD, bool SHARED>
 __device__ __forceinline__ void tile_item(const AttendArgs& a, const AttendCut& cut, const Partials& pt, int item, char* lds) {
   typedef Block<__bf16, D> B;
-  constexpr bool DRAFT = TREE && !SHARED;
   TileBuffer<D>* buf = (TileBuffer<D>*)lds;
   Item it;
-  if (!find_item<SHARED, TREE>(a, cut, item, pt, &it)) return;
+  if (!find_item<SHARED, false>(a, cut, item, pt, &it)) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r16 = lane & 15, g = lane >> 4;
   const int row0 = it.tile * cut.rows + wave * 16 * MT;
   const Source src = source_of(a, it);
@@ -1252,18 +1243,17 @@ __device__ __forceinline__ void tile_item(const AttendArgs& a, const AttendCut& 
   tiles_of<SHARED>(a, it, cut.rows, &t0, &t1);
   PageWindow<4, kKeyTile> window;                          // (ahead of the queries and limits, which wait for loads of their own)
   if (t0 < t1) window.start(src, t0 * kKeyTile);
-  Rows<__bf16, D, MT, DRAFT> rows;
+  Rows<__bf16, D, MT> rows;
   rows.clear();
-  const int all = SHARED ? least_limit<TREE>(a, it.seg) : 0;
-  const int context = DRAFT ? context_of(it.seg.len, it.seg.rows / a.G) : 0;
+  const int all = SHARED ? least_limit<false>(a, it.seg) : 0;
   uint32_t least = 0x7fffffffu, most = 0;
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
     const int r = row0 + 16 * mt + r16;
     const bool in = r < it.seg.rows;
-    rows.lim[mt] = in ? row_limit<SHARED, TREE>(a, it.seg, r, all) : 0;
+    rows.lim[mt] = in ? row_limit<SHARED, false>(a, it.seg, r, all) : 0;
     if (!in) rows.m[mt] = 0.f;                             // rows that are not there have logits 0: no reference to move for them
-    least = min(least, in ? (uint32_t)(DRAFT ? context : rows.lim[mt]) : 0x7fffffffu);
+    least = min(least, in ? (uint32_t)rows.lim[mt] : 0x7fffffffu);
     most = max(most, (uint32_t)rows.lim[mt]);
     const int i = (int)((uint32_t)r / (uint32_t)a.G);
     const __bf16* q = (const __bf16*)a.q + (int64_t)(it.seg.c0 + i) * a.qt + (int64_t)(it.h * a.G + (r - i * a.G)) * a.qh;
@@ -1275,17 +1265,8 @@ __device__ __forceinline__ void tile_item(const AttendArgs& a, const AttendCut& 
   }
   least = wave_min(least);
   most = wave_max(most);
-  if constexpr (DRAFT) {
-    TreeLds<64 * MT, true>& tree = *(TreeLds<64 * MT, true>*)(lds + 2 * sizeof(TileBuffer<D>));
-    rows.base = it.seg.len - it.seg.rows / a.G;
-    const int i0 = (int)((uint32_t)(it.tile * cut.rows) / (uint32_t)a.G);
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
-      rows.bits[mt] = tree.bits[min((int)((uint32_t)(row0 + 16 * mt + r16) / (uint32_t)a.G) - i0, 64 * MT - 1)];
-    if (t1 * kKeyTile > context) read_tree<64 * MT>(a, it.seg, it.tile * cut.rows, tree);   // (else no key of the draft is looked at)
-  }
   // keys that all rows of the workgroup see (an own segment's limits rise with the row)
-  const int all_see = SHARED ? all : DRAFT ? context : row_limit<SHARED, TREE>(a, it.seg, it.tile * cut.rows, 0);
+  const int all_see = SHARED ? all : row_limit<SHARED, false>(a, it.seg, it.tile * cut.rows, 0);
   const float scale = a.scale * kLog2e;
   bool bad = false;
   if (t0 < t1) {
@@ -1312,7 +1293,7 @@ __device__ __forceinline__ void tile_item(const AttendArgs& a, const AttendCut& 
       const int key0 = t * kKeyTile;
       bad = bad || here != 15u;
       if (key0 < (int)most)
-        tile_step<D, MT, PAD, true, DRAFT>(rows, buf[(t - t0) & 1], key0, here, (int)least, (int)most, a.d, scale);
+        tile_step<D, MT, PAD, true>(rows, buf[(t - t0) & 1], key0, here, (int)least, (int)most, a.d, scale);
       fetched = false;
       ++t;
       window.move(src, t - t0);
@@ -1320,7 +1301,7 @@ __device__ __forceinline__ void tile_item(const AttendArgs& a, const AttendCut& 
       // one a tile.)
       while (t < t1 && ok == 15u && (t + 1) * kKeyTile <= all_see) {
         here = next();
-        fetched = !tile_step<D, MT, PAD, false, DRAFT>(rows, buf[(t - t0) & 1], t * kKeyTile, 15u, (int)least, (int)most, a.d, scale);
+        fetched = !tile_step<D, MT, PAD, false>(rows, buf[(t - t0) & 1], t * kKeyTile, 15u, (int)least, (int)most, a.d, scale);
         if (fetched) break;
         ++t;
         window.move(src, t - t0);
@@ -1461,11 +1442,16 @@ __global__ void __launch_bounds__(NW > kWaves ? NW * 64 : kThreads) attend_join_
 }
 
 // ------------------------------------------------------------------------------------------------------------------
+// The tile items of drafted trees (attend_steps.h).
+template <int D, bool PAD, bool SHARED>
+__device__ __forceinline__ void step_item(const AttendArgs& a, const AttendCut& cut, const Partials& pt, int item, char* lds);
+
 template <typename T, int D, int KIND, bool PAD, bool SHARED, bool STREAM, bool TREE>
 __device__ __forceinline__ void run_item(const AttendArgs& a, const AttendCut& cut, const Partials& pt, int item, char* lds) {
   if constexpr (KIND == kSplit) split_item<T, D, 1, PAD, SHARED, STREAM, TREE>(a, cut, pt, item, lds);
-  if constexpr (KIND == kTile1) tile_item<D, 1, PAD, SHARED, TREE>(a, cut, pt, item, lds);
-  if constexpr (KIND == kTile2) tile_item<D, 2, PAD, SHARED, TREE>(a, cut, pt, item, lds);
+  if constexpr (KIND == kTile2 && TREE) step_item<D, PAD, SHARED>(a, cut, pt, item, lds);
+  if constexpr (KIND == kTile1 && !TREE) tile_item<D, 1, PAD, SHARED>(a, cut, pt, item, lds);
+  if constexpr (KIND == kTile2 && !TREE) tile_item<D, 2, PAD, SHARED>(a, cut, pt, item, lds);
 }
 template <int D, int KIND, bool DRAFT>
 constexpr size_t lds_of() {
@@ -1509,7 +1495,8 @@ template <typename T, int D, bool TREE>
 hipError_t launch_d(const PagedWorkspace& ws, const AttendArgs& args, hipStream_t st) {
   AttendArgs a = args;
   constexpr bool kTiles = sizeof(T) == 2 && D <= 128;
-  const AttendRule rule = rule_for(kTiles, a.total_q, a.G, a.Hk, a.n_seqs, a.n_groups, a.max_q_len, a.max_kv_len, a.key_bytes, ws.part_rows);
+  const AttendRule rule = rule_for(kTiles, a.total_q, a.G, a.Hk, a.n_seqs, a.n_groups, a.max_q_len, a.max_kv_len, a.key_bytes, ws.part_rows,
+                                   TREE);
   const AttendCut own = rule.own, shared = rule.shared;
   if (!rule.groups) a.n_groups = 0;
   Partials po, ps;
@@ -1527,7 +1514,18 @@ hipError_t launch_d(const PagedWorkspace& ws, const AttendArgs& args, hipStream_
   hipError_t e = hipErrorInvalidValue;
   const int ks = a.n_groups > 0 ? shared.rows : kNone;
   const bool once = rule.most <= kSplit;                   // a sequence's keys are read by one tile of rows
-  if constexpr (kTiles) {
+  if constexpr (kTiles && TREE) {
+    if (ks == kNone)
+      e = own.rows == kTile2 ? launch_kinds<T, D, kTile2, kNone, true, TREE>(a, own, shared, po, ps, st)
+          : once             ? launch_kinds<T, D, kSplit, kNone, true, TREE>(a, own, shared, po, ps, st)
+                             : launch_kinds<T, D, kSplit, kNone, false, TREE>(a, own, shared, po, ps, st);
+    else if (own.rows == kTile2)
+      e = ks == kTile2 ? launch_kinds<T, D, kTile2, kTile2, true, TREE>(a, own, shared, po, ps, st)
+                       : launch_kinds<T, D, kTile2, kSplit, true, TREE>(a, own, shared, po, ps, st);
+    else
+      e = ks == kTile2 ? launch_kinds<T, D, kSplit, kTile2, true, TREE>(a, own, shared, po, ps, st)
+                       : launch_kinds<T, D, kSplit, kSplit, false, TREE>(a, own, shared, po, ps, st);
+  } else if constexpr (kTiles) {
     if (ks == kNone) {
       e = own.rows == kTile2   ? launch_kinds<T, D, kTile2, kNone, true, TREE>(a, own, shared, po, ps, st)
           : own.rows == kTile1 ? launch_kinds<T, D, kTile1, kNone, true, TREE>(a, own, shared, po, ps, st)

@@ -80,6 +80,18 @@ ASL_HD AttendCut cut_for(bool tiles, int64_t rows, int64_t keys, int64_t segment
   return AttendCut{kSplit, 512, 2, 0};
 }
 
+// The same for drafted trees, which have tiles of 128 rows alone (attend_steps.h).  An item takes 10 us to begin and its pieces 9 to 16 to be
+// joined, so where there are tiles for three quarters of the units a span of up to 128 key tiles is one piece (32 sequences of 2300
+// keys, 16 to 32 nodes, 8 heads: 82 us, in two pieces each 108); where there are not, spans are cut for two items a unit (60 nodes on 131089
+// keys, 4 heads: 186 us, with 384 items 196, with 256 207).  Shared ones into about 192 (8 prompts of 2090 keys for 6 sequences
+// each: 46.6 us, with 128 46.8, with 256 47.5, with 384 54.5, with 96 64).
+ASL_HD AttendCut cut_for_tree(bool tiles, int64_t rows, int64_t keys, int64_t segments, int Hk, bool shared) {
+  AttendCut c = cut_for(tiles, rows, keys, segments, Hk, shared);
+  if (c.rows == kSplit) return c;
+  const int64_t row_tiles = (rows + kTile2 - 1) / kTile2 * segments * Hk;
+  return AttendCut{kTile2, shared ? 192 : 512, !shared && row_tiles >= 192 ? 128 : 8, 0};
+}
+
 // What the host decides about a call.
 struct AttendRule {
   AttendCut own, shared;
@@ -90,17 +102,17 @@ struct AttendRule {
 
 // tiles: the type and head size have tile items; room: rows of pieces in the workspace.
 ASL_HD AttendRule rule_for(bool tiles, int64_t total_q, int G, int Hk, int n_seqs, int n_groups, int max_q_len, int max_kv_len,
-                           int key_bytes, int64_t room) {
+                           int key_bytes, int64_t room, bool tree = false) {
   AttendRule r;
   const int64_t rows = total_q * G;                        // of a KV head
   r.most = (int64_t)max_q_len * G < rows ? (int64_t)max_q_len * G : rows;
-  r.own = cut_for(tiles, r.most, max_kv_len, n_seqs, Hk, false);
-  r.shared = cut_for(tiles, n_groups > 0 ? rows / n_groups : 0, max_kv_len, n_groups, Hk, true);
+  r.own = (tree ? cut_for_tree : cut_for)(tiles, r.most, max_kv_len, n_seqs, Hk, false);
+  r.shared = (tree ? cut_for_tree : cut_for)(tiles, n_groups > 0 ? rows / n_groups : 0, max_kv_len, n_groups, Hk, true);
   r.shared.cap = max_partials(r.shared, rows, Hk);
-  // a sequence whose own rows fill a tile gains nothing, and groups cannot save more than all sequences' keys but one each (kMinSaved);
+  // a sequence whose own rows fill a tile gains nothing (drafts: fill more than one), and groups cannot save more than all sequences' keys but one each (kMinSaved);
   // every row of a group is joined from two parts, for which there has to be room
   const double most_saved = (double)(n_seqs - n_groups) * (double)max_kv_len * (double)key_bytes;
-  r.groups = n_groups > 0 && r.own.rows != kTile2 && most_saved >= (double)kMinSaved && r.shared.cap + rows * Hk <= room;
+  r.groups = n_groups > 0 && (tree ? r.most <= kTile2 : r.own.rows != kTile2) && most_saved >= (double)kMinSaved && r.shared.cap + rows * Hk <= room;
   if (!r.groups) r.shared.cap = 0;
   r.own.cap = room - r.shared.cap;
   // few pieces are joined by the workgroup that brings the last one

@@ -1,6 +1,6 @@
 // Attention of drafted trees over a paged cache (attend_body.h): which kernels a call takes.  Those of bf16 with d <= 64 and of d <= 128 are
 // compiled apart, in attend_tree_64.hip and attend_tree_128.hip.
-#include "attend_body.h"
+#include "attend_steps.h"
 
 namespace asl {
 

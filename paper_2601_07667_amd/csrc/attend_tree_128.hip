@@ -1,5 +1,5 @@
 // The kernels of attend_body.h for drafted trees, bf16 and d <= 128.
-#include "attend_body.h"
+#include "attend_steps.h"
 
 namespace asl {
 
