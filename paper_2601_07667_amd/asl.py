@@ -192,36 +192,29 @@ def _batch_of(attn, q, out, lse):
     return a
 
 
-def _rotation_of(rotation, **tensors):
-    """The description of a rotation with the strides of this call's tensors."""
-    r = AslRotation.from_buffer_copy(rotation)
-    for name, t in tensors.items():
-        if t is None:
-            continue
-        tok, head, one = t.stride()
-        if one != 1:
-            _refuse_gaps(**{name: t})
-        setattr(r, name + "_stride_tok", tok)
-        setattr(r, name + "_stride_head", head)
-    return r
+def _heads_of(name, t, n: int, heads: int, d: int):
+    """The strides of t [n, heads, d] from token to token and from head to head."""
+    if heads == 0:
+        return 0, 0
+    if t is None or t.shape != (n, heads, d):
+        raise AslError(ASL_EINVAL, f"{name} must be [{n}, {heads}, {d}] (it is {None if t is None else tuple(t.shape)})")
+    tok, head, one = t.stride()
+    if one != 1:
+        _refuse_gaps(**{name: t})
+    return tok, head
 
 
-def _tokens_of(r, pos, freqs, *tensors) -> int:
-    """The number of tokens of a rotation, whose tensors have to agree on it."""
-    n = pos.shape[0]
-    for name, t, heads in tensors:
-        if heads > 0 and (t is None or tuple(t.shape) != (n, heads, r.head_dim)):
-            raise AslError(ASL_EINVAL, f"{name} must be [{n}, {heads}, {r.head_dim}] (it is {None if t is None else tuple(t.shape)})")
-    _list_of("pos", pos, n, "int32")
-    _list_of("freqs", freqs, r.rot_dim // 2, "float64")
-    return n
+_TYPES = {}
 
 
 def _list_of(name, t, n: int, dtype: str) -> None:
     """A list that a call reads or writes n entries of, one behind the other."""
     if t is None and n == 0:
         return
-    if t is None or t.numel() < n or not t.is_contiguous() or str(t.dtype) != "torch." + dtype:
+    if not _TYPES:
+        import torch
+        _TYPES.update(int32=torch.int32, int64=torch.int64, float64=torch.float64)
+    if t is None or t.numel() < n or t.dtype is not _TYPES[dtype] or not t.is_contiguous():
         raise AslError(ASL_EINVAL, f"{name} must be {n} x {dtype} without gaps (it is "
                                    f"{None if t is None else (tuple(t.shape), tuple(t.stride()), str(t.dtype))})")
 
@@ -424,16 +417,27 @@ class Asl:
     # -- drafting over the paged cache -------------------------------------------------------------
     def asl_rotate(self, rotation: AslRotation, q, k, pos, freqs, q_out, k_out) -> None:
         """q, q_out: [n, Hq, d], k, k_out: [n, Hk, d] of any strides (d contiguous); None where the rotation has no such heads."""
-        r = _rotation_of(rotation, q=q, k=k, q_out=q_out, k_out=k_out)
-        n = _tokens_of(r, pos, freqs, ("q", q, r.n_q_heads), ("k", k, r.n_kv_heads), ("q_out", q_out, r.n_q_heads),
-                       ("k_out", k_out, r.n_kv_heads))
+        r = AslRotation.from_buffer_copy(rotation)           # (the description may be another thread's too)
+        n, Hq, Hk, d = pos.shape[0], r.n_q_heads, r.n_kv_heads, r.head_dim
+        r.q_stride_tok, r.q_stride_head = _heads_of("q", q, n, Hq, d)
+        r.k_stride_tok, r.k_stride_head = _heads_of("k", k, n, Hk, d)
+        r.q_out_stride_tok, r.q_out_stride_head = _heads_of("q_out", q_out, n, Hq, d)
+        r.k_out_stride_tok, r.k_out_stride_head = _heads_of("k_out", k_out, n, Hk, d)
+        _list_of("pos", pos, n, "int32")
+        _list_of("freqs", freqs, r.rot_dim // 2, "float64")
         self._check(self.lib.asl_rotate(self.h, C.byref(r), _ptr(q), _ptr(k), _ptr(pos), _ptr(freqs), n, _ptr(q_out), _ptr(k_out),
                                         _stream()))
 
     def asl_rotate_write(self, pages: AslPages, rotation: AslRotation, q, k, v, pos, slot, freqs, q_out, k_pages, v_pages) -> None:
         """q, q_out: [n, Hq, d], k, v: [n, Hk, d] of any strides (d contiguous); slot: [n] int64."""
-        r = _rotation_of(rotation, q=q, k=k, v=v, q_out=q_out)
-        n = _tokens_of(r, pos, freqs, ("q", q, r.n_q_heads), ("k", k, r.n_kv_heads), ("v", v, r.n_kv_heads), ("q_out", q_out, r.n_q_heads))
+        r = AslRotation.from_buffer_copy(rotation)
+        n, Hq, Hk, d = pos.shape[0], r.n_q_heads, r.n_kv_heads, r.head_dim
+        r.q_stride_tok, r.q_stride_head = _heads_of("q", q, n, Hq, d)
+        r.k_stride_tok, r.k_stride_head = _heads_of("k", k, n, Hk, d)
+        r.v_stride_tok, r.v_stride_head = _heads_of("v", v, n, Hk, d)
+        r.q_out_stride_tok, r.q_out_stride_head = _heads_of("q_out", q_out, n, Hq, d)
+        _list_of("pos", pos, n, "int32")
+        _list_of("freqs", freqs, r.rot_dim // 2, "float64")
         _list_of("slot", slot, n, "int64")
         self._check(self.lib.asl_rotate_write(self.h, C.byref(pages), C.byref(r), _ptr(q), _ptr(k), _ptr(v), _ptr(pos), _ptr(slot),
                                               _ptr(freqs), n, _ptr(q_out), _ptr(k_pages), _ptr(v_pages), _stream()))

@@ -885,13 +885,28 @@ struct TreeLds<M, true> {
   int16_t parent[kTreeNodes];
 };
 
+// A thread's parents of segment s's nodes, loaded ahead of what else its item waits for.
+struct Parents {
+  static constexpr int N = kTreeNodes / kThreads;
+  int p[N];
+  __device__ __forceinline__ void load(const AttendArgs& a, const Segment& s) {
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+      const int i = u * kThreads + (int)threadIdx.x;
+      p[u] = i < s.rows / a.G ? a.parent[s.c0 + i] : -1;
+    }
+  }
+};
+
 // Fills l for rows tile_row0 .. tile_row0 + M - 1 of segment s (M rows have at most M nodes).  Every thread of the workgroup calls it.
 template <int M>
-__device__ __forceinline__ void read_tree(const AttendArgs& a, const Segment& s, int tile_row0, TreeLds<M, true>& l) {
+__device__ __forceinline__ void read_tree(const AttendArgs& a, const Segment& s, const Parents& parents, int tile_row0, TreeLds<M, true>& l) {
   const int n = s.rows / a.G, i0 = (int)((uint32_t)tile_row0 / (uint32_t)a.G);
   bool bad = false;
-  for (int i = threadIdx.x; i < n; i += kThreads) {
-    const int p = a.parent[s.c0 + i];
+#pragma unroll
+  for (int u = 0; u < Parents::N; ++u) {
+    const int i = u * kThreads + (int)threadIdx.x, p = parents.p[u];
+    if (i >= n) continue;
     const bool in = p >= -1 && p < i;
     bad = bad || !in;
     l.parent[i] = (int16_t)(in ? p : -1);
@@ -937,6 +952,8 @@ __device__ __forceinline__ void split_item(const AttendArgs& a, const AttendCut&
   tiles_of<SHARED>(a, it, cut.rows, &t0, &t1);
   constexpr int STEP = kWaves * B::KEYS;
   int key = t0 * kKeyTile + wave * B::KEYS;
+  Parents parents;
+  if constexpr (DRAFT) parents.load(a, it.seg);
   PageWindow<B::SUB, STEP> window;                         // (ahead of the queries and limits, which wait for loads of their own)
   if (t0 < t1) window.start(src, key);
   Rows<T, D, MT, DRAFT> rows;
@@ -968,7 +985,7 @@ __device__ __forceinline__ void split_item(const AttendArgs& a, const AttendCut&
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
       rows.bits[mt] = tree.bits[min((int)((uint32_t)(it.tile * cut.rows + 16 * mt + r16) / (uint32_t)a.G) - i0, 16 * MT - 1)];
-    if (t1 * kKeyTile > context) read_tree<16 * MT>(a, it.seg, it.tile * cut.rows, tree);   // (else no key of the draft is looked at)
+    if (t1 * kKeyTile > context) read_tree<16 * MT>(a, it.seg, parents, it.tile * cut.rows, tree);   // (else no key of the draft is looked at)
   }
   const int end = min(t1 * kKeyTile, (int)most);
   const float scale = a.scale * kLog2e;

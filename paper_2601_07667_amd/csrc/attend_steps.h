@@ -344,8 +344,10 @@ __device__ __forceinline__ void step_item(const AttendArgs& a, const AttendCut& 
   int t0, t1;
   tiles_of<SHARED>(a, it, kTile2, &t0, &t1);
   const int key_first = t0 * kKeyTile, steps = (t1 - t0) * (kKeyTile / kStep);
-  // (the first page numbers ahead of the queries and limits, which wait for loads of their own)
+  // (the first page numbers and the parents ahead of the queries and limits, which wait for loads of their own)
   int number = 0;
+  Parents parents;
+  if constexpr (DRAFT) parents.load(a, it.seg);
   if (steps > 0) number = src.table[min(key_first + (lane >> 1) * kStep + 16 * (lane & 1), src.last) >> src.shift];
   StepRows<D, DRAFT> rows;
   rows.odd = 0;
@@ -395,7 +397,7 @@ __device__ __forceinline__ void step_item(const AttendArgs& a, const AttendCut& 
     TreeLds<kTile2, true>& tree = *(TreeLds<kTile2, true>*)(lds + sizeof(StepRing<D>));
     rows.base = it.seg.len - it.seg.rows / a.G;
     rows.bits[0] = tree.bits[min((int)((uint32_t)r / (uint32_t)a.G) - (int)((uint32_t)(it.tile * kTile2) / (uint32_t)a.G), kTile2 - 1)];
-    if (t1 * kKeyTile > context) read_tree<kTile2>(a, it.seg, it.tile * kTile2, tree);      // (else no key of the draft is looked at)
+    if (t1 * kKeyTile > context) read_tree<kTile2>(a, it.seg, parents, it.tile * kTile2, tree);      // (else no key of the draft is looked at)
   }
   const int all_see = SHARED ? all : context;              // keys that all rows of the workgroup see
   const float scale = a.scale * kLog2e;

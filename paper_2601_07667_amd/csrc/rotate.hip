@@ -35,12 +35,22 @@ struct Chunk {
   static constexpr int E = W / (int)sizeof(T);
   typedef T Elements __attribute__((ext_vector_type(E), aligned(W == 16 ? 16 : sizeof(T))));
   Elements x;
+
+  // STREAM: past the caches (transfers that do not fit them anyway).
+  template <bool STREAM>
+  __device__ __forceinline__ void load(const char* p) {
+    x = STREAM ? __builtin_nontemporal_load((const Elements*)p) : *(const Elements*)p;
+  }
+  template <bool STREAM>
+  __device__ __forceinline__ void store(char* p) const {
+    if (STREAM) __builtin_nontemporal_store(x, (Elements*)p); else *(Elements*)p = x;
+  }
 };
 
 // A wavefront has some heads of a token: a lane has unit u of every so many-th head, so that the angles of its pairs, which the lanes
 // work out together once, stay in its registers.  Units of a head (E elements in W bytes): rotated ones, with halves E pairs in two
 // pieces, with neighbours E / 2 pairs in one; then the pieces of the rest.  A head of values (WRITE) is copied by the same units.
-template <typename T, int W, bool HALVES, bool WRITE>
+template <typename T, int W, bool HALVES, bool WRITE, bool STREAM>
 __global__ void __launch_bounds__(kThreads) rotate_kernel(RotateArgs a) {
   typedef Chunk<T, W> C;
   constexpr int E = C::E, PAIRS = HALVES ? E : E / 2;
@@ -106,8 +116,8 @@ __global__ void __launch_bounds__(kThreads) rotate_kernel(RotateArgs a) {
           second[k] = v2;
         }
         if (to[k] == nullptr) continue;
-        x[k] = *(const C*)(from + first[k]);
-        if (second[k] >= 0) y[k] = *(const C*)(from + second[k]);
+        x[k].template load<STREAM>(from + first[k]);
+        if (second[k] >= 0) y[k].template load<STREAM>(from + second[k]);
       }
 #pragma unroll
       for (int k = 0; k < kUnroll; ++k) {
@@ -129,30 +139,44 @@ __global__ void __launch_bounds__(kThreads) rotate_kernel(RotateArgs a) {
             }
           }
         }
-        *(C*)(to[k] + first[k]) = x[k];
-        if (second[k] >= 0) *(C*)(to[k] + second[k]) = y[k];
+        x[k].template store<STREAM>(to[k] + first[k]);
+        if (second[k] >= 0) y[k].template store<STREAM>(to[k] + second[k]);
       }
     }
   }
 }
 
+// Bytes read and written from which a rotation goes past the caches (32768 tokens, 40 heads of 128, 671 MB: 134 us, so 117 = 5.8 TB/s; 4085
+// tokens, 36 heads of 128, 75 MB that the caches hold: 16.3, 20.1).
+constexpr int64_t kRotateStreamBytes = int64_t(100) << 20;
+
 template <typename T, int W, bool HALVES>
-void launch(const RotateArgs& a, bool write, dim3 grid, size_t lds, hipStream_t st) {
+void launch(const RotateArgs& a, bool write, bool stream, dim3 grid, size_t lds, hipStream_t st) {
+  if constexpr (W == 16) {
+    if (stream) {
+      if (write)
+        hipLaunchKernelGGL((rotate_kernel<T, W, HALVES, true, true>), grid, dim3(kThreads), lds, st, a);
+      else
+        hipLaunchKernelGGL((rotate_kernel<T, W, HALVES, false, true>), grid, dim3(kThreads), lds, st, a);
+      return;
+    }
+  }
   if (write)
-    hipLaunchKernelGGL((rotate_kernel<T, W, HALVES, true>), grid, dim3(kThreads), lds, st, a);
+    hipLaunchKernelGGL((rotate_kernel<T, W, HALVES, true, false>), grid, dim3(kThreads), lds, st, a);
   else
-    hipLaunchKernelGGL((rotate_kernel<T, W, HALVES, false>), grid, dim3(kThreads), lds, st, a);
+    hipLaunchKernelGGL((rotate_kernel<T, W, HALVES, false, false>), grid, dim3(kThreads), lds, st, a);
 }
 
 template <typename T>
 void launch_type(const RotateArgs& a, int width, bool halves, bool write, dim3 grid, size_t lds, hipStream_t st) {
+  const bool stream = 2 * (int64_t)a.n * (a.Hq + a.Hk * (write ? 2 : 1)) * a.d * (int64_t)sizeof(T) >= kRotateStreamBytes;
   if (halves) {
-    if (width == 16) launch<T, 16, true>(a, write, grid, lds, st);
-    else if (width == 4) launch<T, 4, true>(a, write, grid, lds, st);
-    else if constexpr (sizeof(T) < 4) launch<T, 2, true>(a, write, grid, lds, st);
+    if (width == 16) launch<T, 16, true>(a, write, stream, grid, lds, st);
+    else if (width == 4) launch<T, 4, true>(a, write, stream, grid, lds, st);
+    else if constexpr (sizeof(T) < 4) launch<T, 2, true>(a, write, stream, grid, lds, st);
   } else {
-    if (width == 16) launch<T, 16, false>(a, write, grid, lds, st);
-    else launch<T, 2 * sizeof(T), false>(a, write, grid, lds, st);
+    if (width == 16) launch<T, 16, false>(a, write, stream, grid, lds, st);
+    else launch<T, 2 * sizeof(T), false>(a, write, stream, grid, lds, st);
   }
 }
 

@@ -110,6 +110,32 @@ def test_rotate_sizes(ctx, gpu_device, n, Hq, Hk, dtype):
 
 
 @pytest.mark.parametrize("halves", [True, False])
+def test_rotations_too_large_for_the_caches(ctx, gpu_device, halves):
+    """Calls of more than 100 MB take kernels of their own: the same bits as in two smaller calls, in place, and into pages."""
+    torch = _torch()
+    dev, n, Hq, Hk, d, ps = gpu_device, 4100, 40, 8, 128, 64
+    g = torch.Generator(device=dev).manual_seed(1)
+    x = torch.randn((n, Hq + 2 * Hk, d), generator=g, device=dev).to(torch.bfloat16)
+    q, k, v = x[:, :Hq], x[:, Hq:Hq + Hk], x[:, Hq + Hk:]
+    pos, f = _ints(np.arange(n) * 7, dev), torch.from_numpy(do.freqs(d)).to(dev)
+    r = asl.make_rotation(Hq, Hk, d, pairs=0 if halves else 1)
+    parts = [torch.empty((n, H, d), dtype=torch.bfloat16, device=dev) for H in (Hq, Hk)]
+    for a, b in ((0, 2000), (2000, n)):
+        ctx.asl_rotate(r, q[a:b], k[a:b], pos[a:b], f, parts[0][a:b], parts[1][a:b])
+    whole = [torch.empty_like(t) for t in parts]
+    ctx.asl_rotate(r, q, k, pos, f, *whole)
+    assert torch.equal(whole[0], parts[0]) and torch.equal(whole[1], parts[1])
+    pages = [torch.zeros((n // ps + 1, Hk, ps, d), dtype=torch.bfloat16, device=dev) for _ in range(2)]
+    out = torch.empty_like(parts[0])
+    ctx.asl_rotate_write(asl.make_pages(Hq, Hk, d, ps, n // ps + 1, 1, 1), r, q, k, v, pos, _longs(np.arange(n), dev), f, out, *pages)
+    assert torch.equal(out, parts[0])
+    for t, want in zip(pages, (parts[1], v)):
+        assert torch.equal(t.transpose(1, 2).reshape(-1, Hk, d)[:n], want)
+    ctx.asl_rotate(r, q, k, pos, f, q, k)
+    assert torch.equal(q, parts[0]) and torch.equal(k, parts[1]) and ctx.asl_device_fault() == 0
+
+
+@pytest.mark.parametrize("halves", [True, False])
 def test_rotate_far_positions(ctx, gpu_device, halves):
     """Angles of millions of turns, to the last bit of fp32."""
     pos = [0, 1, -1, 131071, 1048575, 10 ** 7 + 1, 2 ** 31 - 1, -2 ** 31, 2 ** 30 + 12345]
