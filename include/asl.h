@@ -449,7 +449,8 @@ asl_status asl_rotate_write(asl_ctx* ctx, const asl_pages* pages, const asl_rota
  *   pruned [n_rows] int32 or NULL: tokens that pruning has taken out of each row, i.e. position minus place of its last tokens.
  *   cu     [n+1] int32 out.  total: room for tokens; the first request that does not fit in it whole, and all behind it, get none (and
  *          raise the fault word).
- *   slot   [total] int64 out: as asl_rotate_write takes them; -1 where the row did not get its pages, and behind the last request.
+ *   slot   [total] int64 out: as asl_rotate_write takes them; -1 where the row did not get its pages (nothing of its tokens is written then,
+ *          attention takes its last tokens for them, asl_pages_accept leaves it alone), and behind the last request.
  *   pos    [total] int32 out: the row's old length + the token's place among the new ones (or its depth) + pruned; -1 where the row is out
  *          of range, and behind the last request. */
 asl_status asl_pages_plan(asl_ctx* ctx, const asl_pages* pages, const int32_t* rows, const int32_t* add, int32_t n, int32_t total,
@@ -457,7 +458,8 @@ asl_status asl_pages_plan(asl_ctx* ctx, const asl_pages* pages, const int32_t* r
                           int64_t* slot, int32_t* pos, void* stream);
 
 /* asl_paged_attention of drafts: the queries are nodes, sequence b's cu_q[b] .. cu_q[b+1]-1 its last tokens, and each sees the tokens
- * before the draft, its ancestors and itself.  Arguments and results as there, with
+ * before the draft, its ancestors and itself.  Arguments and results as there, but that cu_q[n_seqs] may be less than total_q (rows of out and
+ * lse behind the last sequence stay as they were), and with
  *   parent [total_q] int32: of each node its parent's number in the draft, less than its own, or -1.  Other numbers stand for -1, and raise
  *          the fault word.
  * attn->flags is ASL_ATTN_CAUSAL.  At most 512 nodes a sequence (max_q_len, and what cu_q says: a longer draft is left out, its rows of out
@@ -472,11 +474,13 @@ asl_status asl_tree_attention(asl_ctx* ctx, const asl_pages* pages, const asl_at
  *   path   [n, path_stride] int32, path_stride <= 512: a row's nodes from the root on, ascending (as parents stand before their children).
  *          The first number that does not ascend, or is none of the draft's, ends the path, and raises the fault word.
  *   n_path [n] int32, 0: the whole draft goes.
+ *   slot   [total] int64 or NULL: the nodes' slots as asl_pages_plan gave them.  A row that did not get its pages then, whose nodes have -1,
+ *          has no draft and stays as it is.  (NULL: every row's last tokens are its draft.)
  *   k_ptrs, v_ptrs  DEVICE arrays of n_layers device pointers to each layer's k_pages (v_pages).
  * The pages of a draft are its row's alone.  No row twice. */
 asl_status asl_pages_accept(asl_ctx* ctx, const asl_pages* pages, void* const* k_ptrs, void* const* v_ptrs, int32_t n_layers,
                             const int32_t* rows, const int32_t* cu, const int32_t* path, int32_t path_stride, const int32_t* n_path,
-                            int32_t n, const int32_t* table, int32_t* kv_len, int32_t* refs, void* stream);
+                            int32_t n, const int64_t* slot, int32_t total, const int32_t* table, int32_t* kv_len, int32_t* refs, void* stream);
 
 /* Health check (not a step of the paper's method).  Workgroups of a launch that wait for other workgroups of it do so with
  * a bounded number of polls, and raise a fault word in the workspace if their wait runs out (every wave still exits):

@@ -162,7 +162,7 @@ def load() -> C.CDLL:
             "asl_rotate_write": [vp, C.POINTER(AslPages), C.POINTER(AslRotation)] + [vp] * 6 + [i32] + [vp] * 4,
             "asl_pages_plan": [vp, C.POINTER(AslPages), vp, vp, i32, i32] + [vp] * 9,
             "asl_tree_attention": [vp, C.POINTER(AslPages), C.POINTER(AslAttn)] + [vp] * 13,
-            "asl_pages_accept": [vp, C.POINTER(AslPages), vp, vp, i32, vp, vp, vp, i32, vp, i32] + [vp] * 4}.items():
+            "asl_pages_accept": [vp, C.POINTER(AslPages), vp, vp, i32, vp, vp, vp, i32, vp, i32, vp, i32] + [vp] * 4}.items():
         getattr(lib, name).argtypes = args
         getattr(lib, name).restype = C.c_int
     _lib = lib
@@ -448,6 +448,10 @@ class Asl:
         _list_of("slot", slot, total, "int64")
         _list_of("pos", pos, total, "int32")
         _list_of("cu", cu, n + 1, "int32")
+        if parent is not None:
+            _list_of("parent", parent, total, "int32")
+        if pruned is not None:
+            _list_of("pruned", pruned, pages.n_rows, "int32")
         self._check(self.lib.asl_pages_plan(self.h, C.byref(pages), _ptr(rows), _ptr(add), n, total, _ptr(parent), _ptr(pruned),
                                             _ptr(table), _ptr(kv_len), _ptr(refs), _ptr(cu), _ptr(slot), _ptr(pos), _stream()))
 
@@ -461,14 +465,17 @@ class Asl:
                                                 _ptr(prefix_len), _ptr(out), _ptr(lse), _stream()))
 
     def asl_pages_accept(self, pages: AslPages, k_ptrs, v_ptrs, n_layers: int, rows, cu, path, n_path, n: int, table, kv_len,
-                         refs) -> None:
-        """k_ptrs, v_ptrs: int64 device tensors holding one device pointer per layer; path: [n, longest path] without gaps."""
-        if path.dim() != 2 or path.shape[0] < n or not path.is_contiguous():
-            raise AslError(ASL_EINVAL, f"path must be [{n}, longest path] without gaps (its shape is {tuple(path.shape)}, its strides "
+                         refs, slot=None) -> None:
+        """k_ptrs, v_ptrs: int64 device tensors holding one device pointer per layer; path: [n, longest path] int32 without gaps; slot:
+        what asl_pages_plan gave, so that rows without pages stay as they are."""
+        if path.dim() != 2 or path.shape[0] < n or not path.is_contiguous() or path.element_size() != 4:
+            raise AslError(ASL_EINVAL, f"path must be [{n}, longest path] int32 without gaps (its shape is {tuple(path.shape)}, its strides "
                                        f"{tuple(path.stride())})")
+        if slot is not None:
+            _list_of("slot", slot, slot.numel(), "int64")
         self._check(self.lib.asl_pages_accept(self.h, C.byref(pages), _ptr(k_ptrs), _ptr(v_ptrs), n_layers, _ptr(rows), _ptr(cu),
-                                              _ptr(path), path.shape[1], _ptr(n_path), n, _ptr(table), _ptr(kv_len), _ptr(refs),
-                                              _stream()))
+                                              _ptr(path), path.shape[1], _ptr(n_path), n, _ptr(slot),
+                                              0 if slot is None else slot.numel(), _ptr(table), _ptr(kv_len), _ptr(refs), _stream()))
 
     def asl_gather_kv(self, params: AslParams, k, v, idx, idx_rows: int, n_idx: int, k_out, v_out) -> None:
         self._check(self.lib.asl_gather_kv(self.h, C.byref(params), _ptr(k), _ptr(v), _ptr(idx), idx_rows,

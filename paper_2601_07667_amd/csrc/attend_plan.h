@@ -20,13 +20,17 @@ struct AttendCut {
   int64_t cap;             // rows of partial results that there is room for
 };
 
+// (Divisions of 64 bits take a wavefront about 1000 cycles each, and every one works the cut out: of 32 bits where the numbers allow it.)
 // Key tiles of an item: as many as give about `target` items of `work` (row tiles x heads x key tiles).
 ASL_HD int64_t tiles_per_item(const AttendCut& c, unsigned long long work) {
-  const int64_t t = (int64_t)((work + (unsigned long long)c.target - 1) / (unsigned long long)c.target);
+  const unsigned long long up = work + (unsigned long long)c.target - 1;
+  const int64_t t = up >> 32 == 0 ? (int64_t)((uint32_t)up / (uint32_t)c.target) : (int64_t)(up / (unsigned long long)c.target);
   return t > c.min_tiles ? t : c.min_tiles;
 }
 
-ASL_HD int splits_of(int span, int64_t per_item) { return span < 1 ? 1 : (int)((span + per_item - 1) / per_item); }
+ASL_HD int splits_of(int span, int64_t per_item) {
+  return per_item >= span ? 1 : (int)(((uint32_t)span - 1u) / (uint32_t)per_item) + 1;   // (spans are below 2^31, and so then is per_item)
+}
 
 // Tiles [*t0, *t1) of `span` that split s of n takes; equal shares, the first ones a tile longer.
 ASL_HD void split_range(int span, int n, int s, int* t0, int* t1) {

@@ -48,7 +48,7 @@ struct StepWindow {
   }
   __device__ __forceinline__ void take(const Source& s, int number) {
     const bool in = (uint32_t)number < (uint32_t)s.n_pages;
-    const int64_t place = (int64_t)(in ? number : 0) * s.page + (int64_t)((subtile(s, first) & (s.ps - 1)) * (int)s.tok);
+    const int64_t place = (int64_t)(in ? number : 0) * s.page + (int64_t)(subtile(s, first) & (s.ps - 1)) * s.tok;
     lo = (uint32_t)place;
     hi = (uint32_t)((uint64_t)place >> 32);
     before = good;
@@ -82,17 +82,23 @@ struct StepWindow {
 // register to write, and the compiler's own waits count it as nothing, so that they are longer than they need be.)
 __device__ __forceinline__ void send_to_lds(uint32_t to, const char* base, uint32_t offset) {
   const uint32_t m0 = (uint32_t)__builtin_amdgcn_readfirstlane((int)to);
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(m0), "v"(offset), "s"(uniform(base)) : "memory");
+  uint32_t kept;                                           // (the compiler's m0, which no clobber can name)
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3\n\ts_mov_b32 m0, %0"
+               : "=&s"(kept)
+               : "s"(m0), "v"(offset), "s"(uniform(base))
+               : "memory");
 }
 
 // The same if `on` is not 0.  (A branch that the compiler knew of would cut the products beside it into pieces, which it then keeps
 // registers of twice: 300 of them in memory.)
 __device__ __forceinline__ void send_to_lds_if(uint32_t on, uint32_t to, const char* base, uint32_t offset) {
   const uint32_t m0 = (uint32_t)__builtin_amdgcn_readfirstlane((int)to), cond = (uint32_t)__builtin_amdgcn_readfirstlane((int)on);
-  asm volatile(
-      "s_cmp_eq_u32 %3, 0\n\ts_cbranch_scc1 .Lskip%=\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n.Lskip%=:" ::"s"(m0),
-      "v"(offset), "s"(uniform(base)), "s"(cond)
-      : "memory", "scc");
+  uint32_t kept;
+  asm volatile("s_cmp_eq_u32 %4, 0\n\ts_cbranch_scc1 .Lskip%=\n\ts_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\t"
+               "global_load_lds_dwordx4 %2, %3\n\ts_mov_b32 m0, %0\n.Lskip%=:"
+               : "=&s"(kept)
+               : "s"(m0), "v"(offset), "s"(uniform(base)), "s"(cond)
+               : "memory", "scc");
 }
 
 // A lane's offsets in its wavefront's part of a step: half of the pieces of 16 keys, and 8 rows of values.

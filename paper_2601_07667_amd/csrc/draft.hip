@@ -205,8 +205,12 @@ __global__ void __launch_bounds__(kAcceptThreads) pages_accept_kernel(AcceptArgs
   const int b = (int)blockIdx.x, tid = (int)threadIdx.x;
   const int r = a.rows[b], c0 = a.cu[b], c1 = a.cu[b + 1], wanted = a.n_path[b];
   int len;
-  bool bad = !row_length(m, r, &len) || c0 < 0 || c1 < c0 || c1 - c0 > len || wanted < 0 || wanted > a.path_stride || wanted > c1 - c0;
-  const bool sound = !bad;
+  bool bad = !row_length(m, r, &len) || c0 < 0 || c1 < c0 || wanted < 0 || wanted > a.path_stride || wanted > c1 - c0 ||
+             (a.slot != nullptr && c1 > a.total);
+  // a row that did not get its pages has no draft: its last tokens are others
+  const bool drafted = bad || a.slot == nullptr || c1 == c0 || a.slot[c0] >= 0;
+  if (drafted && c1 - c0 > len) bad = true;
+  const bool sound = !bad && drafted;
   const int base = len - (c1 - c0), n = sound ? wanted : 0;
   if (tid == 0) {
     end = n;
@@ -266,7 +270,7 @@ __global__ void __launch_bounds__(kAcceptThreads) pages_accept_kernel(AcceptArgs
       __hip_atomic_store(&a.arrived[b], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       // (a row that another entry has changed meanwhile stays as that left it)
       last = sound && atomicCAS(&a.kv_len[r], len, base + keep) == len ? 1 : 0;
-      if (last == 0) paged_fault(m);
+      if (drafted && last == 0) paged_fault(m);
     }
   }
   __syncthreads();

@@ -107,7 +107,9 @@ struct AcceptArgs {
   const int32_t* n_path;   // [n]
   void* const* k_ptrs;     // device arrays [n_layers]
   void* const* v_ptrs;
+  const int64_t* slot;     // [total] or null
   uint32_t* arrived;       // [n] zeros between calls
+  int32_t total;
   int32_t n, path_stride, n_layers, Hk, cpr, cpr_shift;
 };
 hipError_t launch_pages_accept(const AcceptArgs& a, hipStream_t st);

@@ -327,12 +327,12 @@ asl_status asl_pages_plan(asl_ctx* ctx, const asl_pages* p, const int32_t* rows,
 
 asl_status asl_pages_accept(asl_ctx* ctx, const asl_pages* p, void* const* k_ptrs, void* const* v_ptrs, int32_t n_layers,
                             const int32_t* rows, const int32_t* cu, const int32_t* path, int32_t path_stride, const int32_t* n_path,
-                            int32_t n, const int32_t* table, int32_t* kv_len, int32_t* refs, void* stream) {
+                            int32_t n, const int64_t* slot, int32_t total, const int32_t* table, int32_t* kv_len, int32_t* refs, void* stream) {
   asl::AcceptArgs a = {};
   asl_status st = check_pages(ctx, p, table, kv_len, &a.map);
   if (st == ASL_OK) st = check_count(ctx, n);
   if (st != ASL_OK) return st;
-  if (n_layers < 0 || path_stride < 0) return fail(ctx, ASL_EINVAL, "n_layers and path_stride must be >= 0");
+  if (n_layers < 0 || path_stride < 0 || total < 0) return fail(ctx, ASL_EINVAL, "n_layers, path_stride and total must be >= 0");
   if (n_layers > 16384) return fail(ctx, ASL_EUNSUPPORTED, "more than 16384 layers per call");
   if (path_stride > asl::kTreeNodes) return fail(ctx, ASL_EUNSUPPORTED, "a path of more than %d nodes", asl::kTreeNodes);
   if (n == 0) return ASL_OK;
@@ -346,6 +346,8 @@ asl_status asl_pages_accept(asl_ctx* ctx, const asl_pages* p, void* const* k_ptr
   a.cu = cu;
   a.path = path;
   a.n_path = n_path;
+  a.slot = total > 0 ? slot : nullptr;
+  a.total = total;
   a.k_ptrs = k_ptrs;
   a.v_ptrs = v_ptrs;
   a.arrived = ctx->paged.arrived;

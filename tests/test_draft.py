@@ -98,7 +98,7 @@ def test_calls_without_a_context_are_refused():
     assert lib.asl_rotate_write(None, None, None, *none[:6], 1, *none[:4]) == libasl.ASL_EINVAL
     assert lib.asl_pages_plan(None, None, None, None, 1, 1, *none[:9]) == libasl.ASL_EINVAL
     assert lib.asl_tree_attention(None, None, None, *none[:13]) == libasl.ASL_EINVAL
-    assert lib.asl_pages_accept(None, None, None, None, 0, None, None, None, 1, None, 1, *none[:4]) == libasl.ASL_EINVAL
+    assert lib.asl_pages_accept(None, None, None, None, 0, None, None, None, 1, None, 1, None, 0, *none[:4]) == libasl.ASL_EINVAL
     assert lib.asl_rotation_freqs(None, None) == libasl.ASL_EINVAL
 
 
@@ -180,12 +180,15 @@ def test_tensors_that_do_not_fit_are_refused(recorded):
     for args in ((slot.int(), pos, i), (slot, pos.long(), i), (slot, pos, i[:2]), (slot[:2], pos, i), (slot, None, i)):
         with pytest.raises(libasl.AslError):
             plan(*args)
+    for more in (dict(parent=i[:2]), dict(parent=slot), dict(pruned=i[:0]), dict(pruned=torch.zeros(2))):
+        with pytest.raises(libasl.AslError):
+            recorded.asl_pages_plan(pages, i, i, 2, 3, i, i, i, i, slot, pos, **more)
     attn = libasl.make_attn(1, 3, 3, 10)
     for parent in (None, i[:2], i.long(), torch.zeros(6, dtype=torch.int32)[::2]):
         with pytest.raises(libasl.AslError):
             recorded.asl_tree_attention(pages, attn, q, k, k, i, i, i, parent, q)
     accept = lambda path: recorded.asl_pages_accept(pages, i, i, 1, i, i, path, i, 2, i, i, i)
-    for path in (i, torch.zeros(1, 4, dtype=torch.int32), torch.zeros(2, 8, dtype=torch.int32)[:, :4]):
+    for path in (i, torch.zeros(1, 4, dtype=torch.int32), torch.zeros(2, 8, dtype=torch.int32)[:, :4], torch.zeros(2, 4, dtype=torch.int64)):
         with pytest.raises(libasl.AslError, match="path"):
             accept(path)
     assert not recorded.lib.seen

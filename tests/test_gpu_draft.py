@@ -528,6 +528,28 @@ def test_tree_prefix_longer_than_the_contexts(ctx, gpu_device, dtype):
     assert ctx.asl_device_fault() == 0
 
 
+def test_tree_token_strides_past_32_bits(ctx, gpu_device):
+    """Tokens of one page a megabyte apart, all heads of a token beside each other: places past 2^31 bytes inside the page."""
+    torch = _torch()
+    dev, L, n, ps, Hk, d, tok = gpu_device, 3000, 40, 4096, 8, 64, 1 << 19
+    k, v = (torch.empty(ps * tok, dtype=torch.bfloat16, device=dev) for _ in range(2))      # whole pages: slots behind the end are read too
+    g = torch.Generator().manual_seed(3)
+    kv = [torch.randn((L, Hk, d), generator=g).to(torch.bfloat16) for _ in range(2)]
+    for x, y in zip((k, v), kv):
+        x.as_strided((L, Hk, d), (tok, d, 1)).copy_(y.to(dev))
+    q = _queries(n, 32, d, "bf16", dev, 4)
+    parent = _random_parents(n, 5)
+    out = torch.empty((n, 32, d), dtype=torch.bfloat16, device=dev)
+    lse = torch.empty((32, n), dtype=torch.float32, device=dev)
+    desc = asl.make_pages(32, Hk, d, ps, 1, 1, 1, strides=(0, d, tok))
+    for max_kv in (L, 1 << 20):
+        ctx.asl_tree_attention(desc, asl.make_attn(1, n, n, max_kv), q, k, v, _ints([0], dev), _ints([L], dev), _ints([0, n], dev), _ints(parent, dev),
+                               out, lse=lse)
+        ref = do.attention(q.double().cpu().numpy(), *(x.double().numpy().transpose(1, 0, 2) for x in kv), d ** -0.5, parent)
+        _check(out, lse, ref, d, L, "bf16", "strides")
+    assert ctx.asl_device_fault() == 0
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_tree_strides_rows_and_scale(ctx, gpu_device, dtype):
     torch = _torch()
@@ -709,6 +731,26 @@ def test_accept_numbers_out_of_range(ctx, gpu_device):
     assert np.array_equal(c2.kv_len.cpu().numpy(), want[1]) and ctx.asl_device_fault() == 0
 
 
+def test_accept_leaves_rows_without_pages_alone(ctx, gpu_device):
+    """A row that the pool had no page for has no draft: with the plan's slots its own tokens stay."""
+    torch = _torch()
+    c = Cache(gpu_device, [40, 90, 33], 2, 64, 16, "bf16", 2)
+    slot = torch.arange(30, device=gpu_device)
+    slot[10:20] = -1
+    want = _accepted(c, 1, [0, 2], [10, 10], [[0, 3], [5]])
+    k_ptrs, v_ptrs = (torch.tensor([x.data_ptr()], dtype=torch.int64, device=gpu_device) for x in (c.k, c.v))
+    cu, path, n_path = _ints([0, 10, 20, 30], gpu_device), _ints([[0, 3], [1, 2], [5, 0]], gpu_device), _ints([2, 2, 1], gpu_device)
+    call = lambda slot: ctx.asl_pages_accept(c.desc(), k_ptrs, v_ptrs, 1, _ints([0, 1, 2], gpu_device), cu, path, n_path, 3, c.table, c.kv_len,
+                                             c.refs, slot=slot)
+    call(slot)
+    torch.cuda.synchronize()
+    _same_pages(c, want[0])
+    assert np.array_equal(c.kv_len.cpu().numpy(), want[1]) and np.array_equal(c.refs.cpu().numpy(), want[2])
+    assert ctx.asl_device_fault() == 0
+    call(slot[:25])                                          # cu goes past the list: the last row is left out
+    assert ctx.asl_device_fault() == 2 and c.kv_len.tolist() == [24, 90, 24 + 0]
+
+
 def test_accept_refusals(ctx, gpu_device):
     c = Cache(gpu_device, [50], 2, 64, 16, "bf16", 2)
     for width, n_path, status in ((513, 1, asl.ASL_EUNSUPPORTED),):
@@ -749,7 +791,7 @@ def _steps(ctx, dev, dtype, graph, steps=5, seed=3):
         for l in range(layers):
             ctx.asl_rotate_write(pages, rot, x[l, :, :Hq], x[l, :, Hq:Hq + Hk], x[l, :, Hq + Hk:], pos, slot, f, q[l], kp[l], vp[l])
             ctx.asl_tree_attention(pages, attn, q[l], kp[l], vp[l], b.d_table, b.d_kv, cu, parent, out[l], rows=rows)
-        ctx.asl_pages_accept(pages, k_ptrs, v_ptrs, layers, rows, cu, path, n_path, n, b.d_table, b.d_kv, b.d_refs)
+        ctx.asl_pages_accept(pages, k_ptrs, v_ptrs, layers, rows, cu, path, n_path, n, b.d_table, b.d_kv, b.d_refs, slot=slot)
 
     recorded = None
     results = []
