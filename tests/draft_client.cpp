@@ -3,6 +3,7 @@
 #include <cstring>
 #include <vector>
 
+#include "attend_plan.h"
 #include "paged_check.h"
 
 static long long num() {
@@ -51,6 +52,14 @@ int main() {
       a.flags = (int)num(); a.max_q_len = (int)num();
       const int st = asl::tree_status(a, &why);
       std::printf("%d %s\n", st, why);
+    } else if (!std::strcmp(what, "rule")) {
+      // total_q, G, Hk, sequences, groups, nodes of a draft, keys, bytes of a key: kinds of items, and the most pieces that are asked for
+      long long x[8];
+      for (long long& y : x) y = num();
+      const asl::AttendRule r = asl::rule_for(true, x[0], (int)x[1], (int)x[2], (int)x[3], (int)x[4], (int)x[5], (int)x[6], (int)x[7],
+                                              1 << 20, true);
+      std::printf("%d %d %d %d %d\n", r.own.rows, r.groups ? r.shared.rows : 0, (int)r.joined, r.own.cap + r.shared.cap <= (1 << 20),
+                  r.own.cap >= 0 && r.shared.cap >= 0);
     } else if (!std::strcmp(what, "null")) {
       asl_freqs f = {};
       double x;

@@ -7,7 +7,7 @@ import pytest
 from oracle import draft_oracle as do
 from oracle import paged_oracle as po
 from paper_2601_07667_amd import asl
-from test_gpu_paged import NP, Cache, _attend, _check, _dt, _ints, _queries, _torch
+from test_gpu_paged import NP, Cache, _attend, _bounds, _check, _dt, _ints, _queries, _torch
 
 pytestmark = pytest.mark.gpu
 
@@ -890,3 +890,54 @@ def test_tree_is_reproducible(ctx, gpu_device):
     for _ in range(50):
         o, l = _tree(ctx, c, q, n_q, parent, 32)
         assert torch.equal(o, out) and torch.equal(l, lse)
+
+
+def test_rows_behind_the_last_sequence_stay(ctx, gpu_device):
+    """out and lse have room for more nodes than the lists have, as where the lists are a replayed step's."""
+    torch = _torch()
+    for n_q, d, lens in (([20, 9, 40], 128, [3000, 70, 900]), ([3, 2, 1], 64, [30, 7, 90])):
+        total, used = 96, sum(n_q)
+        c = Cache(gpu_device, lens, 2, d, 64, "bf16", 5)
+        parent = sum([_random_parents(n, n) for n in n_q], []) + [-1] * (total - used)
+        q = _queries(total, 8, d, "bf16", gpu_device, 6)
+        out, lse = torch.full((total, 8, d), 7.0, dtype=torch.bfloat16, device=gpu_device), torch.full((8, total), 7.0, device=gpu_device)
+        ctx.asl_tree_attention(c.desc(8), asl.make_attn(3, total, 64, 4096), q, c.k, c.v, c.table, c.kv_len, _ints(_cu(n_q), gpu_device),
+                               _ints(parent, gpu_device), out, lse=lse)
+        assert torch.all(out[used:] == 7.0) and torch.all(lse[:, used:] == 7.0)
+        ref = _tree_oracle(c, q[:used], n_q, parent[:used])
+        _check(out[:used], lse[:, :used], ref, d, max(lens), "bf16", "room")
+    assert ctx.asl_device_fault() == 0
+
+
+@pytest.mark.parametrize("nodes,page_size", [(5, 16), (40, 64)])
+def test_the_drafting_example(ctx, gpu_device, nodes, page_size):
+    """examples/draft_pruned.py: positions and lengths, and every step's attention over what was kept so far against the oracle."""
+    import importlib.util
+    import os
+    torch = _torch()
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "draft_pruned.py")
+    spec = importlib.util.spec_from_file_location("draft_pruned", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    Hq, Hk, d, N, keep, n = 8, 2, 64, 1000, 200, 3
+    r = example.run(Hq=Hq, Hk=Hk, d=d, N=N, W=16, budget=keep, sequences=n, nodes=nodes, steps=6, page_size=page_size)
+    assert r["fault"] == 0 and r["left"] == 0
+    f = lambda x: x.double().cpu().numpy()
+    idx, k, v = r["idx"].cpu().numpy(), f(r["k"]), f(r["v"])
+    have = [[np.stack([x[h][idx[h]] for h in range(Hk)]) for x in (k, v)] for _ in range(n)]      # each row's K and V [Hk, tokens, d]
+    for s, step in enumerate(r["history"]):
+        at = 0
+        rotated = torch.empty_like(step["x"][:, Hq:Hq + Hk])
+        ctx.asl_rotate(asl.make_rotation(0, Hk, d), None, step["x"][:, Hq:Hq + Hk], step["pos"], r["freqs"], None, rotated)
+        for b, (tree, kept) in enumerate(zip(step["trees"], step["paths"])):
+            m = len(tree)
+            pos = [N - keep + have[b][0].shape[1] + len(do.path_to(tree, i)) - 1 for i in range(m)]
+            np.testing.assert_array_equal(step["pos"][at:at + m].cpu().numpy(), pos)
+            new = [f(x[at:at + m]).transpose(1, 0, 2) for x in (rotated, step["x"][:, Hq + Hk:])]
+            K, V = (np.concatenate([x, y], axis=1) for x, y in zip(have[b], new))
+            ref = do.attention(f(step["q"][at:at + m]), K, V, d ** -0.5, tree)
+            tol, _ = _bounds(d, K.shape[1], "bf16", ref)
+            assert np.all(np.abs(f(step["out"][at:at + m]) - ref[0]) <= tol), (s, b)
+            have[b] = [np.concatenate([x, y[:, kept]], axis=1) for x, y in zip(have[b], new)]
+            at += m
+    assert r["lengths"] == [keep] + [x[0].shape[1] for x in have]
