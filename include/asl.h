@@ -430,7 +430,8 @@ asl_status asl_rotation_freqs(const asl_freqs* freqs, double* out);
 
 /* Rotates q and k of n tokens (Hq or Hk 0: that one may be NULL).
  *   q, q_out [n, Hq, d], k, k_out [n, Hk, d] by the strides in rotation; an output may be its input (same strides), and must not overlap it
- *          otherwise.  Rows, strides and addresses of 16 bytes are moved in 16-byte pieces, others in narrower ones.
+ *          otherwise.  A stride of 0 broadcasts an input; outputs of several tokens or heads have none.  Rows, strides and addresses of
+ *          16 bytes are moved in 16-byte pieces, others in narrower ones.
  *   pos    [n] int32, negative ones too;  freqs [rot_dim / 2] f64, both device memory.
  * fp32 arithmetic, each output rounded once. */
 asl_status asl_rotate(asl_ctx* ctx, const asl_rotation* rotation, const void* q, const void* k, const int32_t* pos, const double* freqs,
@@ -447,8 +448,8 @@ asl_status asl_rotate_write(asl_ctx* ctx, const asl_pages* pages, const asl_rota
  * place.  Request i's tokens are cu[i] .. cu[i+1]-1.
  *   parent [total] int32 or NULL: the tokens are drafts, and a node's position is by its depth.  NULL: one token behind the other.
  *   pruned [n_rows] int32 or NULL: tokens that pruning has taken out of each row, i.e. position minus place of its last tokens.
- *   cu     [n+1] int32 out.  total: room for tokens; the first request that does not fit in it whole, and all behind it, get none (and
- *          raise the fault word).
+ *   cu     [n+1] int32 out, also where n is 0.  total: room for tokens; the first request that does not fit in it whole, and all behind it,
+ *          get none (and raise the fault word).
  *   slot   [total] int64 out: as asl_rotate_write takes them; -1 where the row did not get its pages (nothing of its tokens is written then,
  *          attention takes its last tokens for them, asl_pages_accept leaves it alone), and behind the last request.
  *   pos    [total] int32 out: the row's old length + the token's place among the new ones (or its depth) + pruned; -1 where the row is out

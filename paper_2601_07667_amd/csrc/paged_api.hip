@@ -302,8 +302,8 @@ asl_status asl_pages_plan(asl_ctx* ctx, const asl_pages* p, const int32_t* rows,
   if (st == ASL_OK) st = check_count(ctx, n);
   if (st != ASL_OK) return st;
   if (total < 0) return fail(ctx, ASL_EINVAL, "total must be >= 0");
-  if (n == 0) return ASL_OK;
-  if (!rows || !add || !refs || !cu || (total > 0 && (!slot || !pos))) return fail(ctx, ASL_EINVAL, "null tensor pointer");
+  // (without requests too cu, slot and pos say that there is none: what they held before may be a step's that is over)
+  if ((n > 0 && (!rows || !add || !refs)) || !cu || (total > 0 && (!slot || !pos))) return fail(ctx, ASL_EINVAL, "null tensor pointer");
   a.table = table;
   a.kv_len = kv_len;
   a.refs = refs;
@@ -372,6 +372,10 @@ static asl_status rotate(asl_ctx* ctx, const asl_rotation* r, asl::RotateArgs& a
   if (n == 0 || (r->n_q_heads == 0 && r->n_kv_heads == 0)) return ASL_OK;
   if (!pos || !freqs || (r->n_q_heads > 0 && (!q || !q_out)) || (r->n_kv_heads > 0 && (!k || !a.k_out)))
     return fail(ctx, ASL_EINVAL, "null tensor pointer");
+  auto one_place = [n](int heads, int64_t tok, int64_t head) { return (heads > 0 && n > 1 && tok == 0) || (heads > 1 && head == 0); };
+  if (one_place(r->n_q_heads, r->q_out_stride_tok, r->q_out_stride_head) ||
+      (!write && one_place(r->n_kv_heads, r->k_out_stride_tok, r->k_out_stride_head)))
+    return fail(ctx, ASL_EINVAL, "outputs of several tokens or heads in one place (a stride of 0)");
   const int eb = elem_bytes(r->dtype);
   a.q = static_cast<const char*>(q);
   a.k = static_cast<const char*>(k);

@@ -236,6 +236,25 @@ def test_slots_out_of_range_are_left_out(ctx, gpu_device):
         assert float(x.sum()) == d and bool((x[0, 0, 5] == 1).all())
 
 
+def test_rotations_of_broadcast_heads(ctx, gpu_device):
+    """Inputs may share one place; outputs of several heads or tokens may not."""
+    torch = _torch()
+    r, pos, f = asl.make_rotation(4, 2, 64), _ints([5, 6, 7], gpu_device), asl.rotation_freqs(64).to(gpu_device)
+    one = torch.randn(3, 1, 64, device=gpu_device).to(torch.bfloat16)
+    q, k = one.expand(3, 4, 64), one[:1].expand(3, 2, 64)
+    qo, ko = torch.empty(3, 4, 64, dtype=torch.bfloat16, device=gpu_device), torch.empty(3, 2, 64, dtype=torch.bfloat16, device=gpu_device)
+    ctx.asl_rotate(r, q, k, pos, f, qo, ko)
+    want_q, want_k = torch.empty_like(qo), torch.empty_like(ko)
+    ctx.asl_rotate(r, q.contiguous(), k.contiguous(), pos, f, want_q, want_k)
+    assert torch.equal(qo, want_q) and torch.equal(ko, want_k)
+    for outs in ((qo[:, :1].expand(3, 4, 64), ko), (qo[:1].expand(3, 4, 64), ko), (qo, ko[:, :1].expand(3, 2, 64)), (qo, ko[:1].expand(3, 2, 64))):
+        with pytest.raises(asl.AslError, match="one place") as e:
+            ctx.asl_rotate(r, q, k, pos, f, *outs)
+        assert e.value.status == asl.ASL_EINVAL
+    ctx.asl_rotate(asl.make_rotation(1, 0, 64), one[:1], None, pos[:1], f, qo[:1, :1].as_strided((1, 1, 64), (0, 0, 1)), None)
+    assert torch.equal(qo[0, 0], want_q[0, 0])
+
+
 def test_rotate_refusals(ctx, gpu_device):
     torch = _torch()
     dev = gpu_device
@@ -324,6 +343,19 @@ def test_plan_sizes(ctx, gpu_device, n, add):
         parent = sum((_random_parents(m, m, root=0.01) for m in add), []) if tree else None
         b.check(ctx, rng.permutation(n).tolist(), add, parent=parent, pruned=rng.integers(0, 1000, n + 1) if tree else None)
     assert ctx.asl_device_fault() == 0
+
+
+@pytest.mark.parametrize("total", [0, 5, 8192, 9000])
+@pytest.mark.parametrize("tree", [False, True])
+def test_plan_of_no_requests(ctx, gpu_device, total, tree):
+    """No token has a slot or a position, whatever the lists held before."""
+    torch = _torch()
+    b = _Book(gpu_device, 3, 5, 16, 20, [30, 0, 7])
+    slot, pos, cu = _longs(np.full(total, 3), gpu_device), _ints(np.full(total, 3), gpu_device), _ints([9], gpu_device)
+    none = _ints([], gpu_device)
+    ctx.asl_pages_plan(b.desc(), none, none, 0, total, b.d_table, b.d_kv, b.d_refs, cu, slot, pos, parent=_ints(np.zeros(total), gpu_device) if tree else None)
+    assert cu.tolist() == [0] and torch.all(slot == -1) and torch.all(pos == -1)
+    assert b.d_kv.tolist() == [30, 0, 7] and ctx.asl_device_fault() == 0
 
 
 def test_plan_without_enough_pages(ctx, gpu_device):
