@@ -1563,7 +1563,7 @@ hipError_t launch_d(const PagedWorkspace& ws, const AttendArgs& args, hipStream_
   } else {
     e = launch_kinds<T, D, kSplit, kSplit, false, TREE>(a, own, shared, po, ps, st);
   }
-  if (e != hipSuccess || po.arrived != nullptr) return e;
+  if (e != hipSuccess || po.arrived != nullptr || rule.single) return e;
   const int64_t out_rows = (int64_t)a.total_q * a.Hq;
   // few rows are cut into many pieces each
   if (out_rows <= 256)

@@ -86,13 +86,15 @@ ASL_HD AttendCut cut_for(bool tiles, int64_t rows, int64_t keys, int64_t segment
 
 // The same for drafted trees, which have tiles of 128 rows alone (attend_steps.h).  An item takes 10 us to begin and its pieces 9 to 16 to be
 // joined, so where there are tiles for three quarters of the units a span of up to 128 key tiles is one piece (32 sequences of 2300
-// keys, 16 to 32 nodes, 8 heads: 82 us, in two pieces each 108); where there are not, spans are cut for two items a unit (60 nodes on 131089
-// keys, 4 heads: 186 us, with 384 items 196, with 256 207).  Shared ones into about 192 (8 prompts of 2090 keys for 6 sequences
-// each: 46.6 us, with 128 46.8, with 256 47.5, with 384 54.5, with 96 64).
+// keys, 16 to 32 nodes, 8 heads: 82 us, in two pieces each 108).  Where by the caller's word no sequence is longer than that, every span is
+// one (one item in all is wanted), however many keys it turns out to have, and no launch looks for pieces to join (83 us, 80 so).  Where there
+// are fewer tiles, spans are cut for two items a unit (60 nodes on 131089 keys, 4 heads: 186 us, with 384 items 196, with 256 207).  Shared
+// ones into about 192 (8 prompts of 2090 keys for 6 sequences each: 46.6 us, with 128 46.8, with 256 47.5, with 384 54.5, with 96 64).
 ASL_HD AttendCut cut_for_tree(bool tiles, int64_t rows, int64_t keys, int64_t segments, int Hk, bool shared) {
   AttendCut c = cut_for(tiles, rows, keys, segments, Hk, shared);
   if (c.rows == kSplit) return c;
   const int64_t row_tiles = (rows + kTile2 - 1) / kTile2 * segments * Hk;
+  if (!shared && row_tiles >= 192 && keys <= 128 * kKeyTile) return AttendCut{kTile2, 1, 128, 0};
   return AttendCut{kTile2, shared ? 192 : 512, !shared && row_tiles >= 192 ? 128 : 8, 0};
 }
 
@@ -102,6 +104,7 @@ struct AttendRule {
   int64_t most;            // rows of a KV head that a sequence has at most
   bool groups;             // prefixes are read apart if the device finds that they save enough
   bool joined;             // pieces are joined within the launch
+  bool single;             // there are none to join
 };
 
 // tiles: the type and head size have tile items; room: rows of pieces in the workspace.
@@ -121,6 +124,7 @@ ASL_HD AttendRule rule_for(bool tiles, int64_t total_q, int G, int Hk, int n_seq
   r.own.cap = room - r.shared.cap;
   // few pieces are joined by the workgroup that brings the last one
   r.joined = !r.groups && r.own.rows == kSplit && max_kv_len <= kJoinKeys;
+  r.single = !r.groups && r.own.target == 1;
   return r;
 }
 

@@ -58,7 +58,7 @@ int main() {
       for (long long& y : x) y = num();
       const asl::AttendRule r = asl::rule_for(true, x[0], (int)x[1], (int)x[2], (int)x[3], (int)x[4], (int)x[5], (int)x[6], (int)x[7],
                                               1 << 20, true);
-      std::printf("%d %d %d %d %d\n", r.own.rows, r.groups ? r.shared.rows : 0, (int)r.joined, r.own.cap + r.shared.cap <= (1 << 20),
+      std::printf("%d %d %d %d %d %d\n", r.own.rows, r.groups ? r.shared.rows : 0, (int)r.joined, (int)r.single, r.own.cap + r.shared.cap <= (1 << 20),
                   r.own.cap >= 0 && r.shared.cap >= 0);
     } else if (!std::strcmp(what, "null")) {
       asl_freqs f = {};

@@ -50,14 +50,15 @@ def test_batches_of_trees_are_checked(client):
 
 
 def test_the_items_that_trees_take(client):
-    """Few rows or little work: split items, joined in the launch where there are few keys; else tiles of 128 rows, never of 64; prefixes apart
-    where that saves enough and a sequence's own rows fit a tile; pieces never more than the workspace has room for."""
+    """Few rows or little work: split items, joined in the launch where there are few keys; else tiles of 128 rows, never of 64, with nothing to
+    join where there are many tiles of few keys; prefixes apart where that saves enough and a sequence's own rows fit a tile; pieces never
+    more than the workspace has room for."""
     # total_q, heads of a group, KV heads, sequences, groups, nodes, keys, bytes of a key
-    want = {(5 * 9, 2, 2, 5, 0, 9, 500, 256): (16, 0, 1), (64, 4, 8, 64, 0, 1, 2100, 4096): (16, 0, 0), (5, 4, 8, 1, 0, 5, 2048, 4096): (16, 0, 1),
-            (32 * 32, 4, 8, 32, 0, 32, 2580, 4096): (128, 0, 0), (60, 7, 4, 1, 0, 60, 131149, 2048): (128, 0, 0),
-            (48 * 12, 7, 4, 48, 8, 12, 2302, 2048): (128, 128, 0), (16 * 12, 4, 8, 16, 0, 12, 8192, 4096): (128, 0, 0),
-            (48 * 12, 7, 4, 48, 8, 12, 1000, 2048): (128, 0, 0), (48 * 20, 7, 4, 48, 8, 20, 2302, 2048): (128, 0, 0),
-            (4096 * 512, 8, 8, 4096, 0, 512, 1 << 20, 4096): (128, 0, 0), (1, 1, 1, 1, 0, 1, 1, 256): (16, 0, 1)}
+    want = {(5 * 9, 2, 2, 5, 0, 9, 500, 256): (16, 0, 1, 0), (64, 4, 8, 64, 0, 1, 2100, 4096): (16, 0, 0, 0), (5, 4, 8, 1, 0, 5, 2048, 4096): (16, 0, 1, 0),
+            (32 * 32, 4, 8, 32, 0, 32, 2580, 4096): (128, 0, 0, 1), (32 * 32, 4, 8, 32, 0, 32, 8193, 4096): (128, 0, 0, 0), (60, 7, 4, 1, 0, 60, 131149, 2048): (128, 0, 0, 0),
+            (48 * 12, 7, 4, 48, 8, 12, 2302, 2048): (128, 128, 0, 0), (16 * 12, 4, 8, 16, 0, 12, 8192, 4096): (128, 0, 0, 0),
+            (48 * 12, 7, 4, 48, 8, 12, 1000, 2048): (128, 0, 0, 1), (48 * 20, 7, 4, 48, 8, 20, 2302, 2048): (128, 0, 0, 1),
+            (4096 * 512, 8, 8, 4096, 0, 512, 1 << 20, 4096): (128, 0, 0, 0), (1, 1, 1, 1, 0, 1, 1, 256): (16, 0, 1, 0)}
     for got, (case, rule) in zip(client(["rule " + " ".join(map(str, c)) for c in want]), want.items()):
         assert tuple(map(int, got.split())) == rule + (1, 1), case
 

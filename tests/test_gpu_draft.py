@@ -523,6 +523,20 @@ def test_tree_tiles(ctx, gpu_device, lo, hi, d, Hq, Hk):
     _tree_case(ctx, gpu_device, lens, n_q, Hq, Hk, d, 16, "bf16", seed=lo, what="tiles", max_kv=1 << 20)
 
 
+def test_tree_sequences_longer_than_stated(ctx, gpu_device):
+    """max_kv_len decides how items are cut, not what is computed: without pieces to join too."""
+    n_q, lens = [32] * 24, [9000, 8500] + [40 + 9 * i for i in range(22)]
+    rng = random.Random(5)
+    c = Cache(gpu_device, lens, 8, 64, 64, "bf16", 5)
+    parent = sum([_random_parents(n, rng.randrange(99)) for n in n_q], [])
+    q = _queries(sum(n_q), 32, 64, "bf16", gpu_device, 6)
+    ref = _tree_oracle(c, q, n_q, parent)
+    for stated in (2048, 9000):
+        out, lse = _tree(ctx, c, q, n_q, parent, 32, max_kv=stated)
+        _check(out, lse, ref, 64, max(lens), "bf16", "stated %d" % stated)
+    assert ctx.asl_device_fault() == 0
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("d,G", [(128, 4), (64, 7), (256, 2), (80, 1)])
 @pytest.mark.parametrize("groups,own,n_q", [
