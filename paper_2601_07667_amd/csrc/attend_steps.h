@@ -460,20 +460,27 @@ __device__ __forceinline__ void step_item(const AttendArgs& a, const AttendCut& 
   auto rises = [&](const StepLogits& l) { return __any(step_top(l) * scale > rows.m + kWideSlack); };
   bool begun = false;
   while (s < steps) {
-    if (!begun) begin();
-    begun = false;
-    send();
-    const uint32_t ok = window.in_range(s);
-    bad = bad || ok != 3u;
-    const int key0 = key_first + s * kStep;
-    if (key0 < (int)most) step_general<D, PAD>(rows, ring, s, key0, ok, (int)least, (int)most, a.d, scale);
-    ++s;
-    // steps that every row sees, as long as no reference has to move
-    if (!plain()) continue;
+    // (A first step that every row sees gives them their references by itself: shared prompts 46.9 us with a general one, 46.2 so.)
+    if (s > 0 || !plain()) {
+      if (!begun) begin();
+      begun = false;
+      send();
+      const uint32_t ok = window.in_range(s);
+      bad = bad || ok != 3u;
+      const int key0 = key_first + s * kStep;
+      if (key0 < (int)most) step_general<D, PAD>(rows, ring, s, key0, ok, (int)least, (int)most, a.d, scale);
+      ++s;
+      // steps that every row sees, as long as no reference has to move
+      if (!plain()) continue;
+    }
     StepLogits l[2];
     StepWeights w[2];
     begin();
     step_logits<D, PAD>(rows, ring, s, a.d, l[0]);
+    if (s == 0) {                                          // (nothing stands on another reference yet)
+      const float top = step_top(l[0]) * scale;
+      rows.m = fmaxf(top, __shfl_xor(top, 32));
+    }
     if (rises(l[0])) {
       begun = true;
       continue;
