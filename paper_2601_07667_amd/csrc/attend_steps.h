@@ -4,9 +4,9 @@
 // (measured on loops of nothing else).  For that it does three things at once that do not wait for each other: the logits of step t + 1, the
 // exponentials of step t, the products of step t - 1 with its values.  Keys are sent for three steps ahead, values two, so that two steps'
 // are always on their way.
-// 32 sequences of 2300 keys, 16 to 32 nodes, 8 heads, d = 128: 75 us; the steps run at 5.5 TB/s, but an item takes 10 us to begin (page numbers,
-// queries, parents, first keys: loads that depend on each other) and end.  60 nodes of 28 heads on 131089 keys: 164 us = 690 TFLOP/s, 1600 cycles
-// for a step of both workgroups of a unit, of which the products are 1024.  With 16x16x32 products and tiles of 64 keys: 120 and 171.
+// 32 sequences of 2300 keys, 16 to 32 nodes, 8 heads, d = 128: 73 us; the steps run at 5.5 TB/s, but an item takes 10 us to begin (page numbers,
+// queries, parents, first keys: loads that depend on each other) and end.  60 nodes of 28 heads on 131089 keys: 159 us = 712 TFLOP/s, 1800 cycles
+// for a step of both workgroups of a unit, where products take 1024 and LDS reads 1280.  With 16x16x32 products and tiles of 64 keys: 120 and 171.
 //
 //   x^T = K Q^T: lane (r = lane % 32, h = lane / 32) holds K[r][16 c + 8 h ..]; its accumulator has row r and keys 8 j + 4 h .. + 3, j < 4;
 //   out^T += V^T P^T: contraction slot (h, e) = key 16 u + 8 (e / 4) + 4 h + e % 4, u < 2, so that a lane's probabilities are the
