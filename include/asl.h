@@ -476,7 +476,8 @@ asl_status asl_tree_attention(asl_ctx* ctx, const asl_pages* pages, const asl_at
  *          The first number that does not ascend, or is none of the draft's, ends the path, and raises the fault word.
  *   n_path [n] int32, 0: the whole draft goes.
  *   slot   [total] int64 or NULL: the nodes' slots as asl_pages_plan gave them.  A row that did not get its pages then, whose nodes have -1,
- *          has no draft and stays as it is.  (NULL: every row's last tokens are its draft.)
+ *          has no draft and stays as it is.  cu does not go past total: a row whose draft does is out of range.  (NULL: every row's last
+ *          tokens are its draft.)
  *   k_ptrs, v_ptrs  DEVICE arrays of n_layers device pointers to each layer's k_pages (v_pages).
  * The pages of a draft are its row's alone.  No row twice. */
 asl_status asl_pages_accept(asl_ctx* ctx, const asl_pages* pages, void* const* k_ptrs, void* const* v_ptrs, int32_t n_layers,

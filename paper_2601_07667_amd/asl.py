@@ -471,11 +471,14 @@ class Asl:
         if path.dim() != 2 or path.shape[0] < n or not path.is_contiguous() or path.element_size() != 4:
             raise AslError(ASL_EINVAL, f"path must be [{n}, longest path] int32 without gaps (its shape is {tuple(path.shape)}, its strides "
                                        f"{tuple(path.stride())})")
+        slots, total = None, 0
         if slot is not None:
-            _list_of("slot", slot, slot.numel(), "int64")
+            total = slot.numel()
+            _list_of("slot", slot, total, "int64")
+            slots = slot.data_ptr() or _ptr(cu)              # a tensor without elements has no address, and a list without entries is a list
         self._check(self.lib.asl_pages_accept(self.h, C.byref(pages), _ptr(k_ptrs), _ptr(v_ptrs), n_layers, _ptr(rows), _ptr(cu),
-                                              _ptr(path), path.shape[1], _ptr(n_path), n, _ptr(slot),
-                                              0 if slot is None else slot.numel(), _ptr(table), _ptr(kv_len), _ptr(refs), _stream()))
+                                              _ptr(path), path.shape[1], _ptr(n_path), n, slots, total, _ptr(table), _ptr(kv_len),
+                                              _ptr(refs), _stream()))
 
     def asl_gather_kv(self, params: AslParams, k, v, idx, idx_rows: int, n_idx: int, k_out, v_out) -> None:
         self._check(self.lib.asl_gather_kv(self.h, C.byref(params), _ptr(k), _ptr(v), _ptr(idx), idx_rows,

@@ -346,7 +346,7 @@ asl_status asl_pages_accept(asl_ctx* ctx, const asl_pages* p, void* const* k_ptr
   a.cu = cu;
   a.path = path;
   a.n_path = n_path;
-  a.slot = total > 0 ? slot : nullptr;
+  a.slot = slot;                                           // (total 0: a list without entries, of which none is read)
   a.total = total;
   a.k_ptrs = k_ptrs;
   a.v_ptrs = v_ptrs;

@@ -1,0 +1,50 @@
+"""Drafting over the paged cache on the GPU: lists that say that there is nothing, and calls of the largest sizes."""
+import ctypes
+
+import numpy as np
+import pytest
+
+from paper_2601_07667_amd import asl
+from test_gpu_draft import _accepted, _longs, _same_pages
+from test_gpu_paged import Cache, _ints, _torch
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def ctx(gpu_device):
+    c = asl.Asl(2, 1, 1)
+    c.asl_paged_reserve(4096, 1 << 17, 256)
+    yield c
+    assert c.asl_device_fault() == 0, "a test left the fault word set"
+    c.close()
+
+
+# ---------------------------------------------------------------------------------------------------------------- accept
+@pytest.mark.parametrize("binding", [True, False])
+def test_accept_takes_an_empty_list_of_slots_for_a_list(ctx, gpu_device, binding):
+    """Slots of no node: rows without a draft stay, and rows that the lists give one all the same are out of range and stay too."""
+    torch = _torch()
+    dev = gpu_device
+    c = Cache(dev, [40, 90], 2, 64, 16, "bf16", 2)
+    before = [x.clone() for x in c.pages_t]
+    k_ptrs, v_ptrs = (torch.tensor([x.data_ptr()], dtype=torch.int64, device=dev) for x in (c.k, c.v))
+    rows, path, none = _ints([0, 1], dev), _ints([[0, 3], [1, 2]], dev), torch.empty(0, dtype=torch.int64, device=dev)
+    for counts, n_path, fault in (([0, 0], [0, 0], 0), ([10, 0], [2, 0], 2), ([10, 10], [2, 0], 2)):
+        cu, m = _ints(np.concatenate([[0], np.cumsum(counts)]), dev), _ints(n_path, dev)
+        if binding:
+            ctx.asl_pages_accept(c.desc(), k_ptrs, v_ptrs, 1, rows, cu, path, m, 2, c.table, c.kv_len, c.refs, slot=none)
+        else:
+            some = _longs([-1], dev)                         # an address, and no entry
+            st = ctx.lib.asl_pages_accept(ctx.h, ctypes.byref(c.desc()), k_ptrs.data_ptr(), v_ptrs.data_ptr(), 1, rows.data_ptr(), cu.data_ptr(),
+                                          path.data_ptr(), 2, m.data_ptr(), 2, some.data_ptr(), 0, c.table.data_ptr(), c.kv_len.data_ptr(),
+                                          c.refs.data_ptr(), torch.cuda.current_stream().cuda_stream)
+            assert st == asl.ASL_OK
+        assert ctx.asl_device_fault() == fault, counts
+        assert c.kv_len.tolist() == [40, 90] and np.array_equal(c.refs.cpu().numpy(), c.refs_host), counts
+        for x, y in zip(c.pages_t, before):
+            assert torch.equal(x.view(torch.int16), y.view(torch.int16)), counts
+    want = _accepted(c, 1, [0, 1], [10, 10], [[0, 3], [1, 2]])     # (without a list every row's last tokens are its draft)
+    ctx.asl_pages_accept(c.desc(), k_ptrs, v_ptrs, 1, rows, _ints([0, 10, 20], dev), path, _ints([2, 2], dev), 2, c.table, c.kv_len, c.refs)
+    _same_pages(c, want[0])
+    assert c.kv_len.tolist() == [32, 82] and ctx.asl_device_fault() == 0
