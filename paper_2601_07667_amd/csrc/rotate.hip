@@ -183,6 +183,9 @@ void launch_type(const RotateArgs& a, int width, bool halves, bool write, dim3 g
 
 }  // namespace
 
+// Tokens of one launch: a wavefront each, so 2^31 threads.  A launch of 2^32 or more in x does not fail: it runs with their number modulo 2^32.
+constexpr int kRotateTokens = 1 << 25;
+
 hipError_t launch_rotate(const RotateArgs& args, int dtype, bool halves, bool write, int width, hipStream_t st) {
   RotateArgs a = args;
   if (a.n == 0) return hipSuccess;
@@ -195,12 +198,29 @@ hipError_t launch_rotate(const RotateArgs& args, int dtype, bool halves, bool wr
   a.parts = 1;
   while (a.parts * 2 * least <= H && (int64_t)a.n * a.parts < 2048) a.parts *= 2;
   a.heads = (H + a.parts - 1) / a.parts;
-  const int64_t jobs = (int64_t)a.n * a.parts;
-  const dim3 grid((unsigned)((jobs + kWaves - 1) / kWaves));
   const size_t lds = (size_t)kWaves * (a.rot / 2) * sizeof(float2);
-  if (dtype == ASL_BF16) launch_type<__bf16>(a, width, halves, write, grid, lds, st);
-  else launch_type<float>(a, width, halves, write, grid, lds, st);
-  return hipGetLastError();
+  for (int32_t left = args.n; left > 0; left -= a.n) {
+    a.n = left < kRotateTokens ? left : kRotateTokens;
+    const int64_t jobs = (int64_t)a.n * a.parts;
+    const dim3 grid((unsigned)((jobs + kWaves - 1) / kWaves));
+    if (dtype == ASL_BF16) launch_type<__bf16>(a, width, halves, write, grid, lds, st);
+    else launch_type<float>(a, width, halves, write, grid, lds, st);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    if (left == a.n) break;
+    a.pos += a.n;
+    if (a.Hq > 0) {
+      a.q += a.n * a.qt;
+      a.q_out += a.n * a.qot;
+    }
+    if (a.Hk > 0) a.k += a.n * a.kt;
+    if (a.Hk > 0 && !write) a.k_out += a.n * a.kot;
+    if (write) {
+      a.v += a.n * a.vt;
+      a.slot += a.n;
+    }
+  }
+  return hipSuccess;
 }
 
 }  // namespace asl

@@ -4,6 +4,7 @@ import ctypes
 import numpy as np
 import pytest
 
+from oracle import draft_oracle as do
 from paper_2601_07667_amd import asl
 from test_gpu_draft import _accepted, _longs, _same_pages
 from test_gpu_paged import Cache, _ints, _torch
@@ -48,3 +49,45 @@ def test_accept_takes_an_empty_list_of_slots_for_a_list(ctx, gpu_device, binding
     ctx.asl_pages_accept(c.desc(), k_ptrs, v_ptrs, 1, rows, _ints([0, 10, 20], dev), path, _ints([2, 2], dev), 2, c.table, c.kv_len, c.refs)
     _same_pages(c, want[0])
     assert c.kv_len.tolist() == [32, 82] and ctx.asl_device_fault() == 0
+
+
+# ---------------------------------------------------------------------------------------------------------------- rotate
+@pytest.mark.parametrize("n", [(1 << 25) + 5, (1 << 26) + 3])
+def test_rotations_of_more_tokens_than_a_launch_takes(ctx, gpu_device, n):
+    """Position 0 leaves a head as it is; some tokens of other positions, around every border of 2^25 tokens, are as in a call of theirs alone."""
+    torch = _torch()
+    dev, d = gpu_device, 2
+    some = sorted({t for b in range(0, n + 1, 1 << 25) for t in range(b - 2, b + 3) if 0 <= t < n} | {n - 1})
+    at = _longs(some, dev)
+    pos = torch.zeros(n, dtype=torch.int32, device=dev)
+    pos[at] = _ints(np.arange(len(some)) * 37 + 1, dev)
+    f, r = torch.from_numpy(do.freqs(d)).to(dev), asl.make_rotation(1, 1, d)
+    x = torch.tensor([[[1.25, -3.0]]], dtype=torch.bfloat16, device=dev)
+    q, k = x.expand(n, 1, d), torch.arange(n, device=dev).remainder_(251).to(torch.bfloat16)[:, None, None].repeat(1, 1, d)
+    want_k = k.clone()
+    q_out = torch.full((n, 1, d), float("nan"), dtype=torch.bfloat16, device=dev)
+    one_q, one_k = torch.empty((len(some), 1, d), dtype=torch.bfloat16, device=dev), torch.empty((len(some), 1, d), dtype=torch.bfloat16, device=dev)
+    ctx.asl_rotate(r, q[at], k[at], pos[at], f, one_q, one_k)
+    ctx.asl_rotate(r, q, k, pos, f, q_out, k)                # k in place
+    want_k[at] = one_k
+    assert torch.equal(k, want_k) and torch.equal(q_out[at], one_q)
+    q_out[at] = x
+    assert torch.equal(q_out, q)
+
+
+def test_rotations_into_pages_of_more_tokens_than_a_launch_takes(ctx, gpu_device):
+    """All but some tokens have no slot."""
+    torch = _torch()
+    dev, d, ps, n = gpu_device, 8, 16, (1 << 26) + 3
+    some = [0, (1 << 25) - 1, 1 << 25, (1 << 25) + 1, (1 << 26) - 1, 1 << 26, n - 1]
+    at = _longs(some, dev)
+    pos, slot = torch.zeros(n, dtype=torch.int32, device=dev), torch.full((n,), -1, dtype=torch.int64, device=dev)
+    pos[at], slot[at] = _ints(np.arange(len(some)) * 91 + 1, dev), _longs(np.arange(len(some)) * 3, dev)
+    f, r = torch.from_numpy(do.freqs(d)).to(dev), asl.make_rotation(0, 1, d)
+    k, v = torch.arange(1, d + 1, device=dev).to(torch.bfloat16)[None, None].expand(n, 1, d), torch.full((1, 1, d), 7.0, dtype=torch.bfloat16, device=dev).expand(n, 1, d)
+    pages = [torch.zeros((2, 1, ps, d), dtype=torch.bfloat16, device=dev) for _ in range(4)]
+    desc = asl.make_pages(1, 1, d, ps, 2, 1, 1)
+    ctx.asl_rotate_write(desc, r, None, k[at], v[at], pos[at], slot[at], f, None, *pages[2:])
+    ctx.asl_rotate_write(desc, r, None, k, v, pos, slot, f, None, *pages[:2])
+    assert torch.equal(pages[0], pages[2]) and torch.equal(pages[1], pages[3]) and int((pages[1] == 7).sum()) == d * len(some)
+    assert ctx.asl_device_fault() == 0
