@@ -361,7 +361,7 @@ asl_status asl_pages_compact(asl_ctx* ctx, const asl_pages* pages, const int32_t
  * int32 ascending from 0 to n_seqs.  The result is that of n_groups = 0 up to rounding.
  * Products take bf16 (fp32) operands and are summed in fp32, ahead of the division and with probabilities of up to 2^24: over n keys,
  * values of 2^103 / n and more may overflow there.  Softmax and sums are fp32 and of a fixed order; in bf16 a probability is rounded to 8 bits before its product with v.  Masked keys and slots behind
- * a sequence's end may hold anything.  d: multiples of 16 bytes up to 256 elements. */
+ * a sequence's end may hold anything.  d: multiples of 16 bytes up to 256 elements.  Hk n_seqs + Hq total_q / 16 from about 2^24 on are refused. */
 asl_status asl_paged_attention(asl_ctx* ctx, const asl_pages* pages, const asl_attn* attn, const void* q, const void* k_pages,
                                const void* v_pages, const int32_t* rows, const int32_t* table, const int32_t* kv_len,
                                const int32_t* cu_q, const int32_t* group_start, const int32_t* prefix_len, void* out,

@@ -35,6 +35,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t Piece __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256;
+static_assert(kMostItems * kThreads == int64_t(1) << 32, "threads of a launch");
 constexpr int kWaves = kThreads / 64;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
@@ -1508,7 +1509,7 @@ hipError_t launch_kinds(const AttendArgs& a, const AttendCut& own, const AttendC
   const int64_t rows = (int64_t)a.total_q * a.G;
   const int64_t n_own = (max_items(own, rows, a.n_seqs, a.Hk) + 7) & ~int64_t(7);
   const int64_t n_shared = SHARED == kNone ? 0 : (max_items(shared, rows, a.n_groups, a.Hk) + 7) & ~int64_t(7);
-  if (n_own + n_shared >= (int64_t(1) << 31)) return hipErrorInvalidValue;
+  if (n_own + n_shared >= kMostItems) return hipErrorInvalidConfiguration;
   const dim3 grid((unsigned)(n_own + n_shared)), block(kThreads);
   if (a.d == D)
     hipLaunchKernelGGL((attend_kernel<T, D, OWN, SHARED, false, STREAM, TREE>), grid, block, 0, st, a, own, shared, po, ps, (int)n_shared);

@@ -45,6 +45,9 @@ ASL_HD int64_t max_items(const AttendCut& c, int64_t rows, int64_t segments, int
   return c.target + Hk * (rows / c.rows + segments);
 }
 
+// Items of a launch: 256 threads each.  One of 2^32 threads or more in x does not fail: it runs with their number modulo 2^32.
+constexpr int64_t kMostItems = (int64_t(1) << 32) / 256;
+
 // Rows of partial results that such a launch can leave at most.
 ASL_HD int64_t max_partials(const AttendCut& c, int64_t rows, int Hk) { return rows * Hk + (int64_t)c.target * c.rows; }
 

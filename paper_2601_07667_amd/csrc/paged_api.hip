@@ -276,6 +276,9 @@ static asl_status attend(asl_ctx* ctx, const asl_pages* p, const asl_attn* at, c
   if (guard.err != hipSuccess) return hip_fail(ctx, guard.err, "set device");
   const hipStream_t s = static_cast<hipStream_t>(stream);
   hipError_t e = tree ? asl::launch_attend_tree(ctx->paged, a, p->dtype, s) : asl::launch_attend(ctx->paged, a, p->dtype, s);
+  if (e == hipErrorInvalidConfiguration)
+    return fail(ctx, ASL_EUNSUPPORTED, "Hk=%d heads of %d sequences and %d query tokens are more than 2^24 work items", p->n_kv_heads, at->n_seqs,
+                at->total_q);
   if (e != hipSuccess) return hip_fail(ctx, e, "attention launch");
   return ASL_OK;
 }

@@ -7,7 +7,7 @@ import pytest
 from oracle import draft_oracle as do
 from paper_2601_07667_amd import asl
 from test_gpu_draft import _accepted, _longs, _same_pages
-from test_gpu_paged import Cache, _ints, _torch
+from test_gpu_paged import Cache, _dt, _ints, _torch
 
 pytestmark = pytest.mark.gpu
 
@@ -91,3 +91,29 @@ def test_rotations_into_pages_of_more_tokens_than_a_launch_takes(ctx, gpu_device
     ctx.asl_rotate_write(desc, r, None, k, v, pos, slot, f, None, *pages[:2])
     assert torch.equal(pages[0], pages[2]) and torch.equal(pages[1], pages[3]) and int((pages[1] == 7).sum()) == d * len(some)
     assert ctx.asl_device_fault() == 0
+
+
+# ------------------------------------------------------------------------------------------------------------- attention
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("tree", [True, False])
+def test_attention_of_more_items_than_a_launch_takes(ctx, gpu_device, tree, dtype):
+    """Refused, and nothing is written: 4096 heads of 4096 sequences, of which one has a token.  Eight sequences are not."""
+    torch = _torch()
+    dev, H, d = gpu_device, 4096, 8
+    pages = [torch.randn((1, H, 16, d), device=dev).to(_dt(dtype)) for _ in range(2)]
+    q = torch.randn((1, H, d), device=dev).to(_dt(dtype))
+    desc = asl.make_pages(H, H, d, 16, 1, 1, 1, dtype=asl.ASL_BF16 if dtype == "bf16" else asl.ASL_F32)
+    for n, refused in ((4096, True), (8, False)):
+        out, lse = torch.full_like(q, 9.0), torch.full((H, 1), 9.0, device=dev)
+        args = (desc, asl.make_attn(n, 1, 1, 1), q, *pages, _ints([[0]], dev), _ints([1], dev), _ints([0] * n + [1], dev))
+        more = dict(lse=lse, rows=_ints([0] * n, dev))
+        call = lambda: ctx.asl_tree_attention(*args, _ints([-1], dev), out, **more) if tree else ctx.asl_paged_attention(*args, out, **more)
+        if refused:
+            with pytest.raises(asl.AslError, match="2\\^24") as e:
+                call()
+            assert e.value.status == asl.ASL_EUNSUPPORTED
+            assert bool((out == 9.0).all()) and bool((lse == 9.0).all())
+        else:
+            call()
+            assert torch.equal(out[0], pages[1][0, :, 0])    # one key: its value
+        assert ctx.asl_device_fault() == 0
