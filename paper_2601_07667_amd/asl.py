@@ -192,29 +192,44 @@ def _batch_of(attn, q, out, lse):
     return a
 
 
-def _heads_of(name, t, n: int, heads: int, d: int):
+_TYPES = {}
+
+
+def _type_of(dtype):
+    """torch's type for the name of one or an ASL_* code; None if there is none (such a code the call refuses itself)."""
+    if not _TYPES:
+        import torch
+        _TYPES.update({"int32": torch.int32, "int64": torch.int64, "float64": torch.float64, ASL_BF16: torch.bfloat16, ASL_F32: torch.float32})
+    return _TYPES.get(dtype)
+
+
+def _refuse_type(name, t, want) -> None:
+    """For elements that are not of the described type.  Tensors of the host are asked for room alone: larger elements are not read past
+    their end."""
+    if want is not None and (t.is_cuda or t.element_size() < want.itemsize):
+        raise AslError(ASL_EINVAL, f"{name} must be of {want}, as described (it is of {t.dtype})")
+
+
+def _heads_of(name, t, n: int, heads: int, d: int, dtype: int):
     """The strides of t [n, heads, d] from token to token and from head to head."""
     if heads == 0:
         return 0, 0
     if t is None or t.shape != (n, heads, d):
         raise AslError(ASL_EINVAL, f"{name} must be [{n}, {heads}, {d}] (it is {None if t is None else tuple(t.shape)})")
+    want = _type_of(dtype)
+    if t.dtype is not want:
+        _refuse_type(name, t, want)
     tok, head, one = t.stride()
     if one != 1:
         _refuse_gaps(**{name: t})
     return tok, head
 
 
-_TYPES = {}
-
-
 def _list_of(name, t, n: int, dtype: str) -> None:
     """A list that a call reads or writes n entries of, one behind the other."""
     if t is None and n == 0:
         return
-    if not _TYPES:
-        import torch
-        _TYPES.update(int32=torch.int32, int64=torch.int64, float64=torch.float64)
-    if t is None or t.numel() < n or t.dtype is not _TYPES[dtype] or not t.is_contiguous():
+    if t is None or t.numel() < n or t.dtype is not _type_of(dtype) or not t.is_contiguous():
         raise AslError(ASL_EINVAL, f"{name} must be {n} x {dtype} without gaps (it is "
                                    f"{None if t is None else (tuple(t.shape), tuple(t.stride()), str(t.dtype))})")
 
@@ -418,11 +433,11 @@ class Asl:
     def asl_rotate(self, rotation: AslRotation, q, k, pos, freqs, q_out, k_out) -> None:
         """q, q_out: [n, Hq, d], k, k_out: [n, Hk, d] of any strides (d contiguous); None where the rotation has no such heads."""
         r = AslRotation.from_buffer_copy(rotation)           # (the description may be another thread's too)
-        n, Hq, Hk, d = pos.shape[0], r.n_q_heads, r.n_kv_heads, r.head_dim
-        r.q_stride_tok, r.q_stride_head = _heads_of("q", q, n, Hq, d)
-        r.k_stride_tok, r.k_stride_head = _heads_of("k", k, n, Hk, d)
-        r.q_out_stride_tok, r.q_out_stride_head = _heads_of("q_out", q_out, n, Hq, d)
-        r.k_out_stride_tok, r.k_out_stride_head = _heads_of("k_out", k_out, n, Hk, d)
+        n, Hq, Hk, d, e = pos.shape[0], r.n_q_heads, r.n_kv_heads, r.head_dim, r.dtype
+        r.q_stride_tok, r.q_stride_head = _heads_of("q", q, n, Hq, d, e)
+        r.k_stride_tok, r.k_stride_head = _heads_of("k", k, n, Hk, d, e)
+        r.q_out_stride_tok, r.q_out_stride_head = _heads_of("q_out", q_out, n, Hq, d, e)
+        r.k_out_stride_tok, r.k_out_stride_head = _heads_of("k_out", k_out, n, Hk, d, e)
         _list_of("pos", pos, n, "int32")
         _list_of("freqs", freqs, r.rot_dim // 2, "float64")
         self._check(self.lib.asl_rotate(self.h, C.byref(r), _ptr(q), _ptr(k), _ptr(pos), _ptr(freqs), n, _ptr(q_out), _ptr(k_out),
@@ -431,11 +446,11 @@ class Asl:
     def asl_rotate_write(self, pages: AslPages, rotation: AslRotation, q, k, v, pos, slot, freqs, q_out, k_pages, v_pages) -> None:
         """q, q_out: [n, Hq, d], k, v: [n, Hk, d] of any strides (d contiguous); slot: [n] int64."""
         r = AslRotation.from_buffer_copy(rotation)
-        n, Hq, Hk, d = pos.shape[0], r.n_q_heads, r.n_kv_heads, r.head_dim
-        r.q_stride_tok, r.q_stride_head = _heads_of("q", q, n, Hq, d)
-        r.k_stride_tok, r.k_stride_head = _heads_of("k", k, n, Hk, d)
-        r.v_stride_tok, r.v_stride_head = _heads_of("v", v, n, Hk, d)
-        r.q_out_stride_tok, r.q_out_stride_head = _heads_of("q_out", q_out, n, Hq, d)
+        n, Hq, Hk, d, e = pos.shape[0], r.n_q_heads, r.n_kv_heads, r.head_dim, r.dtype
+        r.q_stride_tok, r.q_stride_head = _heads_of("q", q, n, Hq, d, e)
+        r.k_stride_tok, r.k_stride_head = _heads_of("k", k, n, Hk, d, e)
+        r.v_stride_tok, r.v_stride_head = _heads_of("v", v, n, Hk, d, e)
+        r.q_out_stride_tok, r.q_out_stride_head = _heads_of("q_out", q_out, n, Hq, d, e)
         _list_of("pos", pos, n, "int32")
         _list_of("freqs", freqs, r.rot_dim // 2, "float64")
         _list_of("slot", slot, n, "int64")

@@ -1,4 +1,6 @@
 """The binding of the drafting calls without a GPU: lists and tensors that the calls would read past their end, or as other numbers."""
+import pytest
+
 from paper_2601_07667_amd import asl as libasl
 from test_draft import recorded  # noqa: F401  (a fixture)
 
@@ -15,3 +17,23 @@ def test_an_empty_list_of_slots_is_a_list(recorded):
     none, empty, full = [seen[11:13] for seen in recorded.lib.seen]
     assert none == (None, 0) and full == (some.data_ptr(), 5)
     assert empty[0] and empty[1] == 0
+
+
+def test_tensors_of_smaller_elements_are_refused(recorded):
+    """A bf16 tensor under a description of fp32 would be read past its end."""
+    import torch
+    r, pages = libasl.make_rotation(4, 2, 8, 6, dtype=libasl.ASL_F32), libasl.make_pages(4, 2, 8, 16, 1, 1, 1, dtype=libasl.ASL_F32)
+    q, k = torch.zeros(3, 4, 8), torch.zeros(3, 2, 8)
+    pos, f, slot = torch.zeros(3, dtype=torch.int32), torch.zeros(3, dtype=torch.float64), torch.zeros(3, dtype=torch.int64)
+    good = dict(q=q, k=k, pos=pos, freqs=f, q_out=q, k_out=k)
+    into = dict(q=q, k=k, v=k, pos=pos, slot=slot, freqs=f, q_out=q, k_pages=k, v_pages=k)
+    for call, args in ((lambda **a: recorded.asl_rotate(r, **a), good), (lambda **a: recorded.asl_rotate_write(pages, r, **a), into)):
+        for name in args:
+            if args[name] is q or (args[name] is k and not name.endswith("pages")):
+                for t in (args[name].bfloat16(), args[name].half(), args[name].byte()):
+                    with pytest.raises(libasl.AslError, match=name) as e:
+                        call(**{**args, name: t})
+                    assert e.value.status == libasl.ASL_EINVAL
+        assert not recorded.lib.seen
+        call(**args)
+        recorded.lib.seen.clear()

@@ -93,6 +93,28 @@ def test_rotations_into_pages_of_more_tokens_than_a_launch_takes(ctx, gpu_device
     assert ctx.asl_device_fault() == 0
 
 
+def test_rotations_of_other_types_are_refused(ctx, gpu_device):
+    """Of any type but the described one, whatever its size; nothing is written."""
+    torch = _torch()
+    pos, f = _ints([1, 2, 3], gpu_device), torch.from_numpy(do.freqs(64)).to(gpu_device)
+    for code, right in ((asl.ASL_BF16, torch.bfloat16), (asl.ASL_F32, torch.float32)):
+        r, desc = asl.make_rotation(4, 2, 64, dtype=code), asl.make_pages(4, 2, 64, 16, 1, 1, 1, dtype=code)
+        t = {d: [torch.ones((3, h, 64), dtype=d, device=gpu_device) for h in (4, 2, 2, 4, 2)] for d in (torch.bfloat16, torch.float32, torch.float16, torch.float64)}
+        pages = [torch.zeros((1, 2, 16, 64), dtype=right, device=gpu_device) for _ in range(2)]
+        for other in t:
+            for i in range(5):
+                q, k, v, q_out, k_out = (t[other if j == i else right][j] for j in range(5))
+                if other is right:
+                    continue
+                if i != 2:
+                    with pytest.raises(asl.AslError, match="as described"):
+                        ctx.asl_rotate(r, q, k, pos, f, q_out, k_out)
+                if i != 4:
+                    with pytest.raises(asl.AslError, match="as described"):
+                        ctx.asl_rotate_write(desc, r, q, k, v, pos, _longs([0, 1, 2], gpu_device), f, q_out, *pages)
+        assert all(bool((x == 1).all()) for x in t[right]) and all(bool((x == 0).all()) for x in pages)
+
+
 # ------------------------------------------------------------------------------------------------------------- attention
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("tree", [True, False])
