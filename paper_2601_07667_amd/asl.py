@@ -21,6 +21,7 @@ ASL_ATTN_CAUSAL = 1
 ASL_PAIRS_HALVES, ASL_PAIRS_NEIGHBOURS = 0, 1
 ASL_ROTATE_BACK = 1
 ASL_FREQS_PLAIN, ASL_FREQS_LINEAR, ASL_FREQS_BASE, ASL_FREQS_PARTS = 0, 1, 2, 3
+PAGED_MAX_SEQS = 4096                                      # a call of more sequences is refused before it reads any list
 _STATUS = {0: "ASL_OK", -1: "ASL_EINVAL", -2: "ASL_ENOMEM", -3: "ASL_EHIP", -4: "ASL_EUNSUPPORTED"}
 
 EXPORTS = ["asl_create", "asl_destroy", "asl_last_error", "asl_workspace_bytes", "asl_score_layer",
@@ -483,9 +484,13 @@ class Asl:
                          refs, slot=None) -> None:
         """k_ptrs, v_ptrs: int64 device tensors holding one device pointer per layer; path: [n, longest path] int32 without gaps; slot:
         what asl_pages_plan gave, so that rows without pages stay as they are."""
-        if path.dim() != 2 or path.shape[0] < n or not path.is_contiguous() or path.element_size() != 4:
+        if path.dim() != 2 or path.shape[0] < n or not path.is_contiguous() or path.dtype is not _type_of("int32"):
             raise AslError(ASL_EINVAL, f"path must be [{n}, longest path] int32 without gaps (its shape is {tuple(path.shape)}, its strides "
-                                       f"{tuple(path.stride())})")
+                                       f"{tuple(path.stride())}, its type {path.dtype})")
+        if n <= PAGED_MAX_SEQS:
+            _list_of("rows", rows, n, "int32")
+            _list_of("cu", cu, n + 1, "int32")
+            _list_of("n_path", n_path, n, "int32")
         slots, total = None, 0
         if slot is not None:
             total = slot.numel()

@@ -37,3 +37,27 @@ def test_tensors_of_smaller_elements_are_refused(recorded):
         assert not recorded.lib.seen
         call(**args)
         recorded.lib.seen.clear()
+
+
+def _wrong(n):
+    """What is no list of n int32 one behind the other."""
+    import torch
+    return [torch.zeros(n, dtype=t) for t in (torch.int64, torch.float32, torch.int16)] + [torch.zeros(2 * n, dtype=torch.int32)[::2][:n], None] \
+        + ([torch.zeros(n - 1, dtype=torch.int32)] if n > 1 else [])
+
+
+def test_lists_of_accepting_are_checked(recorded):
+    import torch
+    pages, i = libasl.make_pages(4, 2, 8, 16, 1, 1, 1), torch.zeros(4, dtype=torch.int32)
+    good = dict(rows=i[:3], cu=i, path=torch.zeros(3, 4, dtype=torch.int32), n_path=i[:3])
+    accept = lambda a, n=3: recorded.asl_pages_accept(pages, i, i, 1, a["rows"], a["cu"], a["path"], a["n_path"], n, i, i, i)
+    bad = [(name, t) for name, n in (("rows", 3), ("cu", 4), ("n_path", 3)) for t in _wrong(n)] + [("path", torch.zeros(3, 4)), ("path", torch.zeros(3, 4).int().T)]
+    for name, t in bad:
+        with pytest.raises(libasl.AslError, match=name) as e:
+            accept({**good, name: t})
+        assert e.value.status == libasl.ASL_EINVAL
+    assert not recorded.lib.seen
+    accept(good), accept({**good, "path": torch.zeros(3, 0, dtype=torch.int32)})
+    accept({**good, "path": torch.zeros(4097, 1, dtype=torch.int32)}, 4097)      # (refused by the call, for its size)
+    accept({**good, "rows": i[:0], "cu": i[:1], "n_path": i[:0]}, 0)
+    assert len(recorded.lib.seen) == 4
