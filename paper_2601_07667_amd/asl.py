@@ -464,6 +464,9 @@ class Asl:
         _list_of("slot", slot, total, "int64")
         _list_of("pos", pos, total, "int32")
         _list_of("cu", cu, n + 1, "int32")
+        if n <= PAGED_MAX_SEQS:
+            _list_of("rows", rows, n, "int32")
+            _list_of("add", add, n, "int32")
         if parent is not None:
             _list_of("parent", parent, total, "int32")
         if pruned is not None:

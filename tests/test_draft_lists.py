@@ -61,3 +61,19 @@ def test_lists_of_accepting_are_checked(recorded):
     accept({**good, "path": torch.zeros(4097, 1, dtype=torch.int32)}, 4097)      # (refused by the call, for its size)
     accept({**good, "rows": i[:0], "cu": i[:1], "n_path": i[:0]}, 0)
     assert len(recorded.lib.seen) == 4
+
+
+def test_lists_of_plans_are_checked(recorded):
+    import torch
+    pages, i = libasl.make_pages(4, 2, 8, 16, 1, 1, 1), torch.zeros(4, dtype=torch.int32)
+    slot, pos = torch.zeros(5, dtype=torch.int64), torch.zeros(5, dtype=torch.int32)
+    plan = lambda rows, add, n=3, cu=i: recorded.asl_pages_plan(pages, rows, add, n, 5, i, i, i, cu, slot, pos)
+    for t in _wrong(3):
+        for name, args in (("rows", (t, i[:3])), ("add", (i[:3], t))):
+            with pytest.raises(libasl.AslError, match=name) as e:
+                plan(*args)
+            assert e.value.status == libasl.ASL_EINVAL
+    assert not recorded.lib.seen
+    plan(i[:3], i), plan(None, None, 0)
+    plan(i, i, 4097, torch.zeros(4098, dtype=torch.int32))   # (refused by the call, for its size)
+    assert len(recorded.lib.seen) == 3
