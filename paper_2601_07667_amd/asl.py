@@ -196,12 +196,12 @@ def _batch_of(attn, q, out, lse):
 _TYPES = {}
 
 
-def _type_of(dtype):
-    """torch's type for the name of one or an ASL_* code; None if there is none (such a code the call refuses itself)."""
-    if not _TYPES:
-        import torch
-        _TYPES.update({"int32": torch.int32, "int64": torch.int64, "float64": torch.float64, ASL_BF16: torch.bfloat16, ASL_F32: torch.float32})
-    return _TYPES.get(dtype)
+def _types():
+    """torch's types by name and, of elements, by ASL_* code.  (A call's checks are a part of its time: `_TYPES or _types()`.)"""
+    import torch
+    _TYPES.update({"int32": torch.int32, "int64": torch.int64, "float32": torch.float32, "float64": torch.float64,
+                   ASL_BF16: torch.bfloat16, ASL_F32: torch.float32})
+    return _TYPES
 
 
 def _refuse_type(name, t, want) -> None:
@@ -217,7 +217,7 @@ def _heads_of(name, t, n: int, heads: int, d: int, dtype: int):
         return 0, 0
     if t is None or t.shape != (n, heads, d):
         raise AslError(ASL_EINVAL, f"{name} must be [{n}, {heads}, {d}] (it is {None if t is None else tuple(t.shape)})")
-    want = _type_of(dtype)
+    want = (_TYPES or _types()).get(dtype)                   # (None: no such code, which the call refuses itself)
     if t.dtype is not want:
         _refuse_type(name, t, want)
     tok, head, one = t.stride()
@@ -230,9 +230,18 @@ def _list_of(name, t, n: int, dtype: str) -> None:
     """A list that a call reads or writes n entries of, one behind the other."""
     if t is None and n == 0:
         return
-    if t is None or t.numel() < n or t.dtype is not _type_of(dtype) or not t.is_contiguous():
+    if t is None or t.numel() < n or t.dtype is not (_TYPES or _types())[dtype] or not t.is_contiguous():
         raise AslError(ASL_EINVAL, f"{name} must be {n} x {dtype} without gaps (it is "
                                    f"{None if t is None else (tuple(t.shape), tuple(t.stride()), str(t.dtype))})")
+
+
+def _room_of(name, t, n: int, heads: int, d: int, dtype: int) -> None:
+    """Room for [n, heads, d] elements of the described type in t, which may have more."""
+    if t.shape != (n, heads, d) and any(have < need for have, need in zip(t.shape, (n, heads, d))):
+        raise AslError(ASL_EINVAL, f"{name} must be [{n}, {heads}, {d}] (it is {tuple(t.shape)})")
+    want = (_TYPES or _types()).get(dtype)                   # (None: no such code, which the call refuses itself)
+    if t.dtype is not want:
+        _refuse_type(name, t, want)
 
 
 def _index_rows(idx, total: int) -> int:
@@ -478,7 +487,19 @@ class Asl:
                            rows=None, group_start=None, prefix_len=None) -> None:
         """q, out: [total_q, Hq, d] of any strides (d contiguous); parent: [total_q] int32; lse: [Hq, total_q]."""
         a = _batch_of(attn, q, out, lse)
-        _list_of("parent", parent, a.total_q, "int32")
+        n, total, groups, Hq = a.n_seqs, a.total_q, a.n_groups, pages.n_q_heads
+        _room_of("q", q, total, Hq, pages.head_dim, pages.dtype)
+        _room_of("out", out, total, Hq, pages.head_dim, pages.dtype)
+        _list_of("parent", parent, total, "int32")
+        if lse is not None:
+            _list_of("lse", lse, Hq * total, "float32")
+        if n <= PAGED_MAX_SEQS:
+            _list_of("cu_q", cu_q, n + 1, "int32")
+            if rows is not None:
+                _list_of("rows", rows, n, "int32")
+            if groups > 0:
+                _list_of("group_start", group_start, groups + 1, "int32")
+                _list_of("prefix_len", prefix_len, groups, "int32")
         self._check(self.lib.asl_tree_attention(self.h, C.byref(pages), C.byref(a), _ptr(q), _ptr(k_pages), _ptr(v_pages),
                                                 _ptr(rows), _ptr(table), _ptr(kv_len), _ptr(cu_q), _ptr(parent), _ptr(group_start),
                                                 _ptr(prefix_len), _ptr(out), _ptr(lse), _stream()))
@@ -487,7 +508,7 @@ class Asl:
                          refs, slot=None) -> None:
         """k_ptrs, v_ptrs: int64 device tensors holding one device pointer per layer; path: [n, longest path] int32 without gaps; slot:
         what asl_pages_plan gave, so that rows without pages stay as they are."""
-        if path.dim() != 2 or path.shape[0] < n or not path.is_contiguous() or path.dtype is not _type_of("int32"):
+        if path.dim() != 2 or path.shape[0] < n or not path.is_contiguous() or path.dtype is not (_TYPES or _types())["int32"]:
             raise AslError(ASL_EINVAL, f"path must be [{n}, longest path] int32 without gaps (its shape is {tuple(path.shape)}, its strides "
                                        f"{tuple(path.stride())}, its type {path.dtype})")
         if n <= PAGED_MAX_SEQS:

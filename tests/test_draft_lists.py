@@ -77,3 +77,30 @@ def test_lists_of_plans_are_checked(recorded):
     plan(i[:3], i), plan(None, None, 0)
     plan(i, i, 4097, torch.zeros(4098, dtype=torch.int32))   # (refused by the call, for its size)
     assert len(recorded.lib.seen) == 3
+
+
+def test_tensors_of_tree_attention_are_checked(recorded):
+    import torch
+    pages, attn, i = libasl.make_pages(4, 2, 8, 16, 1, 1, 1, dtype=libasl.ASL_F32), libasl.make_attn(3, 5, 5, 10, n_groups=3), torch.zeros(5, dtype=torch.int32)
+    q = torch.zeros(5, 4, 8)
+    good = dict(q=q, k_pages=q, v_pages=q, table=i, kv_len=i, cu_q=i[:4], parent=i, out=q, lse=torch.zeros(4, 5), rows=i[:3], group_start=i[:4], prefix_len=i[:3])
+    call = lambda attn=attn, **change: recorded.asl_tree_attention(pages, attn, **{**good, **change})
+    for name, n in (("cu_q", 4), ("rows", 3), ("group_start", 4), ("prefix_len", 3), ("parent", 5)):
+        for t in _wrong(n):
+            if name == "rows" and t is None:
+                continue
+            with pytest.raises(libasl.AslError, match=name) as e:
+                call(**{name: t})
+            assert e.value.status == libasl.ASL_EINVAL
+    for name in ("q", "out"):
+        for t in (q[:4], q[:, :3], q[..., :4], q.bfloat16(), q.half()):
+            with pytest.raises(libasl.AslError, match=name):
+                call(**{name: t})
+    for t in (torch.zeros(4, 4), torch.zeros(4, 5).bfloat16(), torch.zeros(4, 5).double(), torch.zeros(5, 4).T):
+        with pytest.raises(libasl.AslError, match="lse"):
+            call(lse=t)
+    assert not recorded.lib.seen
+    call(), call(lse=None, rows=None), call(q=torch.zeros(7, 4, 8), out=torch.zeros(6, 5, 16)[:, :4, :8])
+    call(libasl.make_attn(3, 5, 5, 10), group_start=None, prefix_len=None)
+    call(libasl.make_attn(4097, 5, 5, 10))                   # (refused by the call, for its size)
+    assert len(recorded.lib.seen) == 5
