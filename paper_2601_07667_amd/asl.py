@@ -235,6 +235,14 @@ def _list_of(name, t, n: int, dtype: str) -> None:
                                    f"{None if t is None else (tuple(t.shape), tuple(t.stride()), str(t.dtype))})")
 
 
+def _freqs_of(freqs, n: int, other) -> None:
+    """n frequencies where the call's other tensors are: rotation_freqs leaves them on the host, whose memory no kernel can read unless it is
+    pinned."""
+    _list_of("freqs", freqs, n, "float64")
+    if freqs.device != other.device and not freqs.is_pinned():
+        raise AslError(ASL_EINVAL, f"freqs must be on {other.device}, where pos is (it is on {freqs.device})")
+
+
 def _room_of(name, t, n: int, heads: int, d: int, dtype: int) -> None:
     """Room for [n, heads, d] elements of the described type in t, which may have more."""
     if t.shape != (n, heads, d) and any(have < need for have, need in zip(t.shape, (n, heads, d))):
@@ -290,7 +298,7 @@ def make_rotation(Hq: int, Hk: int, d: int, rot_dim: Optional[int] = None, pairs
 
 def rotation_freqs(rot_dim: int, base: float = 10000.0, kind: int = ASL_FREQS_PLAIN, factor: float = 1.0, context: float = 0.0,
                    low: float = 1.0, high: float = 32.0):
-    """[rot_dim / 2] float64 on the host: radians that a position adds to the angle of each pair."""
+    """[rot_dim / 2] float64 on the host (the calls take it on the GPU): radians that a position adds to the angle of each pair."""
     import torch
     out = torch.empty(max(rot_dim, 0) // 2, dtype=torch.float64)
     f = AslFreqs(rot_dim, kind, base, factor, context, low, high)
@@ -449,7 +457,7 @@ class Asl:
         r.q_out_stride_tok, r.q_out_stride_head = _heads_of("q_out", q_out, n, Hq, d, e)
         r.k_out_stride_tok, r.k_out_stride_head = _heads_of("k_out", k_out, n, Hk, d, e)
         _list_of("pos", pos, n, "int32")
-        _list_of("freqs", freqs, r.rot_dim // 2, "float64")
+        _freqs_of(freqs, r.rot_dim // 2, pos)
         self._check(self.lib.asl_rotate(self.h, C.byref(r), _ptr(q), _ptr(k), _ptr(pos), _ptr(freqs), n, _ptr(q_out), _ptr(k_out),
                                         _stream()))
 
@@ -462,7 +470,7 @@ class Asl:
         r.v_stride_tok, r.v_stride_head = _heads_of("v", v, n, Hk, d, e)
         r.q_out_stride_tok, r.q_out_stride_head = _heads_of("q_out", q_out, n, Hq, d, e)
         _list_of("pos", pos, n, "int32")
-        _list_of("freqs", freqs, r.rot_dim // 2, "float64")
+        _freqs_of(freqs, r.rot_dim // 2, pos)
         _list_of("slot", slot, n, "int64")
         self._check(self.lib.asl_rotate_write(self.h, C.byref(pages), C.byref(r), _ptr(q), _ptr(k), _ptr(v), _ptr(pos), _ptr(slot),
                                               _ptr(freqs), n, _ptr(q_out), _ptr(k_pages), _ptr(v_pages), _stream()))

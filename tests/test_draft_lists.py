@@ -39,6 +39,21 @@ def test_tensors_of_smaller_elements_are_refused(recorded):
         recorded.lib.seen.clear()
 
 
+def test_frequencies_of_the_host_are_refused(recorded):
+    """rotation_freqs gives them there; the other tensors stand for the GPU's."""
+    import torch
+    r, pages = libasl.make_rotation(4, 2, 8), libasl.make_pages(4, 2, 8, 16, 1, 1, 1)
+    there = lambda *s, dtype=torch.bfloat16: torch.zeros(s, dtype=dtype, device="meta")
+    q, k, pos, slot = there(3, 4, 8), there(3, 2, 8), there(3, dtype=torch.int32), there(3, dtype=torch.int64)
+    f = libasl.rotation_freqs(8)
+    for call in (lambda f: recorded.asl_rotate(r, q, k, pos, f, q, k), lambda f: recorded.asl_rotate_write(pages, r, q, k, k, pos, slot, f, q, k, k)):
+        with pytest.raises(libasl.AslError, match="freqs") as e:
+            call(f)
+        assert e.value.status == libasl.ASL_EINVAL and not recorded.lib.seen
+        call(f.to("meta"))
+        recorded.lib.seen.clear()
+
+
 def _wrong(n):
     """What is no list of n int32 one behind the other."""
     import torch

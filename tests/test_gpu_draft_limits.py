@@ -115,6 +115,17 @@ def test_rotations_of_other_types_are_refused(ctx, gpu_device):
         assert all(bool((x == 1).all()) for x in t[right]) and all(bool((x == 0).all()) for x in pages)
 
 
+def test_frequencies_of_the_host_are_refused(ctx, gpu_device):
+    torch = _torch()
+    q, pos, f, r = torch.ones((3, 4, 64), dtype=torch.bfloat16, device=gpu_device), _ints([0, 0, 0], gpu_device), asl.rotation_freqs(64), asl.make_rotation(4, 0, 64)
+    with pytest.raises(asl.AslError, match="freqs"):
+        ctx.asl_rotate(r, q, None, pos, f, torch.zeros_like(q), None)
+    for there in (f.to(gpu_device), f.pin_memory()):
+        out = torch.zeros_like(q)
+        ctx.asl_rotate(r, q, None, pos, there, out, None)
+        assert torch.equal(out, q)
+
+
 # ------------------------------------------------------------------------------------------------------------- attention
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("tree", [True, False])
