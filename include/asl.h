@@ -446,7 +446,8 @@ asl_status asl_rotate_write(asl_ctx* ctx, const asl_pages* pages, const asl_rota
 
 /* A batch from its requests' lengths alone: rows rows[i] become add[i] tokens longer, as by asl_pages_grow, and of every new token comes its
  * place.  Request i's tokens are cu[i] .. cu[i+1]-1.
- *   parent [total] int32 or NULL: the tokens are drafts, and a node's position is by its depth.  NULL: one token behind the other.
+ *   parent [total] int32 or NULL: the tokens are drafts, and a node's position is by its depth.  NULL: one token behind the other.  A draft
+ *          of more than 16384 nodes is out of range, like a row that is none (attention takes 512).
  *   pruned [n_rows] int32 or NULL: tokens that pruning has taken out of each row, i.e. position minus place of its last tokens.
  *   cu     [n+1] int32 out, also where n is 0.  total: room for tokens; the first request that does not fit in it whole, and all behind it,
  *          get none (and raise the fault word).

@@ -104,7 +104,8 @@ __global__ void __launch_bounds__(kBookThreads) pages_plan_kernel(PlanArgs a) {
     a.cu[i + 1] = end;
     if (FILL) l.cu[i + 1] = end;
     // (a request that does not fit in the tokens that there is room for is left out like one that is out of range)
-    if (upto[u] > room || !g[u].take(m, a.kv_len, row[u], add[u])) bad = true;
+    const bool too_long = a.parent != nullptr && add[u] > kPlanNodes;
+    if (upto[u] > room || too_long || !g[u].take(m, a.kv_len, row[u], add[u])) bad = true;
   }
   if (threadIdx.x == 0) {
     a.cu[0] = 0;
@@ -166,8 +167,8 @@ __global__ void __launch_bounds__(kFillThreads) pages_plan_fill_kernel(PlanArgs 
   const int4 f = a.placed[i];
   bool bad = false;
   int depth = j - c0;
-  if (a.parent != nullptr && in) {
-    int k = depth;
+  if (a.parent != nullptr && in && f.x >= 0) {
+    int k = depth;                         // (less than kPlanNodes, or the request is out of range)
     depth = -1;
     while (k >= 0) {                       // (a parent stands before its node: the walk ends)
       ++depth;

@@ -19,6 +19,7 @@ constexpr int kMaxFresh = 65536;           // pages that one call takes
 constexpr int kCutRows = 131072;           // rows of partial results beside one for each row's own and shared keys
 constexpr int kPagedMaxDim = 256;          // head_dim of asl_paged_attention
 constexpr int kTreeNodes = 512;            // nodes of a draft (asl_tree_attention, asl_pages_accept)
+constexpr int kPlanNodes = 16384;          // nodes of a draft (asl_pages_plan): a node's depth is a walk of as many loads that depend on each other
 constexpr int kTreeWords = kTreeNodes / 32;
 constexpr int kPagedRowsHeld = 131072;     // query rows beyond which the workspace does not grow
 constexpr int kPagedKept = 7;              // workspaces that a context outgrows at most (see room_for)

@@ -6,7 +6,7 @@ import pytest
 
 from oracle import draft_oracle as do
 from paper_2601_07667_amd import asl
-from test_gpu_draft import _accepted, _longs, _same_pages
+from test_gpu_draft import _accepted, _Book, _longs, _same_pages
 from test_gpu_paged import Cache, _dt, _ints, _torch
 
 pytestmark = pytest.mark.gpu
@@ -49,6 +49,29 @@ def test_accept_takes_an_empty_list_of_slots_for_a_list(ctx, gpu_device, binding
     ctx.asl_pages_accept(c.desc(), k_ptrs, v_ptrs, 1, rows, _ints([0, 10, 20], dev), path, _ints([2, 2], dev), 2, c.table, c.kv_len, c.refs)
     _same_pages(c, want[0])
     assert c.kv_len.tolist() == [32, 82] and ctx.asl_device_fault() == 0
+
+
+# ------------------------------------------------------------------------------------------------------------------ plan
+def test_plan_of_drafts_that_are_too_long(ctx, gpu_device):
+    """More than 16384 nodes are out of range, since a node's depth is a walk over its ancestors; as many are not, nor more tokens that are no
+    draft."""
+    most = 16384
+    for first in (most, most + 1):
+        for tree in (True, False):
+            b = _Book(gpu_device, 3, 1100, 16, 2300, [3, 7, 5], seed=first)
+            add, rows = [first, 5, 2], [2, 0, 1]
+            chain = list(range(-1, first - 1)) + [-1, 0, 0, 2, -1] + [-1, 0]
+            if not tree or first == most:
+                b.check(ctx, rows, add, parent=chain if tree else None, pruned=[10, 20, 30])
+                assert ctx.asl_device_fault() == 0
+                continue
+            cu, slot, pos = b.plan(ctx, rows, add, sum(add), parent=chain, pruned=[10, 20, 30])
+            assert ctx.asl_device_fault() == 2 and list(cu) == [0, first, first + 5, first + 7]
+            assert np.all(slot[:first] == -1) and np.all(pos[:first] == -1) and b.d_kv.tolist() == [8, 9, 5]
+            at = b.table[[0, 1], 0] * 16
+            assert list(slot[first:]) == [at[0] + 3 + i for i in range(5)] + [at[1] + 7, at[1] + 8]
+            assert list(pos[first:]) == [13 + x for x in (0, 1, 1, 2, 0)] + [27, 28]
+            np.testing.assert_array_equal(b.d_refs.cpu().numpy(), b.refs)
 
 
 # ---------------------------------------------------------------------------------------------------------------- rotate
