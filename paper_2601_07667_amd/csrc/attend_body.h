@@ -306,13 +306,10 @@ __device__ __forceinline__ bool find_item(const AttendArgs& a, const AttendCut& 
   out->tile = (int)(tiles - 1u - (e / (uint32_t)a.Hk) % tiles);    // causal: the longest first
   out->split = (int)(e / (uint32_t)a.Hk / tiles);
   if (TREE && tiles > 1 && a.Hk < 8) {
-    // Items of the same keys a multiple of 8 apart, so that a die's L2 has them for all of their row tiles: as many splits in turn as make 8
-    // with the heads (60 nodes of 7 heads a group behind 131089 keys, 4 heads: 193 us with the tiles in turn, 187 so).
-    const uint32_t by = (8u + (uint32_t)a.Hk - 1u) / (uint32_t)a.Hk, block = (uint32_t)a.Hk * tiles * by;
-    const uint32_t k = e / block, at = (e - k * block) / (uint32_t)a.Hk;
-    const uint32_t n = min(by, (uint32_t)out->splits - k * by);
-    out->tile = (int)(tiles - 1u - at / n);
-    out->split = (int)(k * by + at % n);
+    uint32_t tile, split;
+    tree_turn(e, (uint32_t)a.Hk, tiles, (uint32_t)out->splits, &tile, &split);
+    out->tile = (int)tile;
+    out->split = (int)split;
   }
   out->slot = is_partial(s, out->splits) ? (int64_t)slot : -1;
   return out->slot < 0 || (int64_t)slot + (int64_t)s.rows * a.Hk * out->splits <= cut.cap;

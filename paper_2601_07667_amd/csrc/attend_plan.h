@@ -45,6 +45,17 @@ ASL_HD int64_t max_items(const AttendCut& c, int64_t rows, int64_t segments, int
   return c.target + Hk * (rows / c.rows + segments);
 }
 
+// Row tile and split of item e of a tree's segment, whose head is e % Hk, for Hk < 8.  Items of the same keys are to be a multiple of 8 apart,
+// so that one die's L2 has the keys for all their row tiles: as many splits take turns as make a multiple of 8 with the heads.  (Not in the
+// last turns where those are fewer.)  60 nodes of 7 heads a group behind 131089 keys, us, with the row tiles in turn and so: 4 heads 193, 187;
+// with 3 splits in turn for 3 heads, 2 for 5 to 7, and so: 3 heads 141, 126; 5 300, 261; 6 307, 303; 7 402, 342.
+ASL_HD void tree_turn(uint32_t e, uint32_t Hk, uint32_t tiles, uint32_t splits, uint32_t* tile, uint32_t* split) {
+  const uint32_t by = Hk % 4 == 0 ? 2u : Hk % 2 == 0 ? 4u : 8u, block = Hk * tiles * by;
+  const uint32_t k = e / block, at = (e - k * block) / Hk, left = splits - k * by, n = by < left ? by : left;
+  *tile = tiles - 1u - at / n;
+  *split = k * by + at % n;
+}
+
 // Items of a launch: 256 threads each.  One of 2^32 threads or more in x does not fail: it runs with their number modulo 2^32.
 constexpr int64_t kMostItems = (int64_t(1) << 32) / 256;
 
