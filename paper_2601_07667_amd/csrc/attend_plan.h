@@ -101,7 +101,9 @@ ASL_HD AttendCut cut_for(bool tiles, int64_t rows, int64_t keys, int64_t segment
 // The same for drafted trees, which have tiles of 128 rows alone (attend_steps.h).  An item takes 10 us to begin and its pieces 9 to 16 to be
 // joined, so where there are tiles for three quarters of the units a span of up to 128 key tiles is one piece (32 sequences of 2300
 // keys, 16 to 32 nodes, 8 heads: 82 us, in two pieces each 108).  Where by the caller's word no sequence is longer than that, every span is
-// one (one item in all is wanted), however many keys it turns out to have, and no launch looks for pieces to join (83 us, 80 so).  Where there
+// one (one item in all is wanted), however many keys it turns out to have, and no launch looks for pieces to join (83 us, 80 so).  The tiles are
+// counted as if every draft had as many nodes as the caller states for the longest: few and uneven ones are not cut either, and take longer
+// (drafts of 200, 8, 8 and 8 nodes on 8192 keys, 4 heads a group, 8 heads: 180 us, apart 76 and 39).  Where there
 // are fewer tiles, spans are cut for two items a unit (60 nodes on 131089 keys, 4 heads: 186 us, with 384 items 196, with 256 207).  Shared
 // ones into about 192 (8 prompts of 2090 keys for 6 sequences each: 46.6 us, with 128 46.8, with 256 47.5, with 384 54.5, with 96 64).
 ASL_HD AttendCut cut_for_tree(bool tiles, int64_t rows, int64_t keys, int64_t segments, int Hk, bool shared) {
@@ -130,8 +132,9 @@ ASL_HD AttendRule rule_for(bool tiles, int64_t total_q, int G, int Hk, int n_seq
   r.own = (tree ? cut_for_tree : cut_for)(tiles, r.most, max_kv_len, n_seqs, Hk, false);
   r.shared = (tree ? cut_for_tree : cut_for)(tiles, n_groups > 0 ? rows / n_groups : 0, max_kv_len, n_groups, Hk, true);
   r.shared.cap = max_partials(r.shared, rows, Hk);
-  // a sequence whose own rows fill a tile gains nothing (drafts: fill more than one), and groups cannot save more than all sequences' keys but one each (kMinSaved);
-  // every row of a group is joined from two parts, for which there has to be room
+  // a sequence whose own rows fill a tile reads its keys once for all of them; groups cannot save more than all sequences' keys but one each
+  // (kMinSaved).  Drafts share up to one tile of rows, a bound that was not measured out: just above it sharing would pay (64 sequences behind
+  // 33024 keys, 4 heads a group: 32 nodes 1183 us, 33 nodes, each reading the prefix for two tiles of rows, 1846).  And every row of a group is joined from two parts, for which there has to be room
   const double most_saved = (double)(n_seqs - n_groups) * (double)max_kv_len * (double)key_bytes;
   r.groups = n_groups > 0 && (tree ? r.most <= kTile2 : r.own.rows != kTile2) && most_saved >= (double)kMinSaved && r.shared.cap + rows * Hk <= room;
   if (!r.groups) r.shared.cap = 0;

@@ -63,7 +63,7 @@ __device__ __forceinline__ unsigned long long block_scan(unsigned long long x, P
 
 // The requests' pages, where their tokens begin, and (FILL) each token's slot and position: one workgroup, bound by the latency of loads
 // that depend on each other (requests, lengths, counts, pages).  A draft's parents are taken to LDS, where a node's depth is a walk.
-// 64 drafts of 5 to 32 nodes 13 to 14 us, 24 prompts 8 and 3 for the launch that fills in their tokens.
+// 64 drafts of 5 to 32 nodes 13 to 15 us, 24 prompts 8 to 10 and 3 to 4 for the launch that fills in their tokens.
 template <bool FILL>
 __global__ void __launch_bounds__(kBookThreads) pages_plan_kernel(PlanArgs a) {
   __shared__ PlanLds l;
