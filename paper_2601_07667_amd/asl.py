@@ -236,10 +236,10 @@ def _list_of(name, t, n: int, dtype: str) -> None:
 
 
 def _freqs_of(freqs, n: int, other) -> None:
-    """n frequencies where the call's other tensors are: rotation_freqs leaves them on the host, whose memory no kernel can read unless it is
-    pinned."""
+    """n frequencies, not on the host where the call's other tensors are not: rotation_freqs leaves them there, and no kernel can read its
+    memory unless it is pinned."""
     _list_of("freqs", freqs, n, "float64")
-    if freqs.device != other.device and not freqs.is_pinned():
+    if not freqs.is_cuda and freqs.device != other.device and not freqs.is_pinned():
         raise AslError(ASL_EINVAL, f"freqs must be on {other.device}, where pos is (it is on {freqs.device})")
 
 

@@ -144,9 +144,11 @@ def test_frequencies_of_the_host_are_refused(ctx, gpu_device):
     with pytest.raises(asl.AslError, match="freqs"):
         ctx.asl_rotate(r, q, None, pos, f, torch.zeros_like(q), None)
     for there in (f.to(gpu_device), f.pin_memory()):
-        out = torch.zeros_like(q)
-        ctx.asl_rotate(r, q, None, pos, there, out, None)
-        assert torch.equal(out, q)
+        for at in (pos, pos.cpu().pin_memory()):
+            out = torch.zeros_like(q)
+            ctx.asl_rotate(r, q, None, at, there, out, None)
+            torch.cuda.synchronize()
+            assert torch.equal(out, q)
 
 
 # ------------------------------------------------------------------------------------------------------------- attention
