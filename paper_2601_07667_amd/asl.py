@@ -22,6 +22,7 @@ ASL_PAIRS_HALVES, ASL_PAIRS_NEIGHBOURS = 0, 1
 ASL_ROTATE_BACK = 1
 ASL_FREQS_PLAIN, ASL_FREQS_LINEAR, ASL_FREQS_BASE, ASL_FREQS_PARTS = 0, 1, 2, 3
 PAGED_MAX_SEQS = 4096                                      # a call of more sequences is refused before it reads any list
+PAGED_MAX_LAYERS = 16384                                   # and one of more layers
 _STATUS = {0: "ASL_OK", -1: "ASL_EINVAL", -2: "ASL_ENOMEM", -3: "ASL_EHIP", -4: "ASL_EUNSUPPORTED"}
 
 EXPORTS = ["asl_create", "asl_destroy", "asl_last_error", "asl_workspace_bytes", "asl_score_layer",
@@ -232,6 +233,13 @@ def _list_of(name, t, n: int, dtype: str) -> None:
         return
     if t is None or t.numel() < n or t.dtype is not (_TYPES or _types())[dtype] or not t.is_contiguous():
         raise AslError(ASL_EINVAL, f"{name} must be {n} x {dtype} without gaps (it is "
+                                   f"{None if t is None else (tuple(t.shape), tuple(t.stride()), str(t.dtype))})")
+
+
+def _pointers_of(name, t, n: int) -> None:
+    """Room for n pointers, which the call follows."""
+    if n > 0 and (t is None or t.numel() * t.element_size() < 8 * n or not t.is_contiguous()):
+        raise AslError(ASL_EINVAL, f"{name} must be {n} x int64 without gaps (it is "
                                    f"{None if t is None else (tuple(t.shape), tuple(t.stride()), str(t.dtype))})")
 
 
@@ -523,6 +531,9 @@ class Asl:
             _list_of("rows", rows, n, "int32")
             _list_of("cu", cu, n + 1, "int32")
             _list_of("n_path", n_path, n, "int32")
+        if 0 < n and n_layers <= PAGED_MAX_LAYERS:
+            _pointers_of("k_ptrs", k_ptrs, n_layers)
+            _pointers_of("v_ptrs", v_ptrs, n_layers)
         slots, total = None, 0
         if slot is not None:
             total = slot.numel()

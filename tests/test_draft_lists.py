@@ -119,3 +119,19 @@ def test_tensors_of_tree_attention_are_checked(recorded):
     call(libasl.make_attn(3, 5, 5, 10), group_start=None, prefix_len=None)
     call(libasl.make_attn(4097, 5, 5, 10))                   # (refused by the call, for its size)
     assert len(recorded.lib.seen) == 5
+
+
+def test_pointers_of_accepting_are_checked(recorded):
+    """A list of fewer pointers than layers would be read past its end, and what stands there be followed."""
+    import torch
+    pages, i, path = libasl.make_pages(4, 2, 8, 16, 1, 1, 1), torch.zeros(4, dtype=torch.int32), torch.zeros(2, 4, dtype=torch.int32)
+    p = torch.zeros(3, dtype=torch.int64)
+    accept = lambda k, v, layers, n=2: recorded.asl_pages_accept(pages, k, v, layers, i, i, path, i, n, i, i, i)
+    for bad in (p[:2], p.int(), torch.zeros(6, dtype=torch.int64)[::2], None):
+        for name, args in (("k_ptrs", (bad, p)), ("v_ptrs", (p, bad))):
+            with pytest.raises(libasl.AslError, match=name) as e:
+                accept(*args, 3)
+            assert e.value.status == libasl.ASL_EINVAL
+    assert not recorded.lib.seen
+    accept(p, p, 3), accept(None, None, 0), accept(None, None, 3, 0), accept(p, p, 16385)     # (the last is refused by the call, for its size)
+    assert len(recorded.lib.seen) == 4
